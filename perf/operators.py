@@ -109,7 +109,7 @@ def draw(rng):
                      ragged=rng.choice((0.0, 0.3, 0.8, 0.95)))
             c["empty"] = c["batch"] > 1 and rng.random() < 0.3
             if op in ("top", "attend"):
-                c["top"] = _log_int(rng, 2, 300)
+                c["top"] = _log_int(rng, 4 if op == "top" else 2, 300)
             if op == "top" and c["tokens"] < 2 * c["top"] * c["page"]:
                 continue                                # the longest sequence has something to leave out
             if op == "bounds":
