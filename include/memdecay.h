@@ -436,6 +436,138 @@ md_status md_attend_mass_noalloc(const void *kv_pool_dev, const int32_t *block_t
                                  int num_kv_heads, int page_size, int max_pages_per_seq,
                                  int num_phys_pages, void *stream);
 
+/* ---- rows for the cache: head norms and rotation ---------------------- */
+
+/* The paper has no counterpart to the calls from here to the end of the
+ * header.  The calls of this section make the query, key and value rows that
+ * md_decode_* and md_append_tokens take out of a projection's output. */
+enum {
+  MD_TYPE_BF16 = 0,
+  MD_TYPE_F16 = 1,
+  MD_TYPE_F32 = 2
+};
+#define MD_MAX_AXES 4             /* position axes of a rotation */
+
+/* Writes the table of a rotation: table[pos][i] = scale * (cos, sin) of
+ * pos * inv_freq[i], computed in 64 bits and rounded once, for the positions
+ * 0 .. table_len - 1 and the rotary_dim / 2 channel pairs.
+ *   inv_freq_host  double [rotary_dim / 2]            (host, read before return)
+ *   table_dev      fp32 [table_len][rotary_dim / 2][2] (device, written, 16-byte
+ *                  aligned)
+ * rotary_dim as in md_norm_rope. */
+md_status md_rope_table(const double *inv_freq_host, int rotary_dim, int table_len, double scale,
+                        float *table_dev, void *stream);
+
+/* One layer's rows, from a projection's output to what the cache takes, in one
+ * pass.  For every token and every query and key head, x being its 128
+ * elements:
+ *   y = x / sqrt(mean(x^2) + eps) * weight   (weight NULL: y = x)
+ * then, for each pair i < rotary_dim / 2 of channels (a, b), (i, i + rotary_dim / 2)
+ * or, if interleaved, (2i, 2i + 1), with (c, s) = table[positions[axis_i][token]][i]:
+ *   out_a = y_a c - y_b s,  out_b = y_b c + y_a s
+ * and out = y in the channels from rotary_dim on.  Value rows are copied.  All
+ * arithmetic is in 32 bits, rounded once to the bf16 outputs.
+ * Rows lie anywhere: element (token, head, d) of x is x[token * x_token +
+ * head * x_head + d] (strides in elements), so the inputs may be parts of one
+ * fused projection output, and the outputs one layer's part of a step's
+ * [batch][L][H][D] or a prompt's [L][Hkv][n][D].  Inputs: bases 8-byte aligned
+ * (fp32: 16), outputs 8; strides multiples of 4.  An output may be the input it
+ * is made from (same address, type and strides); any other overlap is an error
+ * of the caller's.
+ * A position outside [0, table_len) makes the token's rotated channels NaN. */
+typedef struct {
+  int n_tokens;                /* 0: nothing is done */
+  int num_q_heads, num_kv_heads; /* either may be 0; its pointers are then not read */
+  int type;                    /* of q, k and v: MD_TYPE_* */
+  int rotary_dim;              /* a multiple of 8 in [0, 128]; 0: no rotation */
+  int interleaved;
+  int num_axes;                /* rows of positions: 1 .. MD_MAX_AXES */
+  int table_len;
+  float eps;
+  const void *q, *k, *v;       /* (device); v NULL: no value rows */
+  void *q_out, *k_out, *v_out; /* bf16 (device, written) */
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head;
+  int64_t q_out_token, q_out_head, k_out_token, k_out_head, v_out_token, v_out_head;
+  const float *q_weight, *k_weight; /* fp32 [128] (device, 16-byte aligned) or NULL */
+  const float *table;          /* as md_rope_table writes it (device) */
+  const int32_t *positions;    /* [num_axes][n_tokens] (device) */
+  const uint8_t *axis_host;    /* [rotary_dim / 2] axis of each pair (host, read
+                                  before return), or NULL: axis 0 */
+  void *stream;                /* cudaStream_t */
+} md_norm_rope_args;
+md_status md_norm_rope(const md_norm_rope_args *args);
+
+/* ---- attention over selected pages ------------------------------------ */
+
+/* Decode attention that reads, per (sequence, layer, KV head), only the pages
+ * whose tokens may matter to the new token.  Each page keeps the channelwise
+ * least and largest of its keys; with them a query's logit on any of its tokens
+ * is bounded without reading the keys; the pages with the highest bounds are
+ * attended.  A page of 16 (32) tokens costs 512 bytes to score and 8 (16) KiB
+ * to attend.  md_sparse_enable puts this into the decode calls of a handle; the
+ * calls below run its parts over a cache that the caller owns:
+ *   kv_pool_dev      bf16 [L][num_phys_pages][Hkv][2][page_size][128], 16-byte
+ *                    aligned (md_decode_step's pool)
+ *   block_table_dev  int32 [batch][max_pages_per_seq] physical page ids
+ *   n_tokens_host    [batch] cached tokens per sequence (host, read before
+ *                    return), 0 .. max_pages_per_seq * page_size; a sequence's
+ *                    pages are full up to them
+ *   bounds_dev       bf16 [L][num_phys_pages][Hkv][2][128]: least, largest;
+ *                    16-byte aligned
+ * Limits as md_config's (batch <= MD_MAX_BATCH, Hq / Hkv <= MD_MAX_GROUP, pages
+ * of 16 or 32 tokens).  The calls allocate nothing, keep nothing and enqueue
+ * their work on `stream`.  Block-table entries outside [0, num_phys_pages) are
+ * taken for pages without tokens. */
+
+/* Bounds of the logical pages first_page_host[b] .. of each sequence (NULL:
+ * all): lo = min, hi = max over the page's cached tokens; a NaN key makes its
+ * channel's bounds NaN.  Other pages' bounds are left as they are. */
+md_status md_page_bounds(const void *kv_pool_dev, const int32_t *block_table_dev, const int32_t *n_tokens_host,
+                         const int32_t *first_page_host, void *bounds_dev, int batch, int num_layers,
+                         int num_kv_heads, int page_size, int max_pages_per_seq, int num_phys_pages,
+                         void *stream);
+
+/* scores[b][l][kvh][p] = max over the KV head's query heads h of
+ *   sum_d (max(q_hd, 0) hi_pd + min(q_hd, 0) lo_pd) / sqrt(128)
+ * for the sequence's pages p: at least the logit of any of these heads on any
+ * of the page's tokens.  Entries past a sequence's pages are not written.
+ *   q_dev       bf16 [batch][L][Hq][128]             (16-byte aligned)
+ *   scores_dev  fp32 [batch][L][Hkv][max_pages_per_seq] (written) */
+md_status md_page_scores(const void *q_dev, const void *bounds_dev, const int32_t *block_table_dev,
+                         const int32_t *n_tokens_host, float *scores_dev, int batch, int num_layers,
+                         int num_q_heads, int num_kv_heads, int page_size, int max_pages_per_seq,
+                         int num_phys_pages, void *stream);
+
+/* The pages to attend, per row of scores: all of them where a sequence has at
+ * most top_pages; else the first first_pages, the last last_pages and, of those
+ * between, the ones with the highest scores, top_pages in all (NaN counts as
+ * the highest, ties go to the lower index; the first and last pages' scores are
+ * not read).  Logical page numbers in rising order, -1 behind them.
+ *   page_ids_dev  int32 [batch][L][Hkv][top_pages] (written)
+ * first_pages + last_pages <= top_pages. */
+md_status md_page_top(const float *scores_dev, const int32_t *n_tokens_host, int32_t *page_ids_dev, int batch,
+                      int num_layers, int num_kv_heads, int page_size, int max_pages_per_seq, int top_pages,
+                      int first_pages, int last_pages, void *stream);
+
+/* Attention over the cached tokens of the listed pages, for every layer and
+ * query head, with md_decode_step's arithmetic but for the softmax weights, which
+ * enter the product with V as two bf16 terms each; entries outside a sequence's
+ * pages (-1) are skipped, and a row that lists no token yields zeros.
+ *   page_ids_dev  int32 [batch][L][Hkv][top_pages], each page at most once
+ *   q_dev         bf16 [batch][L][Hq][128] (16-byte aligned)
+ *   out_dev       bf16 [batch][L][Hq][128] (written)
+ *   mass_dev      fp32 [batch][L][Hkv][top_pages][page_size], or NULL: for every
+ *                 token of the listed pages, the sum over the KV head's query
+ *                 heads of their softmax weight on it; 0 at entries and slots
+ *                 without a token
+ * top_pages * page_size <= MD_MAX_TOP_TOKENS. */
+#define MD_MAX_TOP_TOKENS 65536
+md_status md_attend_pages(const void *q_dev, const void *kv_pool_dev, const int32_t *block_table_dev,
+                          const int32_t *n_tokens_host, const int32_t *page_ids_dev, void *out_dev,
+                          float *mass_dev, int batch, int num_layers, int num_q_heads, int num_kv_heads,
+                          int page_size, int max_pages_per_seq, int num_phys_pages, int top_pages,
+                          void *stream);
+
 #ifdef __cplusplus
 }
 #endif

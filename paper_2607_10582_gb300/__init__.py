@@ -45,6 +45,9 @@ MD_MAX_CHUNK_TOKENS = 4096
  MD_STATE_T_INS, MD_STATE_PAGE_FILL, MD_STATE_SEQ_TOKENS, MD_STATE_CALIB) = range(15)
 MD_CALIB_BUCKETS = 256
 MD_CALIB_BUCKET_WIDTH = 4
+MD_TYPE_BF16, MD_TYPE_F16, MD_TYPE_F32 = range(3)
+MD_MAX_AXES = 4
+MD_MAX_TOP_TOKENS = 65536
 (MD_QUERY_TOKENS, MD_QUERY_PAGES, MD_QUERY_FREE_TOP, MD_QUERY_STEP, MD_QUERY_WINDOW,
  MD_QUERY_PINNED_PAGES) = range(6)
 (MD_DEBUG_SPIN_LIMIT_NS, MD_DEBUG_EXTRA_ARRIVALS, MD_DEBUG_GRID_LIMIT, MD_DEBUG_UNIT_OVERHEAD,
@@ -65,6 +68,17 @@ class md_config(ctypes.Structure):
         ("random_seed", ctypes.c_uint64),
         ("region_aligned_pages", ctypes.c_int),
     ]
+
+
+class md_norm_rope_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("n_tokens", "num_q_heads", "num_kv_heads", "type", "rotary_dim",
+                                             "interleaved", "num_axes", "table_len")] +
+                [("eps", ctypes.c_float)] +
+                [(n, ctypes.c_void_p) for n in ("q", "k", "v", "q_out", "k_out", "v_out")] +
+                [(n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head",
+                                               "q_out_token", "q_out_head", "k_out_token", "k_out_head",
+                                               "v_out_token", "v_out_head")] +
+                [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "table", "positions", "axis_host", "stream")])
 
 
 # name -> (restype, argtypes); the names and order of include/memdecay.h
@@ -96,6 +110,12 @@ SIGNATURES = {
     "md_last_error": (_c.c_char_p, [_P]),
     "md_attend_mass_noalloc": (_c.c_int, [_P, _P, _P, _P, _P, _P, _c.c_int, _c.c_int, _c.c_int, _c.c_int,
                                           _c.c_int, _c.c_int, _c.c_int, _P]),
+    "md_rope_table": (_c.c_int, [_P, _c.c_int, _c.c_int, _c.c_double, _P, _P]),
+    "md_norm_rope": (_c.c_int, [_c.POINTER(md_norm_rope_args)]),
+    "md_page_bounds": (_c.c_int, [_P] * 5 + [_c.c_int] * 6 + [_P]),
+    "md_page_scores": (_c.c_int, [_P] * 5 + [_c.c_int] * 7 + [_P]),
+    "md_page_top": (_c.c_int, [_P] * 3 + [_c.c_int] * 8 + [_P]),
+    "md_attend_pages": (_c.c_int, [_P] * 7 + [_c.c_int] * 8 + [_P]),
 }
 
 _lib = None
@@ -199,6 +219,183 @@ def md_calib_fit(mass_sum: np.ndarray, count: np.ndarray, bucket_width: int = MD
     if st != MD_OK:
         raise MemDecayError(st, "md_calib_fit")
     return rate, half
+
+
+# ---- rows for the cache, attention over selected pages: calls without a handle ----
+def _bad(what: str):
+    raise MemDecayError(MD_ERR_INVALID_ARG, what)
+
+
+def _on(t, stream):
+    """The stream a call on tensor t goes to (default: the current one of its device)."""
+    import torch
+    if not t.is_cuda:
+        _bad("device tensors expected")
+    if t.device.index != torch.cuda.current_device():
+        _bad(f"tensors on {t.device}, which is not the current device")
+    return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+
+
+def _dense(name, t, shape, size):
+    """Address of a contiguous device tensor of this shape and element size."""
+    if tuple(t.shape) != tuple(shape) or t.element_size() != size or not t.is_contiguous() or not t.is_cuda:
+        _bad(f"{name}: a contiguous device tensor {tuple(shape)} of {size}-byte elements expected, "
+             f"not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _status(st: int, what: str):
+    if st != MD_OK:
+        raise MemDecayError(st, what)
+
+
+def md_rope_table(inv_freq, table_len: int, *, scale: float = 1.0, stream=None):
+    """Table of a rotation, fp32 [table_len][rotary_dim / 2][2] on the current device:
+    scale * (cos, sin) of pos * inv_freq[i], from 64-bit angles.  inv_freq: float64
+    [rotary_dim / 2] on the host."""
+    import torch
+    f, p = _host(inv_freq, np.float64)
+    if f.ndim != 1 or table_len < 1:
+        _bad("inv_freq must have one dimension, table_len must be positive")
+    out = torch.empty((table_len, f.size, 2), dtype=torch.float32, device="cuda")
+    _status(lib().md_rope_table(p, 2 * f.size, table_len, scale, out.data_ptr(), _on(out, stream)), "md_rope_table")
+    return out
+
+
+def _row_types():
+    import torch
+    return {torch.bfloat16: MD_TYPE_BF16, torch.float16: MD_TYPE_F16, torch.float32: MD_TYPE_F32}
+
+
+def md_norm_rope(q, k, v, q_out, k_out, v_out, *, positions, table, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 axes=None, interleaved: bool = False, stream=None):
+    """One layer's rows from a projection's output to what the cache takes: head norms
+    (where a weight is given), rotation by position, layout; see md_norm_rope in the header.
+      q, k, v      [tokens][heads][128] bf16, f16 or f32, any strides over tokens and heads
+                   (parts of one fused tensor); q, or k and v, or v alone may be None
+      *_out        the same shapes in bf16 (or its raw bits), any such strides; written
+      positions    int32 [tokens] or [num_axes][tokens]
+      table        md_rope_table's, or None: no rotation
+      axes         uint8 [rotary_dim / 2] on the host: the axis of each pair (None: the first)
+      weights      fp32 [128]"""
+    a = md_norm_rope_args()
+    types = _row_types()
+    first = q if q is not None else k
+    if first is None:
+        _bad("neither q nor k")
+    T = first.shape[0]
+    for name, x, y in (("q", q, q_out), ("k", k, k_out), ("v", v, v_out)):
+        if x is None:
+            continue
+        if x.dim() != 3 or x.shape[0] != T or x.shape[2] != MD_HEAD_DIM or x.dtype != first.dtype or not x.is_cuda:
+            _bad(f"{name}: {T} tokens of heads of 128 elements, of {first.dtype}, expected")
+        if y is None or y.shape != x.shape or y.element_size() != 2 or not y.is_cuda:
+            _bad(f"{name}_out: bf16 of the shape of {name} expected")
+        if x.numel() and (x.stride(2) != 1 or y.stride(2) != 1):
+            _bad(f"{name}: the elements of a row must be adjacent")
+        setattr(a, name, x.data_ptr())
+        setattr(a, name + "_out", y.data_ptr())
+        for n, s, dim in (("_token", x, 0), ("_head", x, 1), ("_out_token", y, 0), ("_out_head", y, 1)):
+            setattr(a, name + n, s.stride(dim) if s.shape[dim] > 1 else 0)
+    if first.dtype not in types:
+        _bad(f"rows of {first.dtype}")
+    if v is not None and (k is None or v.shape != k.shape):
+        _bad("v must have k's shape")
+    a.n_tokens, a.type, a.eps, a.interleaved = T, types[first.dtype], eps, int(interleaved)
+    a.num_q_heads = q.shape[1] if q is not None else 0
+    a.num_kv_heads = k.shape[1] if k is not None else 0
+    if q is not None and q_weight is not None:
+        a.q_weight = _dense("q_weight", q_weight, (MD_HEAD_DIM,), 4)
+    if k is not None and k_weight is not None:
+        a.k_weight = _dense("k_weight", k_weight, (MD_HEAD_DIM,), 4)
+    host = None
+    if table is not None:
+        if table.dim() != 3:
+            _bad("table: [positions][pairs][2] expected")
+        a.table = _dense("table", table, (table.shape[0], table.shape[1], 2), 4)
+        a.table_len, a.rotary_dim = table.shape[0], 2 * table.shape[1]
+        a.num_axes = positions.shape[0] if positions.dim() == 2 else 1
+        a.positions = _dense("positions", positions, (a.num_axes, T) if positions.dim() == 2 else (T,), 4)
+        if axes is not None:
+            host, a.axis_host = _host(axes, np.uint8)
+            if host.size < table.shape[1]:
+                _bad(f"{host.size} axes for {table.shape[1]} pairs")
+    a.stream = _on(first, stream)
+    _status(lib().md_norm_rope(ctypes.byref(a)), "md_norm_rope: head counts, alignment or strides")
+
+
+def _counts(n_tokens, batch: int):
+    n, p = _host(n_tokens, np.int32)
+    if n.size < batch:
+        _bad(f"{n.size} token counts for a batch of {batch}")
+    return n, p
+
+
+def _table_shape(block_table):
+    if block_table.dim() != 2:
+        _bad("block_table: [batch][max_pages_per_seq] expected")
+    return block_table.shape
+
+
+def md_page_bounds(pool, block_table, n_tokens, bounds, *, first_pages=None, stream=None):
+    """Channelwise least and largest key of the pages from first_pages[b] on (None: all).
+      pool         bf16 [L][pages][Hkv][2][page_size][128]
+      block_table  int32 [batch][max_pages_per_seq]
+      n_tokens     int32 [batch] on the host
+      bounds       bf16 [L][pages][Hkv][2][128]; written for those pages"""
+    B, P_max = _table_shape(block_table)
+    L, P, Hkv, _, ps, _ = pool.shape
+    n, np_ = _counts(n_tokens, B)
+    f, fp = (None, None) if first_pages is None else _counts(first_pages, B)
+    _status(lib().md_page_bounds(_dense("pool", pool, (L, P, Hkv, 2, ps, MD_HEAD_DIM), 2),
+                                 _dense("block_table", block_table, (B, P_max), 4), np_, fp,
+                                 _dense("bounds", bounds, (L, P, Hkv, 2, MD_HEAD_DIM), 2), B, L, Hkv, ps, P_max, P,
+                                 _on(pool, stream)), "md_page_bounds")
+
+
+def md_page_scores(q, bounds, block_table, n_tokens, scores, *, page_size: int, stream=None):
+    """Per page, the largest logit that any query head of a KV head could have on one of its tokens.
+      q       bf16 [batch][L][Hq][128]
+      bounds  as md_page_bounds writes them
+      scores  fp32 [batch][L][Hkv][max_pages_per_seq]; written for each sequence's pages"""
+    B, P_max = _table_shape(block_table)
+    L, P, Hkv = bounds.shape[:3]
+    Hq = q.shape[2]
+    n, np_ = _counts(n_tokens, B)
+    _status(lib().md_page_scores(_dense("q", q, (B, L, Hq, MD_HEAD_DIM), 2),
+                                 _dense("bounds", bounds, (L, P, Hkv, 2, MD_HEAD_DIM), 2),
+                                 _dense("block_table", block_table, (B, P_max), 4), np_,
+                                 _dense("scores", scores, (B, L, Hkv, P_max), 4), B, L, Hq, Hkv, page_size, P_max, P,
+                                 _on(q, stream)), "md_page_scores")
+
+
+def md_page_top(scores, n_tokens, page_ids, *, page_size: int, first: int = 1, last: int = 1, stream=None):
+    """The pages to attend: the first, the last, and the highest scored of the others.
+      scores    fp32 [batch][L][Hkv][max_pages_per_seq]
+      page_ids  int32 [batch][L][Hkv][top_pages]; written, in rising order, -1 behind them"""
+    B, L, Hkv, P_max = scores.shape
+    top = page_ids.shape[-1]
+    n, np_ = _counts(n_tokens, B)
+    _status(lib().md_page_top(_dense("scores", scores, (B, L, Hkv, P_max), 4), np_,
+                              _dense("page_ids", page_ids, (B, L, Hkv, top), 4), B, L, Hkv, page_size, P_max, top,
+                              first, last, _on(scores, stream)), "md_page_top")
+
+
+def md_attend_pages(q, pool, block_table, n_tokens, page_ids, out, *, mass=None, stream=None):
+    """Attention of one new token per sequence over the listed pages.
+      q, out    bf16 [batch][L][Hq][128]
+      page_ids  int32 [batch][L][Hkv][top_pages]
+      mass      fp32 [batch][L][Hkv][top_pages * page_size] or None; written"""
+    B, P_max = _table_shape(block_table)
+    L, P, Hkv, _, ps, _ = pool.shape
+    Hq, top = q.shape[2], page_ids.shape[-1]
+    n, np_ = _counts(n_tokens, B)
+    _status(lib().md_attend_pages(
+        _dense("q", q, (B, L, Hq, MD_HEAD_DIM), 2), _dense("pool", pool, (L, P, Hkv, 2, ps, MD_HEAD_DIM), 2),
+        _dense("block_table", block_table, (B, P_max), 4), np_, _dense("page_ids", page_ids, (B, L, Hkv, top), 4),
+        _dense("out", out, (B, L, Hq, MD_HEAD_DIM), 2),
+        None if mass is None else _dense("mass", mass, (B, L, Hkv, top * ps), 4), B, L, Hq, Hkv, ps, P_max, P, top,
+        _on(q, stream)), "md_attend_pages")
 
 
 class Cache:

@@ -268,6 +268,46 @@ struct ObserveParams {
 };
 cudaError_t launch_observe(const ObserveParams &p, cudaStream_t s);
 
+/* ------------------------------------------- attention over selected pages */
+/* What the page kernels (md_pages.cu) share.  Layers are counted from the
+ * launch's first one: pool, bounds, q and out point at its part. */
+struct PageSet {
+  const int32_t *block_table;            // [n_seqs][P_max]
+  const uint8_t *page_fill;              // [n_seqs][P_max] tokens per page, or null: full up to n_tokens
+  int L, Hq, Hkv, G, ps, P_phys, P_max, n_seqs;
+  int n_tokens[MD_MAX_BATCH];
+  int n_pages[MD_MAX_BATCH];
+};
+struct BoundsParams : PageSet {
+  const uint16_t *pool;
+  uint16_t *bounds;                      // [L][P_phys][Hkv][2][D]
+  int first[MD_MAX_BATCH];               // pages first[b] .. end[b] - 1 are bounded
+  int start[MD_MAX_BATCH + 1];           // their running count
+};
+cudaError_t launch_bounds(const BoundsParams &p, cudaStream_t s);
+struct PageScoresParams : PageSet {
+  const uint16_t *q, *bounds;
+  float *scores;                         // [n_seqs][L][Hkv][P_max]
+  float scale;                           // 1 / sqrt(D)
+};
+cudaError_t launch_page_scores(const PageScoresParams &p, cudaStream_t s);
+struct PageTopParams {
+  const float *scores;
+  int32_t *ids;                          // [n_seqs][L][Hkv][top]
+  int rows, P_max, top, first, last, n_seqs;   // rows: L * Hkv per sequence
+  int n_pages[MD_MAX_BATCH];
+};
+cudaError_t launch_page_top(const PageTopParams &p, cudaStream_t s);
+struct AttendPagesParams : PageSet {
+  const uint16_t *q, *pool;
+  uint16_t *out;
+  const int32_t *ids;                    // [n_seqs][L][Hkv][top]
+  float *mass;                           // [n_seqs][L][Hkv][top][ps], or null
+  float scale_log2;                      // log2(e) / sqrt(D)
+  int top;
+};
+cudaError_t launch_attend_pages(const AttendPagesParams &p, cudaStream_t s);
+
 /* Launch of a kernel taking one parameter struct, with programmatic stream
  * serialization (the kernel calls pdl_wait() before touching global memory). */
 template <class P>
