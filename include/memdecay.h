@@ -568,6 +568,28 @@ md_status md_attend_pages(const void *q_dev, const void *kv_pool_dev, const int3
                           int page_size, int max_pages_per_seq, int num_phys_pages, int top_pages,
                           void *stream);
 
+/* Puts the selection into the decode calls of a handle (md_decode_step,
+ * md_decode_step_host, md_decode_layer): from the next step on, where a sequence
+ * of the batch holds more than top_pages pages, each (sequence, layer, KV head)
+ * attends the first_pages first, the last_pages last and the highest scored of
+ * its other pages, top_pages in all; steps of shorter sequences are unchanged.
+ * top_pages = 0 turns it off.  last_pages >= 1: the page being written is always
+ * attended.
+ * The step's mass is that of the tokens attended: the others receive none, and
+ * md_evict observes that.  Evicted pages are gone; pages that are not selected
+ * stay, and any later step may select them.
+ *   buffer_dev  md_sparse_bytes() of device memory, 256-byte aligned, the
+ *               caller's, used until another md_sparse_enable or md_destroy has
+ *               passed on the handle's stream: the bounds of every physical page
+ *               and a step's scores and lists
+ * Bounds are made when they are first needed, from the pages' keys: of all pages
+ * after this call (and after md_load_state or md_set_state of the table or the
+ * fills), later of the pages that were filled since.
+ * MD_ERR_STATE inside a layer-by-layer step. */
+size_t md_sparse_bytes(const md_config *cfg, int top_pages);
+md_status md_sparse_enable(md_ctx *ctx, int top_pages, int first_pages, int last_pages, void *buffer_dev,
+                           size_t bytes);
+
 #ifdef __cplusplus
 }
 #endif

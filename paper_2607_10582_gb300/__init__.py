@@ -116,6 +116,8 @@ SIGNATURES = {
     "md_page_scores": (_c.c_int, [_P] * 5 + [_c.c_int] * 7 + [_P]),
     "md_page_top": (_c.c_int, [_P] * 3 + [_c.c_int] * 8 + [_P]),
     "md_attend_pages": (_c.c_int, [_P] * 7 + [_c.c_int] * 8 + [_P]),
+    "md_sparse_bytes": (_c.c_size_t, [_c.POINTER(md_config), _c.c_int]),
+    "md_sparse_enable": (_c.c_int, [_P, _c.c_int, _c.c_int, _c.c_int, _P, _c.c_size_t]),
 }
 
 _lib = None
@@ -590,6 +592,19 @@ class Cache:
         n = np.zeros((MD_NUM_REGIONS, MD_CALIB_BUCKETS), np.int64)
         self._check(lib().md_calib_read(self.h, s.ctypes.data, n.ctypes.data))
         return s, n
+
+    def sparse_enable(self, top_pages: int, first_pages: int = 1, last_pages: int = 1):
+        """md_sparse_enable with a buffer from torch's allocator: decode steps of sequences of
+        more than top_pages pages attend that many of them.  0: off."""
+        buf, p, n = None, None, 0
+        if top_pages:
+            n = int(lib().md_sparse_bytes(ctypes.byref(self.cfg), top_pages))
+            if n:
+                buf = self.torch.empty(n + 256, dtype=self.torch.uint8, device=self.device)
+                buf.record_stream(self.stream)     # steps in flight may use it when it is given up
+                p = (buf.data_ptr() + 255) // 256 * 256
+        self._check(lib().md_sparse_enable(self.h, top_pages, first_pages, last_pages, p, n))
+        self.sparse_buffer = buf
 
     def debug_set(self, key: int, value: int):
         self._check(lib().md_debug_set(self.h, key, value))

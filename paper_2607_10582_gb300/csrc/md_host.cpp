@@ -76,6 +76,11 @@ struct md_ctx {
   int plan_batch = -1, plan_layers = -1, plan_T = 0, plan_G = 0;
   int plan_knobs[5] = {-1, -1, -1, -1, -1};
   bool calib_on = false;     // calibration histogram being gathered
+  struct {                   // md_sparse_enable
+    int top = 0, first = 0, last = 0;   // top 0: off
+    uint8_t *buf = nullptr;
+    std::vector<int> bounded;           // leading pages of each sequence whose bounds are made
+  } sparse;
   int device = 0;
   int pageable_access = 0;   // the device reads and writes pageable host memory coherently
   int zero_copy = 1;         // md_decode_step_host: new K/V and output used in place when reachable
@@ -850,12 +855,114 @@ bool append_inside(const md_ctx *c, int batch, int layers) {
   return items <= 4LL * c->grid_limit && pages * lh <= 100000;
 }
 
+/* Arrays of an md_sparse_enable buffer. */
+struct SparseLayout {
+  size_t bounds, scores, ids, total;
+};
+SparseLayout sparse_layout(const md_config &cf, int top) {
+  const size_t rows = (size_t)cf.max_batch * cf.num_layers * cf.num_kv_heads;
+  SparseLayout s;
+  s.bounds = 0;
+  s.scores = align_up((size_t)cf.num_layers * cf.num_phys_pages * cf.num_kv_heads * 2 * D * 2, 256);
+  s.ids = align_up(s.scores + rows * cf.max_pages_per_seq * 4, 256);
+  s.total = align_up(s.ids + rows * top * 4, 256);
+  return s;
+}
+
+/* Whether a step of this batch selects pages. */
+bool sparse_step(const md_ctx *c, int batch) {
+  if (c->sparse.top == 0) return false;
+  for (int b = 0; b < batch; ++b)
+    if (c->n_pages[b] > c->sparse.top) return true;
+  return false;
+}
+
+/* Stage 1 over selected pages in layers [l0, l0 + L), which the step's new tokens
+ * are in already: bounds of the pages filled since they were last made (never the
+ * page being written, which is attended whatever its bounds), scores, lists,
+ * attention. */
+md_status run_sparse(md_ctx *c, int batch, int l0, int L, const void *q_dev, void *out_dev) {
+  const md_config &cf = c->cfg;
+  const SparseLayout sl = sparse_layout(cf, c->sparse.top);
+  const size_t layer_pages = (size_t)l0 * cf.num_phys_pages * cf.num_kv_heads;
+  PageSet set;
+  set.block_table = ptr<int32_t>(c, c->lay.block_table);
+  set.page_fill = cf.region_aligned_pages ? ptr<uint8_t>(c, c->lay.page_fill) : nullptr;
+  set.L = L;
+  set.Hq = cf.num_q_heads;
+  set.Hkv = cf.num_kv_heads;
+  set.G = cf.num_q_heads / cf.num_kv_heads;
+  set.ps = cf.page_size;
+  set.P_phys = cf.num_phys_pages;
+  set.P_max = cf.max_pages_per_seq;
+  set.n_seqs = batch;
+  BoundsParams bp;
+  PageTopParams tp;
+  bp.start[0] = 0;
+  for (int b = 0; b < batch; ++b) {
+    set.n_tokens[b] = (int)c->n_tokens[b];
+    tp.n_pages[b] = set.n_pages[b] = c->n_pages[b];
+    bp.first[b] = c->sparse.bounded[b];
+    bp.start[b + 1] = bp.start[b] + c->n_pages[b] - 1 - c->sparse.bounded[b];
+  }
+  uint16_t *pool = ptr<uint16_t>(c, c->lay.pool) + layer_pages * 2 * cf.page_size * D;
+  uint16_t *bounds = (uint16_t *)(c->sparse.buf + sl.bounds) + layer_pages * 2 * D;
+  cudaEvent_t e0;
+  prof_begin(c, &e0);
+  (PageSet &)bp = set;
+  bp.pool = pool;
+  bp.bounds = bounds;
+  cudaError_t e = launch_bounds(bp, c->stream);
+  if (e == cudaSuccess) {
+    PageScoresParams sp;
+    (PageSet &)sp = set;
+    sp.q = (const uint16_t *)q_dev;
+    sp.bounds = bounds;
+    sp.scores = (float *)(c->sparse.buf + sl.scores);
+    sp.scale = (float)(1.0 / sqrt((double)D));
+    e = launch_page_scores(sp, c->stream);
+  }
+  if (e == cudaSuccess) {
+    tp.scores = (const float *)(c->sparse.buf + sl.scores);
+    tp.ids = (int32_t *)(c->sparse.buf + sl.ids);
+    tp.rows = L * cf.num_kv_heads;
+    tp.P_max = cf.max_pages_per_seq;
+    tp.top = c->sparse.top;
+    tp.first = c->sparse.first;
+    tp.last = c->sparse.last;
+    tp.n_seqs = batch;
+    e = launch_page_top(tp, c->stream);
+  }
+  if (e == cudaSuccess) {
+    AttendPagesParams ap;
+    (PageSet &)ap = set;
+    ap.q = (const uint16_t *)q_dev;
+    ap.pool = pool;
+    ap.out = (uint16_t *)out_dev;
+    ap.ids = tp.ids;
+    ap.mass = nullptr;
+    ap.mass_acc = ptr<unsigned long long>(c, c->lay.mass_acc);
+    ap.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
+    ap.top = c->sparse.top;
+    e = launch_attend_pages(ap, c->stream);
+  }
+  prof_end(c, STAGE_ATTN, e0);
+  if (e != cudaSuccess) return cuda_fail(c, e, "attention launch");
+  if (l0 + L == cf.num_layers)
+    for (int b = 0; b < batch; ++b) c->sparse.bounded[b] = c->n_pages[b] - 1;
+  return MD_OK;
+}
+
 /* Stage 1 over layers [l0, l0 + L); q/out hold q_layers layers.  With k_new
  * the step's new tokens are appended too (device rows [batch][L][Hkv][D]), by
  * the attention launch or by one ahead of it. */
 md_status run_attention(md_ctx *c, int batch, int l0, int L, int q_layers, const void *q_dev,
                         const void *k_new, const void *v_new, void *out_dev) {
   const md_config &cf = c->cfg;
+  if (sparse_step(c, batch)) {
+    const md_status st = k_new ? append_step(c, batch, l0, L, k_new, v_new, nullptr, nullptr, 0) : MD_OK;
+    return st == MD_OK ? run_sparse(c, batch, l0, L, q_dev, out_dev) : st;
+  }
   AttnBase base;
   memset(&base, 0, sizeof(base));
   base.q = (const uint16_t *)q_dev;
@@ -1189,6 +1296,9 @@ MD_API md_status md_evict(md_ctx *c, int batch, const int32_t *budget, int32_t *
     }
   }
   for (int b = 0; b < batch; ++b) {
+    /* all of the evicted pages may have been bounded ones; where every page but
+     * the last was, they were, and the last one stays */
+    if (c->sparse.top) c->sparse.bounded[b] = std::max(0, c->sparse.bounded[b] - ev[b]);
     c->n_pages[b] -= ev[b];
     /* evicted pages are never the tail; they are full unless pages are
      * region-aligned, where their fill is known on the device only */
@@ -1305,6 +1415,7 @@ MD_API md_status md_set_state(md_ctx *c, int what, const void *src, size_t bytes
   size_t off, n;
   state_array(c, what, &off, &n);
   if (bytes != n) return fail(c, MD_ERR_INVALID_ARG, "state array is %zu bytes, not %zu", n, bytes);
+  if (what == MD_STATE_BLOCK_TABLE || what == MD_STATE_PAGE_FILL) c->sparse.bounded.assign(c->sparse.bounded.size(), 0);
   cudaError_t e = cudaMemcpyAsync(c->ws + off, src, n, cudaMemcpyDeviceToDevice, c->stream);
   return e == cudaSuccess ? MD_OK : cuda_fail(c, e, "state copy");
 }
@@ -1423,10 +1534,38 @@ MD_API md_status md_load_state(md_ctx *c, const void *src_dev, const void *host_
   memcpy(c->tokens_exact.data(), h, B);
   h += B;
   c->calib_on = *h != 0;
+  c->sparse.bounded.assign(c->sparse.bounded.size(), 0);
   /* a checkpoint holds no pending step mass; clear whatever the live state
    * had accumulated, or the next step would add to it */
   cudaError_t e = cudaMemsetAsync(c->ws + c->lay.mass_acc, 0, c->lay.slots * 8, c->stream);
   if (e != cudaSuccess) return cuda_fail(c, e, "restore: clear the step mass");
+  return MD_OK;
+}
+
+MD_API size_t md_sparse_bytes(const md_config *cfg, int top_pages) {
+  if (!cfg || check_config(*cfg) || top_pages < 1 || (long long)top_pages * cfg->page_size > MD_MAX_TOP_TOKENS) return 0;
+  return sparse_layout(*cfg, top_pages).total;
+}
+
+MD_API md_status md_sparse_enable(md_ctx *c, int top, int first, int last, void *buf, size_t bytes) {
+  if (!c) return MD_ERR_INVALID_ARG;
+  if (c->poisoned) return fail(c, MD_ERR_STATE, "handle unusable after an earlier error");
+  if (c->m.layer_next != 0) return fail(c, MD_ERR_STATE, "a layer-by-layer step is in progress");
+  if (top == 0) {
+    c->sparse.top = 0;
+    return MD_OK;
+  }
+  const size_t need = md_sparse_bytes(&c->cfg, top);
+  if (need == 0) return fail(c, MD_ERR_INVALID_ARG, "top_pages out of range");
+  if (first < 0 || last < 1 || first > top || last > top - first)
+    return fail(c, MD_ERR_INVALID_ARG, "first and last pages: at least 0 and 1, at most top_pages together");
+  if (!buf || ((uintptr_t)buf & 255) || bytes < need)
+    return fail(c, MD_ERR_WORKSPACE, "buffer missing, misaligned or below %zu bytes", need);
+  c->sparse.top = top;
+  c->sparse.first = first;
+  c->sparse.last = last;
+  c->sparse.buf = (uint8_t *)buf;
+  c->sparse.bounded.assign(c->cfg.max_batch, 0);
   return MD_OK;
 }
 

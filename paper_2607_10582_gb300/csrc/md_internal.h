@@ -303,6 +303,7 @@ struct AttendPagesParams : PageSet {
   uint16_t *out;
   const int32_t *ids;                    // [n_seqs][L][Hkv][top]
   float *mass;                           // [n_seqs][L][Hkv][top][ps], or null
+  unsigned long long *mass_acc;          // [slots] fixed-point mass of the step, or null
   float scale_log2;                      // log2(e) / sqrt(D)
   int top;
 };

@@ -411,9 +411,10 @@ __global__ void __launch_bounds__(32 * AT_WARPS) attend_pages_kernel(const __gri
       fz[head] = head < p.G ? r : 0.f;
     }
   }
-  if (!p.mass) return;
+  if (!p.mass && !p.mass_acc) return;
   __syncthreads();
   float *mass = p.mass + row * p.top * p.ps;
+  const uint64_t keep = policy_evict_last();
   const float m0 = fm[2 * t], m1 = fm[2 * t + 1], r0 = fz[2 * t], r1 = fz[2 * t + 1];
   for (int tile = warp; tile < tiles; tile += AT_WARPS) {
     int valid;
@@ -432,9 +433,14 @@ __global__ void __launch_bounds__(32 * AT_WARPS) attend_pages_kernel(const __gri
       w0 += __shfl_xor_sync(0xffffffffu, w0, s);
       w1 += __shfl_xor_sync(0xffffffffu, w1, s);
     }
-    if (t == 0) {
+    if (t == 0 && p.mass) {
       mass[tile * TILE + g] = w0;
       mass[tile * TILE + 8 + g] = w1;
+    }
+    if (t == 0 && p.mass_acc && valid > 0) {
+      unsigned long long *acc = p.mass_acc + (size_t)page_id(p, b, ids[tile / tpp]) * p.ps + tile % tpp * TILE;
+      if (g < valid) red_add_u64_hint(acc + g, __float2ull_rn(w0 * MASS_SCALE), keep);
+      if (g + 8 < valid) red_add_u64_hint(acc + g + 8, __float2ull_rn(w1 * MASS_SCALE), keep);
     }
   }
 }
@@ -586,6 +592,7 @@ MD_API md_status md_attend_pages(const void *q, const void *pool, const int32_t 
   p.out = (uint16_t *)out;
   p.ids = page_ids;
   p.mass = mass;
+  p.mass_acc = nullptr;
   p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
   p.top = top_pages;
   return launch_attend_pages(p, (cudaStream_t)stream) == cudaSuccess ? MD_OK : MD_ERR_CUDA;

@@ -1,0 +1,262 @@
+"""md_sparse_enable: decode steps of a handle over selected pages.
+
+With contiguous pages a step's output is that of the page calls on the handle's own pool
+and table, bit for bit, and its mass their masses' sum; tests/test_pages.py holds those
+calls to their formulas.  Region-aligned pages are held to the formulas directly, with the
+tolerances given there."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+import paper_2607_10582_gb300 as md
+from paper_2607_10582_gb300 import build as mdbuild
+
+torch = pytest.importorskip("torch")
+D = 128
+mdbuild.build()
+gpu = pytest.mark.gpu
+UNIT = 2.0 ** -48
+CHAIN = 18 * 2.0 ** -24
+
+
+class Loop:
+    """A decode loop with its own inputs."""
+
+    def __init__(self, L, Hq, Hkv, ps, lengths, seed=0, room=200, **kw):
+        if not torch.cuda.is_available():  # pragma: no cover
+            pytest.skip("needs a CUDA GPU")
+        self.L, self.Hq, self.Hkv, self.ps, self.B = L, Hq, Hkv, ps, len(lengths)
+        self.g = torch.Generator(device="cuda").manual_seed(seed)
+        self.rng = np.random.default_rng(seed)
+        width = max(lengths) // ps + room
+        self.c = md.Cache(L, Hq, Hkv, ps, self.B, width, sum(lengths) // ps + self.B * room, **kw)
+        for r in range(7):
+            self.c.set_region_params(r, 1.0 - 0.1 * r, 20.0 + 10 * r, r == 0)
+        for b, n in enumerate(lengths):
+            self.append(b, n)
+
+    def rand(self, *shape):
+        return torch.randn(shape, generator=self.g, device="cuda").bfloat16()
+
+    def append(self, b, n):
+        lab = np.sort(self.rng.integers(0, 7, n)).astype(np.uint8)
+        self.c.append_tokens(b, lab, self.rand(self.L, self.Hkv, n, D), self.rand(self.L, self.Hkv, n, D))
+
+    def step(self, how="step", q=None, kv=None, regions=None):
+        B, L = self.B, self.L
+        q = self.rand(B, L, self.Hq, D) if q is None else q
+        k, v = (self.rand(B, L, self.Hkv, D) for _ in range(2)) if kv is None else kv
+        regions = np.full(B, 6, np.uint8) if regions is None else regions
+        out = torch.full_like(q, math.nan)
+        if how == "layers":
+            for l in range(L):
+                o = torch.empty_like(q[:, l])
+                self.c.decode_layer(l, B, q[:, l].contiguous(), k[:, l].contiguous(), v[:, l].contiguous(), regions, o)
+                out[:, l] = o
+        elif how == "host":
+            h = torch.empty(q.shape, dtype=q.dtype, pin_memory=True)
+            self.c.decode_step_host(B, *(x.cpu().pin_memory() for x in (q, k, v)), regions, h)
+            assert self.c.sync() == md.MD_OK
+            out = h.cuda()
+        else:
+            self.c.decode_step(B, q, k, v, regions, out)
+        return q, out
+
+    def tokens(self):
+        return np.array([self.c.query(md.MD_QUERY_TOKENS, b) for b in range(self.B)], np.int32)
+
+    def pages(self):
+        return [self.c.query(md.MD_QUERY_PAGES, b) for b in range(self.B)]
+
+    def by_page_calls(self, q, top, first, last):
+        """The step just run, by the page calls: output, and mass per slot."""
+        pool, bt, n = self.c.get_state(md.MD_STATE_POOL), self.c.get_state(md.MD_STATE_BLOCK_TABLE), self.tokens()
+        L, P, W, rows = self.L, pool.shape[1], bt.shape[1], (self.B, self.L, self.Hkv)
+        bounds = torch.zeros((L, P, self.Hkv, 2, D), dtype=torch.bfloat16, device="cuda")
+        scores = torch.zeros(rows + (W,), device="cuda")
+        ids = torch.empty(rows + (top,), dtype=torch.int32, device="cuda")
+        out, mass = torch.empty_like(q), torch.empty(rows + (top * self.ps,), device="cuda")
+        md.md_page_bounds(pool, bt, n, bounds)
+        md.md_page_scores(q, bounds, bt, n, scores, page_size=self.ps)
+        md.md_page_top(scores, n, ids, page_size=self.ps, first=first, last=last)
+        md.md_attend_pages(q, pool, bt, n, ids, out, mass=mass)
+        acc = torch.zeros(P * self.ps, dtype=torch.float64, device="cuda")
+        for b in range(self.B):
+            i = ids[b].long()
+            slot = bt[b, i.clamp(min=0)].long()[..., None] * self.ps + torch.arange(self.ps, device="cuda")
+            keep = (i >= 0)[..., None].expand_as(slot)
+            acc.index_add_(0, slot[keep], mass[b].double().view(slot.shape)[keep])
+        return out, acc
+
+    def check(self, how, top, first=1, last=1):
+        q, out = self.step(how)
+        mass = self.c.get_state(md.MD_STATE_MASS).double() * UNIT
+        want, acc = self.by_page_calls(q, top, first, last)
+        assert torch.equal(out, want)
+        # each addend is rounded to 2^-48
+        assert (mass - acc).abs().max() <= self.L * self.Hkv * 2.0 ** -48 + 2.0 ** -50 * self.L * self.Hq
+        assert abs(float(mass.sum()) - self.B * self.L * self.Hq) < 1e-3 * self.B * self.L * self.Hq
+
+
+@gpu
+@pytest.mark.parametrize("how", ["step", "layers", "host"])
+@pytest.mark.parametrize("L,Hq,Hkv,ps,lengths,top,first,last", [
+    (1, 12, 2, 16, [448], 6, 1, 1),
+    (3, 16, 2, 32, [900, 20, 3000], 17, 2, 3),
+    (2, 8, 4, 16, [1700, 1500, 40, 1], 24, 0, 1),
+])
+def test_steps_attend_the_selected_pages(L, Hq, Hkv, ps, lengths, top, first, last, how):
+    """Steps that fill pages, appends and evictions in between."""
+    s = Loop(L, Hq, Hkv, ps, lengths, seed=top)
+    s.c.sparse_enable(top, first, last)
+    for i in range(2 * ps + 3):
+        if i % 11 in (0, 1, 7) or s.ps - 2 <= i % s.ps:
+            s.check(how, top, first, last)
+        else:
+            s.step(how)
+        if i % 5 == 4:
+            s.c.evict(np.array([max(top + 2, p - 2) for p in s.pages()], np.int32))
+        if i % 13 == 12:
+            s.append(i % s.B, 70)
+    assert s.c.sync() == md.MD_OK
+
+
+@gpu
+def test_short_sequences_are_attended_in_full():
+    """No sequence above top_pages: the step is the one without a selection, bit for bit;
+    the same for a handle whose selection was turned off."""
+    L, lengths = 2, [300, 77]
+    a, b, c = (Loop(L, 16, 2, 16, lengths, seed=4) for _ in range(3))
+    a.c.sparse_enable(25)
+    c.c.sparse_enable(3)
+    c.c.sparse_enable(0)
+    for how in ("step", "layers", "host"):
+        outs = [x.step(how)[1] for x in (a, b, c)]
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+        assert torch.equal(a.c.get_state(md.MD_STATE_MASS), b.c.get_state(md.MD_STATE_MASS))
+
+
+@gpu
+def test_selecting_all_but_nothing_changes_the_sum():
+    """Just above the threshold: one page of many is left out; and sparse and dense steps
+    may alternate, pages filled under dense steps being bounded when they are needed."""
+    s = Loop(2, 16, 2, 16, [640 + 5], seed=5)
+    for i in range(40):
+        if i % 3 == 2:
+            s.c.sparse_enable(0)
+            s.step()
+        elif i % 3 == 0:
+            s.c.sparse_enable(s.pages()[0] - 1)
+            s.check("step", s.pages()[0] - 1) if s.tokens()[0] % 16 else s.step()
+        else:
+            s.c.sparse_enable(7)
+            s.check("layers", 7)
+
+
+@gpu
+def test_eviction_observes_the_selected_tokens():
+    """Pages that were not attended have no mass, and go first under pure accumulation."""
+    s = Loop(1, 8, 1, 16, [1600], seed=6, rho=1.0, gamma=1.0, attn_weight=1.0)
+    for r in range(7):
+        s.c.set_region_params(r, 0.0, math.inf, r == 0)
+    s.c.sparse_enable(30)
+    q, _ = s.step()
+    mass = s.c.get_state(md.MD_STATE_MASS).view(-1, 16).sum(1)
+    table = s.c.get_state(md.MD_STATE_BLOCK_TABLE)[0, :101].long()
+    pinned = s.c.query(md.MD_QUERY_PINNED_PAGES, 0)
+    seen = mass[table] > 0
+    assert int(seen.sum()) == 30
+    unseen = [int(x) for x in table[~seen]]
+    ids = torch.empty((1, s.c.P_max), dtype=torch.int32, device="cuda")
+    s.c.evict([101 - 20], ids)
+    gone = [int(x) for x in ids[0] if x >= 0]
+    assert len(gone) == 20 and set(gone) <= set(unseen) and pinned < 101 - 30
+    s.check("step", 30)
+
+
+@gpu
+def test_checkpoint_under_selection():
+    s = Loop(2, 16, 2, 16, [700, 300], seed=7)
+    s.c.sparse_enable(9)
+    s.step()
+    s.c.evict([40, 20])
+    saved = s.c.save_state()
+    q, k, v = s.rand(2, 2, 16, D), s.rand(2, 2, 2, D), s.rand(2, 2, 2, D)
+    _, first = s.step(q=q, kv=(k, v))
+    s.c.evict([39, 19])
+    s.c.load_state(saved)
+    _, again = s.step(q=q, kv=(k, v))
+    assert torch.equal(first, again)
+    for _ in range(20):
+        s.check("step", 9)
+
+
+@gpu
+@pytest.mark.parametrize("ps", [16, 32])
+def test_region_aligned_pages(ps):
+    """Partly filled pages in the middle: one layer and KV head, so that the mass shows the
+    pages attended."""
+    s = Loop(1, 8, 1, ps, [900], seed=8, region_aligned_pages=1)
+    top = 11
+    s.c.sparse_enable(top, 1, 2)
+    for i in range(45):
+        q, out = s.step(regions=np.array([(i // 5) % 7], np.uint8))
+        n = s.pages()[0]
+        table = s.c.get_state(md.MD_STATE_BLOCK_TABLE)[0, :n].long()
+        fill = s.c.get_state(md.MD_STATE_PAGE_FILL)[0, :n].long()
+        pool = s.c.get_state(md.MD_STATE_POOL).view(torch.bfloat16)[0, table, 0].double()   # [n][2][ps][D]
+        mass = s.c.get_state(md.MD_STATE_MASS).double().view(-1, ps)[table] * UNIT
+        held = torch.arange(ps, device="cuda") < fill[:, None]
+        k, v = pool[:, 0], torch.where(held[..., None], pool[:, 1], 0)
+        hi = torch.where(held[..., None], k, -math.inf).amax(1)
+        lo = torch.where(held[..., None], k, math.inf).amin(1)
+        x = q[0, 0].double()
+        bound = (x.clamp(min=0) @ hi.T + x.clamp(max=0) @ lo.T).amax(0) / math.sqrt(D)
+        seen = mass.sum(1) > 0
+        assert int(seen.sum()) == top and seen[0] and seen[-2:].all()
+        slack = 16 * CHAIN * float((x.abs() @ torch.maximum(hi.abs(), lo.abs()).T).max()) / math.sqrt(D)
+        mid = slice(1, n - 2)
+        assert bound[mid][seen[mid]].min() >= bound[mid][~seen[mid]].max() - 2 * slack
+        use = (held & seen[:, None]).flatten()
+        kk, vv = k.flatten(0, 1)[use], v.flatten(0, 1)[use]
+        p = torch.softmax(x @ kk.T / math.sqrt(D), -1)
+        delta = 8 * CHAIN * float((x.abs() @ kk.abs().T).max()) / math.sqrt(D)
+        ref = p @ vv
+        tol = 2.0 ** -8 * ref.abs() + (2 * delta + 2.0 ** -15) * (p @ vv.abs())
+        assert ((out[0, 0].double() - ref).abs() <= tol).all()
+        assert ((mass.flatten()[use] - p.sum(0)).abs() <= (2 * delta + 2.0 ** -18) * p.sum(0) + 8 * UNIT).all()
+        assert not mass.flatten()[~use].any()
+        if i % 6 == 5:
+            s.c.evict([max(20, n - 3)])
+
+
+@gpu
+def test_refusals_leave_the_handle_as_it_was():
+    s = Loop(2, 16, 2, 16, [400], seed=9)
+    for top, first, last in ((-1, 1, 1), (5000, 1, 1), (4, 1, 0), (4, -1, 1), (4, 3, 2), (4, 5, 1)):
+        with pytest.raises(md.MemDecayError) as e:
+            s.c.sparse_enable(top, first, last)
+        assert e.value.status == md.MD_ERR_INVALID_ARG
+    lib, need = md.lib(), int(md.lib().md_sparse_bytes(ctypes.byref(s.c.cfg), 4))
+    buf = torch.empty(need + 512, dtype=torch.uint8, device="cuda")
+    at = (buf.data_ptr() + 255) // 256 * 256
+    for p, n in ((None, need), (at + 16, need), (at, need - 1)):
+        assert lib.md_sparse_enable(s.c.h, 4, 1, 1, p, n) == md.MD_ERR_WORKSPACE
+    q, k = s.rand(1, 16, D), s.rand(1, 2, D)
+    s.c.decode_layer(0, 1, q, k, k, [6], torch.empty_like(q))
+    assert lib.md_sparse_enable(s.c.h, 4, 1, 1, at, need) == md.MD_ERR_STATE
+    s.c.decode_layer(1, 1, q, k, k, [6], torch.empty_like(q))
+    s.c.sparse_enable(4)
+    s.check("step", 4)
+
+
+def test_buffer_size_is_host_arithmetic():
+    cfg = md.md_config(2, 16, 2, 128, 16, 4, 64, 256, 0.9, 0.1, 2.0, 1.0, 0, 0, 1, None, 0, None, 0, 0)
+    size = lambda top: int(md.lib().md_sparse_bytes(ctypes.byref(cfg), top))  # noqa: E731
+    assert size(8) >= 2 * 256 * 2 * 512 + 4 * 4 * 64 * 4 + 4 * 4 * 8 * 4
+    assert size(0) == size(-1) == size(md.MD_MAX_TOP_TOKENS // 16 + 1) == 0 and size(64) > size(8)
+    cfg.page_size = 8
+    assert size(8) == 0 and int(md.lib().md_sparse_bytes(None, 8)) == 0
+    assert md.lib().md_sparse_enable(None, 0, 0, 0, None, 0) == md.MD_ERR_INVALID_ARG
