@@ -152,6 +152,7 @@ class _NoCalls:
         return None
 
     decode_step = decode_step_host = decode_layer = evict = get_state = _leave
+    load_torch = norm_rope = page_bounds = page_scores = page_top = attend_pages = _leave
 
 
 def _binding():
@@ -224,6 +225,25 @@ def md_calib_fit(mass_sum: np.ndarray, count: np.ndarray, bucket_width: int = MD
 
 
 # ---- rows for the cache, attention over selected pages: calls without a handle ----
+# The C module takes a call whose arguments are as its description says; what it leaves
+# goes through the checks below, which say what is wrong.
+_torch_calls = None
+
+
+def _ops():
+    """The C module with what it needs of torch."""
+    global _torch_calls
+    if _torch_calls is None:
+        import torch
+        b = _binding()
+        b.load_torch((torch.bfloat16, torch.float16, torch.float32, torch.int16, torch.int32),
+                     getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
+                     getattr(torch._C, "_cuda_getCurrentRawStream",
+                             lambda d: torch.cuda.current_stream(d).cuda_stream))
+        _torch_calls = b
+    return _torch_calls
+
+
 def _bad(what: str):
     raise MemDecayError(MD_ERR_INVALID_ARG, what)
 
@@ -238,12 +258,22 @@ def _on(t, stream):
     return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
 
 
-def _dense(name, t, shape, size):
-    """Address of a contiguous device tensor of this shape and element size."""
-    if tuple(t.shape) != tuple(shape) or t.element_size() != size or not t.is_contiguous() or not t.is_cuda:
-        _bad(f"{name}: a contiguous device tensor {tuple(shape)} of {size}-byte elements expected, "
+_KINDS = {"bf16": ("bfloat16", "int16"), "f32": ("float32",), "i32": ("int32",)}    # int16: raw bf16 bits
+
+
+def _dense(name, t, shape, kind):
+    """Address of a contiguous device tensor of this shape and kind."""
+    if (tuple(t.shape) != tuple(shape) or str(t.dtype).split(".")[-1] not in _KINDS[kind] or not t.is_contiguous()
+            or not t.is_cuda):
+        _bad(f"{name}: a contiguous device tensor {tuple(shape)} of {kind} expected, "
              f"not {tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
+
+
+def _dims(name, t, n):
+    if t.dim() != n:
+        _bad(f"{name}: {n} dimensions expected, not {t.dim()}")
+    return t.shape
 
 
 def _status(st: int, what: str):
@@ -280,6 +310,10 @@ def md_norm_rope(q, k, v, q_out, k_out, v_out, *, positions, table, q_weight=Non
       table        md_rope_table's, or None: no rotation
       axes         uint8 [rotary_dim / 2] on the host: the axis of each pair (None: the first)
       weights      fp32 [128]"""
+    st = (_torch_calls or _ops()).norm_rope(q, k, v, q_out, k_out, v_out, positions, table, q_weight, k_weight, eps,
+                                             axes, interleaved, None if stream is None else stream.cuda_stream)
+    if st is not None:
+        return _status(st, "md_norm_rope: head counts, alignment or strides")
     a = md_norm_rope_args()
     types = _row_types()
     first = q if q is not None else k
@@ -307,17 +341,16 @@ def md_norm_rope(q, k, v, q_out, k_out, v_out, *, positions, table, q_weight=Non
     a.num_q_heads = q.shape[1] if q is not None else 0
     a.num_kv_heads = k.shape[1] if k is not None else 0
     if q is not None and q_weight is not None:
-        a.q_weight = _dense("q_weight", q_weight, (MD_HEAD_DIM,), 4)
+        a.q_weight = _dense("q_weight", q_weight, (MD_HEAD_DIM,), "f32")
     if k is not None and k_weight is not None:
-        a.k_weight = _dense("k_weight", k_weight, (MD_HEAD_DIM,), 4)
+        a.k_weight = _dense("k_weight", k_weight, (MD_HEAD_DIM,), "f32")
     host = None
     if table is not None:
-        if table.dim() != 3:
-            _bad("table: [positions][pairs][2] expected")
-        a.table = _dense("table", table, (table.shape[0], table.shape[1], 2), 4)
+        _dims("table", table, 3)
+        a.table = _dense("table", table, (table.shape[0], table.shape[1], 2), "f32")
         a.table_len, a.rotary_dim = table.shape[0], 2 * table.shape[1]
         a.num_axes = positions.shape[0] if positions.dim() == 2 else 1
-        a.positions = _dense("positions", positions, (a.num_axes, T) if positions.dim() == 2 else (T,), 4)
+        a.positions = _dense("positions", positions, (a.num_axes, T) if positions.dim() == 2 else (T,), "i32")
         if axes is not None:
             host, a.axis_host = _host(axes, np.uint8)
             if host.size < table.shape[1]:
@@ -333,25 +366,23 @@ def _counts(n_tokens, batch: int):
     return n, p
 
 
-def _table_shape(block_table):
-    if block_table.dim() != 2:
-        _bad("block_table: [batch][max_pages_per_seq] expected")
-    return block_table.shape
-
-
 def md_page_bounds(pool, block_table, n_tokens, bounds, *, first_pages=None, stream=None):
     """Channelwise least and largest key of the pages from first_pages[b] on (None: all).
       pool         bf16 [L][pages][Hkv][2][page_size][128]
       block_table  int32 [batch][max_pages_per_seq]
       n_tokens     int32 [batch] on the host
       bounds       bf16 [L][pages][Hkv][2][128]; written for those pages"""
-    B, P_max = _table_shape(block_table)
-    L, P, Hkv, _, ps, _ = pool.shape
+    st = (_torch_calls or _ops()).page_bounds(pool, block_table, n_tokens, first_pages, bounds,
+                                              None if stream is None else stream.cuda_stream)
+    if st is not None:
+        return _status(st, "md_page_bounds")
+    B, P_max = _dims("block_table", block_table, 2)
+    L, P, Hkv, _, ps, _ = _dims("pool", pool, 6)
     n, np_ = _counts(n_tokens, B)
     f, fp = (None, None) if first_pages is None else _counts(first_pages, B)
-    _status(lib().md_page_bounds(_dense("pool", pool, (L, P, Hkv, 2, ps, MD_HEAD_DIM), 2),
-                                 _dense("block_table", block_table, (B, P_max), 4), np_, fp,
-                                 _dense("bounds", bounds, (L, P, Hkv, 2, MD_HEAD_DIM), 2), B, L, Hkv, ps, P_max, P,
+    _status(lib().md_page_bounds(_dense("pool", pool, (L, P, Hkv, 2, ps, MD_HEAD_DIM), "bf16"),
+                                 _dense("block_table", block_table, (B, P_max), "i32"), np_, fp,
+                                 _dense("bounds", bounds, (L, P, Hkv, 2, MD_HEAD_DIM), "bf16"), B, L, Hkv, ps, P_max, P,
                                  _on(pool, stream)), "md_page_bounds")
 
 
@@ -360,14 +391,18 @@ def md_page_scores(q, bounds, block_table, n_tokens, scores, *, page_size: int, 
       q       bf16 [batch][L][Hq][128]
       bounds  as md_page_bounds writes them
       scores  fp32 [batch][L][Hkv][max_pages_per_seq]; written for each sequence's pages"""
-    B, P_max = _table_shape(block_table)
-    L, P, Hkv = bounds.shape[:3]
-    Hq = q.shape[2]
+    st = (_torch_calls or _ops()).page_scores(q, bounds, block_table, n_tokens, scores, page_size,
+                                              None if stream is None else stream.cuda_stream)
+    if st is not None:
+        return _status(st, "md_page_scores")
+    B, P_max = _dims("block_table", block_table, 2)
+    L, P, Hkv = _dims("bounds", bounds, 5)[:3]
+    Hq = _dims("q", q, 4)[2]
     n, np_ = _counts(n_tokens, B)
-    _status(lib().md_page_scores(_dense("q", q, (B, L, Hq, MD_HEAD_DIM), 2),
-                                 _dense("bounds", bounds, (L, P, Hkv, 2, MD_HEAD_DIM), 2),
-                                 _dense("block_table", block_table, (B, P_max), 4), np_,
-                                 _dense("scores", scores, (B, L, Hkv, P_max), 4), B, L, Hq, Hkv, page_size, P_max, P,
+    _status(lib().md_page_scores(_dense("q", q, (B, L, Hq, MD_HEAD_DIM), "bf16"),
+                                 _dense("bounds", bounds, (L, P, Hkv, 2, MD_HEAD_DIM), "bf16"),
+                                 _dense("block_table", block_table, (B, P_max), "i32"), np_,
+                                 _dense("scores", scores, (B, L, Hkv, P_max), "f32"), B, L, Hq, Hkv, page_size, P_max, P,
                                  _on(q, stream)), "md_page_scores")
 
 
@@ -375,11 +410,15 @@ def md_page_top(scores, n_tokens, page_ids, *, page_size: int, first: int = 1, l
     """The pages to attend: the first, the last, and the highest scored of the others.
       scores    fp32 [batch][L][Hkv][max_pages_per_seq]
       page_ids  int32 [batch][L][Hkv][top_pages]; written, in rising order, -1 behind them"""
-    B, L, Hkv, P_max = scores.shape
-    top = page_ids.shape[-1]
+    st = (_torch_calls or _ops()).page_top(scores, n_tokens, page_ids, page_size, first, last,
+                                           None if stream is None else stream.cuda_stream)
+    if st is not None:
+        return _status(st, "md_page_top")
+    B, L, Hkv, P_max = _dims("scores", scores, 4)
+    top = _dims("page_ids", page_ids, 4)[3]
     n, np_ = _counts(n_tokens, B)
-    _status(lib().md_page_top(_dense("scores", scores, (B, L, Hkv, P_max), 4), np_,
-                              _dense("page_ids", page_ids, (B, L, Hkv, top), 4), B, L, Hkv, page_size, P_max, top,
+    _status(lib().md_page_top(_dense("scores", scores, (B, L, Hkv, P_max), "f32"), np_,
+                              _dense("page_ids", page_ids, (B, L, Hkv, top), "i32"), B, L, Hkv, page_size, P_max, top,
                               first, last, _on(scores, stream)), "md_page_top")
 
 
@@ -388,15 +427,19 @@ def md_attend_pages(q, pool, block_table, n_tokens, page_ids, out, *, mass=None,
       q, out    bf16 [batch][L][Hq][128]
       page_ids  int32 [batch][L][Hkv][top_pages]
       mass      fp32 [batch][L][Hkv][top_pages * page_size] or None; written"""
-    B, P_max = _table_shape(block_table)
-    L, P, Hkv, _, ps, _ = pool.shape
-    Hq, top = q.shape[2], page_ids.shape[-1]
+    st = (_torch_calls or _ops()).attend_pages(q, pool, block_table, n_tokens, page_ids, out, mass,
+                                               None if stream is None else stream.cuda_stream)
+    if st is not None:
+        return _status(st, "md_attend_pages")
+    B, P_max = _dims("block_table", block_table, 2)
+    L, P, Hkv, _, ps, _ = _dims("pool", pool, 6)
+    Hq, top = _dims("q", q, 4)[2], _dims("page_ids", page_ids, 4)[3]
     n, np_ = _counts(n_tokens, B)
     _status(lib().md_attend_pages(
-        _dense("q", q, (B, L, Hq, MD_HEAD_DIM), 2), _dense("pool", pool, (L, P, Hkv, 2, ps, MD_HEAD_DIM), 2),
-        _dense("block_table", block_table, (B, P_max), 4), np_, _dense("page_ids", page_ids, (B, L, Hkv, top), 4),
-        _dense("out", out, (B, L, Hq, MD_HEAD_DIM), 2),
-        None if mass is None else _dense("mass", mass, (B, L, Hkv, top * ps), 4), B, L, Hq, Hkv, ps, P_max, P, top,
+        _dense("q", q, (B, L, Hq, MD_HEAD_DIM), "bf16"), _dense("pool", pool, (L, P, Hkv, 2, ps, MD_HEAD_DIM), "bf16"),
+        _dense("block_table", block_table, (B, P_max), "i32"), np_, _dense("page_ids", page_ids, (B, L, Hkv, top), "i32"),
+        _dense("out", out, (B, L, Hq, MD_HEAD_DIM), "bf16"),
+        None if mass is None else _dense("mass", mass, (B, L, Hkv, top * ps), "f32"), B, L, Hq, Hkv, ps, P_max, P, top,
         _on(q, stream)), "md_attend_pages")
 
 

@@ -18,7 +18,7 @@
 
 #include "../../include/memdecay.h"
 
-static PyObject *s_data_ptr, *s_is_cuda, *s_is_contiguous;
+static PyObject *s_data_ptr, *s_is_cuda, *s_is_contiguous, *s_shape, *s_stride, *s_dtype, *s_get_device;
 static md_status (*f_decode_step)(md_ctx *, int, const void *, const void *, const void *, const uint8_t *, void *);
 static md_status (*f_decode_step_host)(md_ctx *, int, const void *, const void *, const void *, const uint8_t *,
                                        void *);
@@ -26,6 +26,17 @@ static md_status (*f_decode_layer)(md_ctx *, int, int, const void *, const void 
                                    void *);
 static md_status (*f_evict)(md_ctx *, int, const int32_t *, int32_t *, int32_t *);
 static md_status (*f_get_state)(md_ctx *, int, void *, size_t);
+static md_status (*f_norm_rope)(const md_norm_rope_args *);
+static md_status (*f_page_bounds)(const void *, const int32_t *, const int32_t *, const int32_t *, void *, int, int, int,
+                                  int, int, int, void *);
+static md_status (*f_page_scores)(const void *, const void *, const int32_t *, const int32_t *, float *, int, int, int,
+                                  int, int, int, int, void *);
+static md_status (*f_page_top)(const float *, const int32_t *, int32_t *, int, int, int, int, int, int, int, int, void *);
+static md_status (*f_attend_pages)(const void *, const void *, const int32_t *, const int32_t *, const int32_t *, void *,
+                                   float *, int, int, int, int, int, int, int, int, void *);
+/* torch's dtypes bfloat16, float16, float32, int16, int32, and its functions for
+ * the current device and the raw current stream of a device (load_torch) */
+static PyObject *t_types[5], *t_device, *t_stream;
 
 static PyObject *load(PyObject *self, PyObject *path) {
   const char *s = PyUnicode_AsUTF8(path);
@@ -40,7 +51,13 @@ static PyObject *load(PyObject *self, PyObject *path) {
   *(void **)&f_decode_layer = dlsym(h, "md_decode_layer");
   *(void **)&f_evict = dlsym(h, "md_evict");
   *(void **)&f_get_state = dlsym(h, "md_get_state");
-  if (!f_decode_step || !f_decode_step_host || !f_decode_layer || !f_evict || !f_get_state) {
+  *(void **)&f_norm_rope = dlsym(h, "md_norm_rope");
+  *(void **)&f_page_bounds = dlsym(h, "md_page_bounds");
+  *(void **)&f_page_scores = dlsym(h, "md_page_scores");
+  *(void **)&f_page_top = dlsym(h, "md_page_top");
+  *(void **)&f_attend_pages = dlsym(h, "md_attend_pages");
+  if (!f_decode_step || !f_decode_step_host || !f_decode_layer || !f_evict || !f_get_state || !f_norm_rope ||
+      !f_page_bounds || !f_page_scores || !f_page_top || !f_attend_pages) {
     PyErr_SetString(PyExc_OSError, "libmemdecay.so lacks an entry point");
     return NULL;
   }
@@ -210,6 +227,289 @@ static PyObject *get_state(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
+/* ---- calls without a handle: whatever they do not take as it is (another type,
+ * shape, layout or device, an argument missing) they leave to the caller, by
+ * None, who converts it or says what is wrong ---- */
+
+/* load_torch(types, current_device, current_raw_stream) */
+static PyObject *load_torch(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  if (arity(n, 3)) return NULL;
+  if (!PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 5) {
+    PyErr_SetString(PyExc_TypeError, "five types expected");
+    return NULL;
+  }
+  for (int i = 0; i < 5; ++i) Py_XSETREF(t_types[i], Py_NewRef(PyTuple_GET_ITEM(a[0], i)));
+  Py_XSETREF(t_device, Py_NewRef(a[1]));
+  Py_XSETREF(t_stream, Py_NewRef(a[2]));
+  Py_RETURN_NONE;
+}
+
+enum { T_BF16, T_F16, T_F32, T_I16, T_I32, T_OTHER };
+#define MAX_DIMS 6
+
+typedef struct {
+  void *p;
+  int dims, type;
+  long long n[MAX_DIMS];
+} tensor;
+
+/* Integers of a tuple: their number, or -1. */
+static int tuple_of(PyObject *t, long long *out) {
+  if (!t || !PyTuple_Check(t) || PyTuple_GET_SIZE(t) > MAX_DIMS) return -1;
+  const int n = (int)PyTuple_GET_SIZE(t);
+  for (int i = 0; i < n; ++i) out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+  return n;
+}
+
+static int is_true(PyObject *v) {
+  const int r = v == Py_True;
+  Py_XDECREF(v);
+  return r;
+}
+
+/* A device tensor's address, type and shape: 1, or 0 (an exception may be set). */
+static int device_tensor(PyObject *o, tensor *t) {
+  if (o == Py_None || !is_true(PyObject_GetAttr(o, s_is_cuda))) return 0;
+  PyObject *v = PyObject_GetAttr(o, s_shape);
+  t->dims = tuple_of(v, t->n);
+  Py_XDECREF(v);
+  if (t->dims < 0) return 0;
+  v = PyObject_GetAttr(o, s_dtype);
+  for (t->type = 0; t->type < T_OTHER && v != t_types[t->type]; ++t->type) {
+  }
+  Py_XDECREF(v);
+  return v && dev_ptr(o, &t->p) == 0;
+}
+
+static int two_bytes(const tensor *t) { return t->type == T_BF16 || t->type == T_I16; }
+
+/* A contiguous one. */
+static int dense_tensor(PyObject *o, tensor *t) {
+  return device_tensor(o, t) && is_true(PyObject_CallMethodNoArgs(o, s_is_contiguous));
+}
+
+static int has_shape(const tensor *t, int dims, long long a, long long b, long long c, long long d, long long e) {
+  const long long want[5] = {a, b, c, d, e};
+  if (t->dims != dims) return 0;
+  for (int i = 0; i < dims; ++i)
+    if (t->n[i] != want[i]) return 0;
+  return 1;
+}
+
+/* The stream of a call on tensor x: an address, or None for the current one.  x
+ * has to lie on the current device (the others are taken to lie there too). */
+static int call_stream(PyObject *x, PyObject *o, void **out) {
+  PyObject *dev = PyObject_CallNoArgs(t_device), *own = dev ? PyObject_CallMethodNoArgs(x, s_get_device) : NULL;
+  const int here = own && PyLong_AsLong(own) == PyLong_AsLong(dev);
+  Py_XDECREF(own);
+  int ok = here;
+  if (here && o == Py_None) {
+    PyObject *s = PyObject_CallOneArg(t_stream, dev);
+    *out = s ? (void *)(uintptr_t)PyLong_AsUnsignedLongLongMask(s) : NULL;
+    ok = s && !PyErr_Occurred();
+    Py_XDECREF(s);
+  } else if (here) {
+    ok = dev_ptr(o, out) == 0;
+  }
+  Py_XDECREF(dev);
+  return ok;
+}
+
+static PyObject *leave(void) {
+  PyErr_Clear();
+  Py_RETURN_NONE;
+}
+
+/* int32 counts, one per sequence at least */
+static int count_view(PyObject *o, long long batch, Py_buffer *view) {
+  if (!host_view(o, 'i', 4, 0, view)) return 0;
+  if (view->shape[0] >= batch) return 1;
+  PyBuffer_Release(view);
+  return 0;
+}
+
+/* Rows [tokens][heads][128] with their strides over tokens and heads. */
+static int row_tensor(PyObject *o, tensor *t, int64_t *token, int64_t *head) {
+  long long s[MAX_DIMS];
+  if (!device_tensor(o, t) || t->dims != 3 || t->n[2] != MD_HEAD_DIM) return 0;
+  PyObject *v = PyObject_CallMethodNoArgs(o, s_stride);
+  const int n = tuple_of(v, s);
+  Py_XDECREF(v);
+  if (n != 3 || s[2] != 1) return 0;
+  *token = t->n[0] > 1 ? s[0] : 0;
+  *head = t->n[1] > 1 ? s[1] : 0;
+  return 1;
+}
+
+/* norm_rope(q, k, v, q_out, k_out, v_out, positions, table, q_weight, k_weight,
+ * eps, axes, interleaved, stream) */
+static PyObject *norm_rope(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  if (arity(n, 14)) return NULL;
+  md_norm_rope_args r = {0};
+  tensor x[3], y[3], t;
+  int64_t *in[3][2] = {{&r.q_token, &r.q_head}, {&r.k_token, &r.k_head}, {&r.v_token, &r.v_head}};
+  int64_t *out[3][2] = {{&r.q_out_token, &r.q_out_head}, {&r.k_out_token, &r.k_out_head}, {&r.v_out_token, &r.v_out_head}};
+  if (a[0] == Py_None && a[1] == Py_None) return leave();
+  const int first = a[0] != Py_None ? 0 : 1;
+  for (int i = first; i < 3; ++i) {
+    if (a[i] == Py_None) continue;
+    if (!row_tensor(a[i], &x[i], in[i][0], in[i][1]) || !row_tensor(a[3 + i], &y[i], out[i][0], out[i][1]))
+      return leave();
+    if (x[i].type != x[first].type || x[i].n[0] != x[first].n[0] || !two_bytes(&y[i]) || y[i].n[0] != x[i].n[0] ||
+        y[i].n[1] != x[i].n[1])
+      return leave();
+  }
+  const int hq = a[0] != Py_None, hk = a[1] != Py_None, hv = a[2] != Py_None;
+  if (x[first].type > T_F32 || x[first].n[0] > INT32_MAX || (hv && (!hk || x[2].n[1] != x[1].n[1]))) return leave();
+  r.n_tokens = (int)x[first].n[0];
+  r.type = x[first].type == T_BF16 ? MD_TYPE_BF16 : x[first].type == T_F16 ? MD_TYPE_F16 : MD_TYPE_F32;
+  if (hq) r.q = x[0].p, r.q_out = y[0].p, r.num_q_heads = (int)x[0].n[1];
+  if (hk) r.k = x[1].p, r.k_out = y[1].p, r.num_kv_heads = (int)x[1].n[1];
+  if (hv) r.v = x[2].p, r.v_out = y[2].p;
+  for (int i = 0; i < 2; ++i) {
+    if (a[8 + i] == Py_None || a[i] == Py_None) continue;
+    if (!dense_tensor(a[8 + i], &t) || t.type != T_F32 || !has_shape(&t, 1, MD_HEAD_DIM, 0, 0, 0, 0)) return leave();
+    *(i ? &r.k_weight : &r.q_weight) = (const float *)t.p;
+  }
+  Py_buffer axes = {0};
+  const double eps = PyFloat_AsDouble(a[10]);
+  if (PyErr_Occurred() || !call_stream(a[first], a[13], &r.stream)) return leave();
+  r.eps = (float)eps;
+  r.interleaved = a[12] != Py_False;
+  if (a[7] != Py_None) {
+    if (!dense_tensor(a[7], &t) || t.type != T_F32 || t.dims != 3 || t.n[2] != 2 || t.n[0] > INT32_MAX ||
+        t.n[1] > MD_HEAD_DIM / 2)
+      return leave();
+    r.table = (const float *)t.p;
+    r.table_len = (int)t.n[0];
+    r.rotary_dim = 2 * (int)t.n[1];
+    if (!dense_tensor(a[6], &t) || t.type != T_I32 || t.dims < 1 || t.dims > 2 || t.n[t.dims - 1] != r.n_tokens ||
+        (t.dims == 2 && t.n[0] > MD_MAX_AXES))
+      return leave();
+    r.positions = (const int32_t *)t.p;
+    r.num_axes = t.dims == 2 ? (int)t.n[0] : 1;
+    if (a[11] != Py_None) {
+      if (!host_view(a[11], 'B', 1, 0, &axes)) return leave();
+      if (axes.shape[0] < r.rotary_dim / 2) {
+        PyBuffer_Release(&axes);
+        return leave();
+      }
+      r.axis_host = (const uint8_t *)axes.buf;
+    }
+  }
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_norm_rope(&r);
+  Py_END_ALLOW_THREADS
+  if (r.axis_host) PyBuffer_Release(&axes);
+  return PyLong_FromLong(st);
+}
+
+/* A pool [L][pages][Hkv][2][page_size][128]. */
+static int pool_tensor(PyObject *o, tensor *t) {
+  return dense_tensor(o, t) && t->dims == 6 && two_bytes(t) && t->n[3] == 2 && t->n[5] == MD_HEAD_DIM &&
+         t->n[0] < 256 && t->n[1] < INT32_MAX && t->n[2] < INT32_MAX;
+}
+static int block_table_tensor(PyObject *o, tensor *t) {
+  return dense_tensor(o, t) && t->dims == 2 && t->type == T_I32 && t->n[0] <= MD_MAX_BATCH && t->n[1] < INT32_MAX;
+}
+
+/* page_bounds(pool, block_table, n_tokens, first_pages, bounds, stream) */
+static PyObject *page_bounds(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  tensor pool, table, bounds;
+  void *s;
+  Py_buffer count, first = {0};
+  if (arity(n, 6)) return NULL;
+  if (!pool_tensor(a[0], &pool) || !block_table_tensor(a[1], &table) || !dense_tensor(a[4], &bounds) ||
+      !two_bytes(&bounds) || !has_shape(&bounds, 5, pool.n[0], pool.n[1], pool.n[2], 2, MD_HEAD_DIM) ||
+      !call_stream(a[0], a[5], &s) || !count_view(a[2], table.n[0], &count))
+    return leave();
+  if (a[3] != Py_None && !count_view(a[3], table.n[0], &first)) {
+    PyBuffer_Release(&count);
+    return leave();
+  }
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_page_bounds(pool.p, table.p, count.buf, a[3] == Py_None ? NULL : first.buf, bounds.p, (int)table.n[0],
+                               (int)pool.n[0], (int)pool.n[2], (int)pool.n[4], (int)table.n[1], (int)pool.n[1], s);
+  Py_END_ALLOW_THREADS
+  PyBuffer_Release(&count);
+  if (a[3] != Py_None) PyBuffer_Release(&first);
+  return PyLong_FromLong(st);
+}
+
+/* page_scores(q, bounds, block_table, n_tokens, scores, page_size, stream) */
+static PyObject *page_scores(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  tensor q, bounds, table, scores;
+  void *s;
+  int ps;
+  Py_buffer count;
+  if (arity(n, 7)) return NULL;
+  if (!dense_tensor(a[0], &q) || !two_bytes(&q) || q.dims != 4 || q.n[2] > INT32_MAX || !dense_tensor(a[1], &bounds) ||
+      !two_bytes(&bounds) || bounds.dims != 5 || bounds.n[0] > 255 || bounds.n[1] > INT32_MAX ||
+      bounds.n[2] > INT32_MAX || bounds.n[3] != 2 || bounds.n[4] != MD_HEAD_DIM || !block_table_tensor(a[2], &table) ||
+      !has_shape(&q, 4, table.n[0], bounds.n[0], q.n[2], MD_HEAD_DIM, 0) || !dense_tensor(a[4], &scores) ||
+      scores.type != T_F32 || !has_shape(&scores, 4, table.n[0], bounds.n[0], bounds.n[2], table.n[1], 0) ||
+      as_int(a[5], &ps) || !call_stream(a[0], a[6], &s) || !count_view(a[3], table.n[0], &count))
+    return leave();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_page_scores(q.p, bounds.p, table.p, count.buf, scores.p, (int)table.n[0], (int)bounds.n[0],
+                               (int)q.n[2], (int)bounds.n[2], ps, (int)table.n[1], (int)bounds.n[1], s);
+  Py_END_ALLOW_THREADS
+  PyBuffer_Release(&count);
+  return PyLong_FromLong(st);
+}
+
+/* page_top(scores, n_tokens, page_ids, page_size, first, last, stream) */
+static PyObject *page_top(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  tensor scores, ids;
+  void *s;
+  int ps, first, last;
+  Py_buffer count;
+  if (arity(n, 7)) return NULL;
+  if (!dense_tensor(a[0], &scores) || scores.type != T_F32 || scores.dims != 4 || scores.n[0] > MD_MAX_BATCH ||
+      scores.n[1] > 255 || scores.n[2] > INT32_MAX || scores.n[3] > INT32_MAX || !dense_tensor(a[2], &ids) ||
+      ids.type != T_I32 || ids.dims != 4 || ids.n[3] > INT32_MAX ||
+      !has_shape(&ids, 4, scores.n[0], scores.n[1], scores.n[2], ids.n[3], 0) || as_int(a[3], &ps) ||
+      as_int(a[4], &first) || as_int(a[5], &last) || !call_stream(a[0], a[6], &s) || !count_view(a[1], scores.n[0], &count))
+    return leave();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_page_top(scores.p, count.buf, ids.p, (int)scores.n[0], (int)scores.n[1], (int)scores.n[2], ps,
+                            (int)scores.n[3], (int)ids.n[3], first, last, s);
+  Py_END_ALLOW_THREADS
+  PyBuffer_Release(&count);
+  return PyLong_FromLong(st);
+}
+
+/* attend_pages(q, pool, block_table, n_tokens, page_ids, out, mass, stream) */
+static PyObject *attend_pages(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  tensor q, pool, table, ids, out, mass = {0};
+  void *s;
+  Py_buffer count;
+  if (arity(n, 8)) return NULL;
+  if (!dense_tensor(a[0], &q) || !two_bytes(&q) || q.dims != 4 || q.n[2] > INT32_MAX || !pool_tensor(a[1], &pool) ||
+      !block_table_tensor(a[2], &table) || !has_shape(&q, 4, table.n[0], pool.n[0], q.n[2], MD_HEAD_DIM, 0) ||
+      !dense_tensor(a[4], &ids) || ids.type != T_I32 || ids.dims != 4 || ids.n[3] > MD_MAX_TOP_TOKENS ||
+      !has_shape(&ids, 4, table.n[0], pool.n[0], pool.n[2], ids.n[3], 0) || !dense_tensor(a[5], &out) ||
+      !two_bytes(&out) || !has_shape(&out, 4, q.n[0], q.n[1], q.n[2], q.n[3], 0))
+    return leave();
+  if (a[6] != Py_None &&
+      (!dense_tensor(a[6], &mass) || mass.type != T_F32 ||
+       !has_shape(&mass, 4, table.n[0], pool.n[0], pool.n[2], ids.n[3] * pool.n[4], 0)))
+    return leave();
+  if (!call_stream(a[0], a[7], &s) || !count_view(a[3], table.n[0], &count)) return leave();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_attend_pages(q.p, pool.p, table.p, count.buf, ids.p, out.p, mass.p, (int)table.n[0], (int)pool.n[0],
+                                (int)q.n[2], (int)pool.n[2], (int)pool.n[4], (int)table.n[1], (int)pool.n[1],
+                                (int)ids.n[3], s);
+  Py_END_ALLOW_THREADS
+  PyBuffer_Release(&count);
+  return PyLong_FromLong(st);
+}
+
 static PyMethodDef methods[] = {
     {"load", load, METH_O, "load(path): binds the calls to libmemdecay.so"},
     {"decode_step", (PyCFunction)(void (*)(void))decode_step, METH_FASTCALL, "md_decode_step"},
@@ -217,6 +517,12 @@ static PyMethodDef methods[] = {
     {"decode_layer", (PyCFunction)(void (*)(void))decode_layer, METH_FASTCALL, "md_decode_layer"},
     {"evict", (PyCFunction)(void (*)(void))evict, METH_FASTCALL, "md_evict"},
     {"get_state", (PyCFunction)(void (*)(void))get_state, METH_FASTCALL, "md_get_state"},
+    {"load_torch", (PyCFunction)(void (*)(void))load_torch, METH_FASTCALL, "load_torch(types, device, stream)"},
+    {"norm_rope", (PyCFunction)(void (*)(void))norm_rope, METH_FASTCALL, "md_norm_rope"},
+    {"page_bounds", (PyCFunction)(void (*)(void))page_bounds, METH_FASTCALL, "md_page_bounds"},
+    {"page_scores", (PyCFunction)(void (*)(void))page_scores, METH_FASTCALL, "md_page_scores"},
+    {"page_top", (PyCFunction)(void (*)(void))page_top, METH_FASTCALL, "md_page_top"},
+    {"attend_pages", (PyCFunction)(void (*)(void))attend_pages, METH_FASTCALL, "md_attend_pages"},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
@@ -224,5 +530,9 @@ PyMODINIT_FUNC PyInit__calls(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_is_cuda = PyUnicode_InternFromString("is_cuda");
   s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-  return s_data_ptr && s_is_cuda && s_is_contiguous ? PyModule_Create(&module) : NULL;
+  s_shape = PyUnicode_InternFromString("shape");
+  s_stride = PyUnicode_InternFromString("stride");
+  s_dtype = PyUnicode_InternFromString("dtype");
+  s_get_device = PyUnicode_InternFromString("get_device");
+  return s_data_ptr && s_is_cuda && s_is_contiguous && s_shape && s_stride && s_dtype && s_get_device ? PyModule_Create(&module) : NULL;
 }

@@ -292,6 +292,22 @@ def test_results_repeat_and_streams_are_kept():
 
 
 @gpu
+def test_calls_without_the_c_module_are_the_same(monkeypatch):
+    _need_gpu()
+    c = Case(2, 16, 2, 16, [700, 40, 0], seed=15)
+    got = []
+    for b in (md._binding(), md._NoCalls):
+        monkeypatch.setattr(md, "_torch_calls", None)
+        monkeypatch.setattr(md, "_fast", b)
+        bounds, scores = c.bounds(), torch.zeros((3, 2, 2, c.W), device="cuda")
+        ids = torch.zeros((3, 2, 2, 9), dtype=torch.int32, device="cuda")
+        md.md_page_scores(c.q, bounds, c.bt, c.n, scores, page_size=16)
+        md.md_page_top(scores, c.n.tolist(), ids, page_size=16, first=2, last=3)
+        got.append((bounds, scores, ids) + c.attend(ids))
+    assert all(torch.equal(x, y) for x, y in zip(*got)) and got[0][3].any()
+
+
+@gpu
 def test_pages_past_32_bit_offsets():
     """A pool of more than 2^32 bytes and 2^31 elements: pages at its end."""
     _need_gpu()

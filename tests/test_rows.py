@@ -142,6 +142,24 @@ def test_infinities_and_positions_outside_the_table():
 
 
 @gpu
+def test_calls_without_the_c_module_are_the_same(monkeypatch):
+    """Where Python's headers are missing every call goes through ctypes."""
+    _need_gpu()
+    x = torch.randn((40, 10, D), device="cuda").half()
+    table, pos = md.md_rope_table(_freq(64), 4000), torch.randint(0, 4000, (3, 40), dtype=torch.int32, device="cuda")
+    w, axes = torch.rand(D, device="cuda"), np.arange(64, dtype=np.uint8) % 3
+    outs = []
+    for b in (md._binding(), md._NoCalls):
+        monkeypatch.setattr(md, "_torch_calls", None)
+        monkeypatch.setattr(md, "_fast", b)
+        y = torch.zeros((40, 10, D), dtype=torch.bfloat16, device="cuda")
+        md.md_norm_rope(x[:, :6], x[:, 6:8], x[:, 8:], y[:, :6], y[:, 6:8], y[:, 8:], positions=pos, table=table,
+                        q_weight=w, axes=axes, interleaved=True)
+        outs.append(y)
+    assert torch.equal(*outs) and outs[0].any()
+
+
+@gpu
 def test_rows_on_another_stream():
     """The call goes to the stream it is given, behind the work that stream holds."""
     _need_gpu()
