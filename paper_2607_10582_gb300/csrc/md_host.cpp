@@ -937,14 +937,16 @@ md_status run_sparse(md_ctx *c, int batch, int l0, int L, const void *q_dev, voi
     AttendPagesParams ap;
     (PageSet &)ap = set;
     ap.q = (const uint16_t *)q_dev;
-    ap.pool = pool;
+    ap.l0 = l0;
+    ap.status = ptr<int>(c, c->lay.status);
+    ap.limit_ns = c->spin_limit_ns;
     ap.out = (uint16_t *)out_dev;
     ap.ids = tp.ids;
     ap.mass = nullptr;
     ap.mass_acc = ptr<unsigned long long>(c, c->lay.mass_acc);
     ap.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
     ap.top = c->sparse.top;
-    e = launch_attend_pages(ap, c->stream);
+    e = launch_attend_pages(ap, c->tmap_tile, c->stream);
   }
   prof_end(c, STAGE_ATTN, e0);
   if (e != cudaSuccess) return cuda_fail(c, e, "attention launch");

@@ -270,7 +270,8 @@ cudaError_t launch_observe(const ObserveParams &p, cudaStream_t s);
 
 /* ------------------------------------------- attention over selected pages */
 /* What the page kernels (md_pages.cu) share.  Layers are counted from the
- * launch's first one: pool, bounds, q and out point at its part. */
+ * launch's first one: bounds, q, out and (but for the attention, whose tensor map
+ * holds all layers) pool point at its part. */
 struct PageSet {
   const int32_t *block_table;            // [n_seqs][P_max]
   const uint8_t *page_fill;              // [n_seqs][P_max] tokens per page, or null: full up to n_tokens
@@ -299,15 +300,18 @@ struct PageTopParams {
 };
 cudaError_t launch_page_top(const PageTopParams &p, cudaStream_t s);
 struct AttendPagesParams : PageSet {
-  const uint16_t *q, *pool;
+  const uint16_t *q;
   uint16_t *out;
+  int l0;                                // first layer, in the tensor map
+  int *status;                           // sticky device status words, or null
+  long long limit_ns;                    // of the wait for a copy
   const int32_t *ids;                    // [n_seqs][L][Hkv][top]
   float *mass;                           // [n_seqs][L][Hkv][top][ps], or null
   unsigned long long *mass_acc;          // [slots] fixed-point mass of the step, or null
   float scale_log2;                      // log2(e) / sqrt(D)
   int top;
 };
-cudaError_t launch_attend_pages(const AttendPagesParams &p, cudaStream_t s);
+cudaError_t launch_attend_pages(const AttendPagesParams &p, const CUtensorMap &tile_map, cudaStream_t s);
 
 /* Launch of a kernel taking one parameter struct, with programmatic stream
  * serialization (the kernel calls pdl_wait() before touching global memory). */

@@ -5,8 +5,9 @@
 #include <math.h>
 #include <string.h>
 
-#include "md_internal.h"
-#include "md_ptx.cuh"
+#include <atomic>
+
+#include "md_attn.cuh"
 
 namespace md {
 
@@ -164,210 +165,340 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-/* A block per row: radix select of the k-th largest key, eight bits at a time,
- * then an ordered write of the pages above it and of the first ones equal to it. */
-constexpr int TOP_THREADS = 512;
-__global__ void __launch_bounds__(TOP_THREADS) page_top_kernel(const __grid_constant__ PageTopParams p) {
-  __shared__ int hist[256], warp_gt[TOP_THREADS / 32], warp_eq[TOP_THREADS / 32];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_k;
+/* A block per row.  The keys between the fixed first and last pages go to shared
+ * memory; a histogram over the range that they span (not over fixed bits: the
+ * scores of a row lie close together) finds the bin with the k-th largest, then
+ * one over that bin, until a bin is taken whole or holds equal keys: two rounds
+ * for most rows.  A thread then counts and writes a run of consecutive pages, so that
+ * one scan over the threads gives all places. */
+constexpr int BINS = 2048, TOP_WARPS = 32;
+
+/* Sums of a and b over the threads before this one; every thread calls it. */
+__device__ __forceinline__ int2 scan_before(int a, int b, int2 *warp_sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  int x = a, y = b;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
+    if (lane >= o) {
+      x += u;
+      y += v;
+    }
+  }
+  if (lane == 31) warp_sum[warp] = make_int2(x, y);
+  __syncthreads();
+  int2 w = lane < warps && lane < warp ? warp_sum[lane] : make_int2(0, 0);
+  w.x = __reduce_add_sync(0xffffffffu, w.x);
+  w.y = __reduce_add_sync(0xffffffffu, w.y);
+  return make_int2(x - a + w.x, y - b + w.y);
+}
+
+__global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_constant__ PageTopParams p) {
+  extern __shared__ uint32_t keys[];
+  __shared__ int hist[BINS];
+  __shared__ int2 warp_sum[TOP_WARPS];
+  __shared__ uint32_t warp_lo[TOP_WARPS], warp_hi[TOP_WARPS];
+  __shared__ int s_bin, s_left, s_in;
   pdl_wait();
   pdl_trigger();
   const long long row = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   const int P = p.n_pages[row / p.rows];
-  const float *sc = p.scores + row * p.P_max;
   int32_t *out = p.ids + row * p.top;
   if (P <= p.top) {
-    for (int i = tid; i < p.top; i += TOP_THREADS) out[i] = i < P ? i : -1;
+    for (int i = tid; i < p.top; i += threads) out[i] = i < P ? i : -1;
     return;
   }
-  const int lo = p.first, hi = P - p.last;     // the pages to choose from
-  const int k = p.top - p.first - p.last;
-  for (int i = tid; i < p.first; i += TOP_THREADS) out[i] = i;
-  for (int i = tid; i < p.last; i += TOP_THREADS) out[p.top - p.last + i] = hi + i;
-  if (k == 0) return;
-  uint32_t prefix = 0, mask = 0;
-  int left = k;                                // still to be taken among the keys that match the prefix
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += TOP_THREADS) hist[i] = 0;
-    __syncthreads();
-    for (int i = lo + tid; i < hi; i += TOP_THREADS) {
-      const uint32_t key = score_key(sc[i]);
-      if ((key & mask) == prefix) atomicAdd(&hist[key >> shift & 255], 1);
+  const int n = P - p.first - p.last;          // pages to choose from
+  int left = p.top - p.first - p.last;         // how many
+  const float *sc = p.scores + row * p.P_max + p.first;
+  for (int i = tid; i < p.first; i += threads) out[i] = i;
+  for (int i = tid; i < p.last; i += threads) out[p.top - p.last + i] = P - p.last + i;
+  if (left == 0) return;
+  uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll 4
+  for (int i = tid; i < n; i += threads) {
+    const uint32_t k = score_key(sc[i]);
+    keys[i] = k;
+    lo = min(lo, k);
+    hi = max(hi, k);
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if (lane == 0) {
+    warp_lo[warp] = lo;
+    warp_hi[warp] = hi;
+  }
+  for (int i = tid; i < BINS; i += threads) hist[i] = 0;
+  __syncthreads();
+  lo = __reduce_min_sync(0xffffffffu, lane < warps ? warp_lo[lane] : 0xffffffffu);
+  hi = __reduce_max_sync(0xffffffffu, lane < warps ? warp_hi[lane] : 0u);
+  /* keys above hi are taken, and `left` of those in [lo, hi] */
+  while (true) {
+    const int bits = 32 - __clz(hi - lo), shift = bits > 11 ? bits - 11 : 0;
+    for (int i = tid; i < n; i += threads) {
+      const uint32_t k = keys[i];
+      if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1);
     }
     __syncthreads();
-    if (tid < 32) {                            // the digit of the left-th largest: bins from the top, eight per lane
-      int c[8], sum = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum += c[i] = hist[255 - 8 * lane - i];
-      int incl = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
-      }
-      int before = incl - sum;
-      if (before < left && left <= incl) {
-        int i = 0;
-        while (before + c[i] < left) before += c[i++];
-        s_prefix = prefix | (uint32_t)(255 - 8 * lane - i) << shift;
-        s_k = left - before;
-      }
+    const int each = BINS / threads;           // bins per thread, from the top down
+    int sum = 0;
+    for (int i = 0; i < each; ++i) sum += hist[BINS - 1 - tid * each - i];
+    int before = scan_before(sum, 0, warp_sum).x;
+    if (before < left && left <= before + sum) {
+      int bin = BINS - 1 - tid * each;
+      while (before + hist[bin] < left) before += hist[bin--];
+      s_bin = bin;
+      s_left = left - before;
+      s_in = hist[bin];
     }
     __syncthreads();
-    prefix = s_prefix;
-    left = s_k;
-    mask |= 255u << shift;
+    left = s_left;
+    lo += (uint32_t)s_bin << shift;
+    hi = lo + min(hi - lo, (1u << shift) - 1);
+    if (s_in == left || shift == 0) break;
+    for (int i = tid; i < BINS; i += threads) hist[i] = 0;
     __syncthreads();
   }
-  int done_gt = 0, done_eq = 0;
-  for (int base = lo; base < hi; base += TOP_THREADS) {
-    const int i = base + tid;
-    const uint32_t key = i < hi ? score_key(sc[i]) : 0;
-    const bool gt = i < hi && key > prefix, eq = i < hi && key == prefix;
-    const unsigned mg = __ballot_sync(0xffffffffu, gt), me = __ballot_sync(0xffffffffu, eq);
-    if (lane == 0) {
-      warp_gt[warp] = __popc(mg);
-      warp_eq[warp] = __popc(me);
-    }
-    __syncthreads();
-    int g = done_gt + __popc(mg & ((1u << lane) - 1)), e = done_eq + __popc(me & ((1u << lane) - 1));
-    int tg = 0, te = 0;
-    for (int w = 0; w < TOP_THREADS / 32; ++w) {
-      if (w < warp) {
-        g += warp_gt[w];
-        e += warp_eq[w];
-      }
-      tg += warp_gt[w];
-      te += warp_eq[w];
-    }
-    if (gt || (eq && e < left)) out[p.first + g + min(e, left)] = i;
-    done_gt += tg;
-    done_eq += te;
-    __syncthreads();
+  const int run = (n + threads - 1) / threads | 1;   // odd: no bank conflicts
+  const int r0 = min(n, tid * run), r1 = min(n, r0 + run);
+  int above = 0, equal = 0;
+  for (int i = r0; i < r1; ++i) {
+    above += keys[i] > hi;
+    equal += keys[i] >= lo && keys[i] <= hi;
+  }
+  const int2 at = scan_before(above, equal, warp_sum);
+  int a = at.x, e = at.y;
+  for (int i = r0; i < r1; ++i) {
+    const bool gt = keys[i] > hi, eq = !gt && keys[i] >= lo;
+    if (gt || (eq && e < left)) out[p.first + a + min(e, left)] = p.first + i;
+    a += gt;
+    e += eq;
   }
 }
 
 /* ------------------------------------------------------------- attend --- */
-/* A block per (sequence, layer, KV head).  A warp takes 16 tokens of a page at
- * a time, straight from global memory into MMA fragments:
+/* A cluster of C CTAs of NW warps per (sequence, layer, KV head).  The tiles of
+ * a list, 16 tokens of a page each, go to the cluster's warps in turn; a warp
+ * copies its own tiles by TMA (K and V rows, 64-channel halves, 128-byte
+ * swizzle), one or two in flight, and computes
  *   S = K Q^T   rows are tokens, columns the group's heads
- *   O^T = V^T P^T  rows are channels, summed over the tokens
- * A lane's V words hold two neighbouring channels of one token; exchanging
- * halves with the next token's word makes the fragments of two rows. */
-constexpr int AT_WARPS = 8;
+ *   O^T = V^T P^T  rows are channels, summed over the tokens.
+ *
+ * The weights enter the product as two bf16 terms each (16 bits of them): one
+ * term would add about as much error as the output's own rounding.
+ * They are taken against a base that follows the running maximum only when a
+ * score exceeds it by SLACK: most tiles then need no exchange between lanes and
+ * no rescaling.
+ *
+ * Scores stay in shared memory for the masses, which need the final maxima and
+ * sums.  Each CTA pushes those, and its part of the others' slices of O, into the
+ * others' shared memory; after one cluster barrier each has all it needs.
+ *
+ * A copy that does not land within the limit makes its row NaN (and is reported
+ * in the status words, where there are any). */
+constexpr int SCORE_BYTES = TILE * GP * 4;   // one tile's
+constexpr int TILE_BYTES = 2 * TILE * D * 2; // 16 K rows and 16 V rows
+constexpr int STAGES = 2;                    // most tiles in flight per warp
+constexpr float SLACK = 10.f;                // log2 of the most that a weight may be
+constexpr int OS = D + 4;                    // padded row of a warp's O
+constexpr int MAX_ATTEND_SMEM = 227 * 1024;
+static_assert(GP * OS * 4 <= TILE_BYTES, "a warp's O fits a stage");
+constexpr size_t attend_smem(int C, int warps, int stages, int warp_tiles) {
+  return 1024 + (size_t)warps * (stages * TILE_BYTES + warp_tiles * (SCORE_BYTES + 4)) + 2 * warps * GP * 4 + 2 * GP * 4 +
+         (C > 1 ? (MAX_CLUSTER * GP * 2 + GP * D) * 4 : 0) + warps * STAGES * 8;
+}
 
-struct Tile {
-  uint4 k[8];   // rows g and g + 8: 16 bytes at channels 32 j + 8 t
-  uint4 v[8];   // tokens 2t, 2t + 1, 2t + 8, 2t + 9: channels 8 g .. and 64 + 8 g ..
+struct AttendParams : AttendPagesParams {
+  int C, stages;       // CTAs per row; tiles in flight per warp
+  int warp_tiles;      // most tiles of a warp whose scores are kept
 };
 
-__device__ __forceinline__ void load_k(const uint16_t *page, int valid, int g, int t, uint4 (&k)[8]) {
-  const uint4 none = make_uint4(0, 0, 0, 0);
-  const uint4 *r = (const uint4 *)(page + (size_t)g * D) + t;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    k[2 * j] = g < valid ? r[4 * j] : none;
-    k[2 * j + 1] = g + 8 < valid ? r[4 * j + 16 * 8] : none;
-  }
-}
-__device__ __forceinline__ void load_v(const uint16_t *page, int valid, int g, int t, uint4 (&v)[8]) {
-  const uint4 none = make_uint4(0, 0, 0, 0);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int tok = 2 * t + (i & 1) + 8 * (i >> 1);
-    const uint4 *r = (const uint4 *)(page + (size_t)tok * D) + g;
-    v[2 * i] = tok < valid ? r[0] : none;
-    v[2 * i + 1] = tok < valid ? r[8] : none;
-  }
-}
-/* c[0], c[1]: token g, heads 2t, 2t + 1; c[2], c[3]: token g + 8 */
-__device__ __forceinline__ void tile_scores(const uint4 (&k)[8], const uint32_t (&q)[16], float scale, int valid, int g,
-                                            float (&c)[4]) {
-  float c2[4] = {0.f, 0.f, 0.f, 0.f};
-  c[0] = c[1] = c[2] = c[3] = 0.f;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint4 &x = k[2 * j], &y = k[2 * j + 1];
-    mma_bf16(c, x.x, y.x, x.y, y.y, q[4 * j], q[4 * j + 1]);
-    mma_bf16(c2, x.z, y.z, x.w, y.w, q[4 * j + 2], q[4 * j + 3]);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) c[i] = g + 8 * (i >> 1) < valid ? (c[i] + c2[i]) * scale : -INFINITY;
+/* Bounded wait on an mbarrier phase. */
+__device__ __noinline__ bool wait_copy(uint32_t bar, uint32_t parity, long long limit_ns) {
+  const long long t0 = globaltimer();
+  while (!mbar_try_wait(bar, parity))
+    if (globaltimer() - t0 > limit_ns) return false;
+  return true;
 }
 
-__global__ void __launch_bounds__(32 * AT_WARPS) attend_pages_kernel(const __grid_constant__ AttendPagesParams p) {
-  __shared__ float sm[AT_WARPS][GP], sl[AT_WARPS][GP], so[AT_WARPS][GP][D + 4];
-  __shared__ float fm[GP], fz[GP];
+/* The maxima against which weights are taken: 0 where nothing but -inf was seen. */
+__device__ __forceinline__ float max_base(float m) { return m == -INFINITY ? 0.f : m; }
+
+template <int NW>
+__global__ void __launch_bounds__(32 * NW)
+    attend_pages_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ CUtensorMap tmap) {
+  extern __shared__ uint8_t smem_raw[];
+  const int stages = p.stages, WARP_FLOATS = stages * TILE_BYTES / 4;
+  float *so = (float *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);   // [NW] the warps' stages, later their O [8][OS]
+  float *sc = so + NW * WARP_FLOATS;                 // [NW][warp_tiles][16][8] scores
+  float *sm = sc + NW * p.warp_tiles * TILE * GP;    // [NW][8] maxima, then sums
+  float *sl = sm + NW * GP;
+  float *fin = sl + NW * GP;                         // [8] final maxima, [8] 1 / sums
+  float *xo = fin + 2 * GP;                          // [C][1024 / C] every CTA's part of this one's slice
+  float *xml = xo + (p.C > 1 ? GP * D : 0);          // [C][8][2]
+  uint64_t *full = (uint64_t *)(xml + (p.C > 1 ? MAX_CLUSTER * GP * 2 : 0));   // [NW][STAGES]
+  int *sv = (int *)(full + NW * STAGES);             // [NW][warp_tiles] tokens per tile
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int mi = lane >> 3, rr = lane & 7;           // ldmatrix: matrix and row of this lane's address
+  const int C = p.C, row = blockIdx.x / C, rank = blockIdx.x - row * C;
+  const uint32_t ring = smem_u32(so) + warp * stages * TILE_BYTES, bars = smem_u32(full + warp * STAGES);
+  if (lane < STAGES) {
+    mbar_init(bars + lane * 8, 1);
+    fence_barrier_init();
+  }
+  if (lane == 0) tma_prefetch_desc(&tmap);
+  __syncwarp();
+  if (C > 1) cluster_arrive();                       // this CTA runs: the others may write its shared memory
+  const int lh = p.L * p.Hkv;
+  const int b = row / lh, l = row % lh / p.Hkv, h = row % p.Hkv;
+  const int shift = p.ps / TILE - 1, tiles = p.top << shift;   // tiles per page: 1 or 2
+  const size_t q_row = ((size_t)b * p.L + l) * p.Hq + h * p.G;
+  const int W = C * NW, w = rank * NW + warp;        // warps of the row; this one takes tiles w, w + W, ...
+  const int nt = tiles > w ? (tiles - w + W - 1) / W : 0;
+  float *wsc = sc + warp * p.warp_tiles * TILE * GP;
+  int *wsv = sv + warp * p.warp_tiles;
+  const bool masses = p.mass || p.mass_acc;
+  const uint64_t stream = policy_evict_first();
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const long long row = blockIdx.x;
-  const int lh = p.L * p.Hkv;
-  const int b = (int)(row / lh), l = (int)(row % lh) / p.Hkv, h = (int)(row % p.Hkv);
-  const int tpp = p.ps / TILE, tiles = p.top * tpp;
-  const int32_t *ids = p.ids + row * p.top;
-  const size_t q_row = ((size_t)b * p.L + l) * p.Hq + h * p.G;
-  uint32_t q[16];
-  load_q(p.q + q_row * D, p.G, g, t, q);
-  /* a tile's K rows, or null, and its tokens */
-  auto tile_at = [&](int tile, int &valid) -> const uint16_t * {
-    const int pg = ids[tile / tpp], phys = page_id(p, b, pg), sub = tile % tpp * TILE;
-    valid = 0;
-    if (phys < 0) return nullptr;
-    valid = min(TILE, page_tokens(p, b, pg) - sub);
-    return p.pool + ((((size_t)l * p.P_phys + phys) * p.Hkv + h) * 2 * p.ps + sub) * D;
+  /* tile n0 + lane of this warp: its page's row of the tensor map, its rows' offset there, its tokens */
+  auto tile_info = [&](int n0, int &at, int &sub, int &valid) {
+    at = sub = valid = 0;
+    if (n0 + lane < nt) {
+      const int tile = w + W * (n0 + lane), pg = p.ids[(size_t)row * p.top + (tile >> shift)];
+      const int phys = page_id(p, b, pg);
+      sub = (tile & shift) * TILE;
+      if (phys >= 0) {
+        valid = max(0, min(TILE, page_tokens(p, b, pg) - sub));
+        at = ((p.l0 + l) * p.P_phys + phys) * p.Hkv + h;
+      }
+    }
   };
+  auto copy_tile = [&](int stage, int at, int sub) {
+    const uint32_t dst = ring + stage * TILE_BYTES, bar = bars + stage * 8;
+    mbar_arrive_expect_tx(bar, TILE_BYTES);
+    tma_load_4d(dst, &tmap, 0, sub, 0, at, bar, stream);
+    tma_load_4d(dst + TILE_BYTES / 2, &tmap, 64, sub, 0, at, bar, stream);
+  };
+  int at, sub, valid;
+  tile_info(0, at, sub, valid);
+  uint32_t q[8][2];                                  // head g, channels 16 kk + 2t, + 1 and + 8, + 9
+  {
+    const uint16_t *r = p.q + (q_row + g) * D + 2 * t;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      q[kk][0] = g < p.G ? *(const uint32_t *)(r + 16 * kk) : 0u;
+      q[kk][1] = g < p.G ? *(const uint32_t *)(r + 16 * kk + 8) : 0u;
+    }
+  }
   float m[2] = {-INFINITY, -INFINITY}, z[2] = {0.f, 0.f}, o[8][4];
+  float base[2] = {0.f, 0.f}, lim[2] = {-INFINITY, -INFINITY};
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-  for (int tile = warp; tile < tiles; tile += AT_WARPS) {
-    int valid;
-    const uint16_t *page = tile_at(tile, valid);
-    if (valid <= 0) continue;
-    Tile x;
-    load_k(page, valid, g, t, x.k);
-    load_v(page + (size_t)p.ps * D, valid, g, t, x.v);
-    float c[4];
-    tile_scores(x.k, q, p.scale_log2, valid, g, c);
-    float mx[2] = {fmaxf(c[0], c[2]), fmaxf(c[1], c[3])};
-#pragma unroll
-    for (int s = 4; s < 32; s <<= 1)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], s));
-    float base[2], alpha[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float n = fmaxf(m[i], mx[i]);
-      base[i] = n == -INFINITY ? 0.f : n;     // nothing but -inf so far: weights 0
-      alpha[i] = exp2f(m[i] - base[i]);
-      m[i] = n;
+  int done = 0, issued = 0;                          // tiles of this warp, across the lists of 32
+  bool landed = true;
+  for (int n0 = 0; n0 < nt && landed; n0 += 32) {
+    if (n0) tile_info(n0, at, sub, valid);
+    if (masses && n0 + lane < nt) wsv[n0 + lane] = valid;
+    const unsigned some = __ballot_sync(0xffffffffu, valid > 0);
+    unsigned todo = some, ahead = some;              // tiles to compute, to copy
+    /* the first tiles, a lane each */
+    {
+      if (n0) fence_proxy_async_smem();              // behind the reads of the tiles before
+      const int i = __popc(some & ((1u << lane) - 1));
+      if (valid > 0 && i < stages) copy_tile((done + i) & (stages - 1), at, sub);
+      issued += min(__popc(some), stages);
+      for (int k = 0; k < stages; ++k) ahead &= ahead - 1;
     }
-    float w[4];
+    for (; todo; todo &= todo - 1, ++done) {
+      const int n = __ffs(todo) - 1, have = __shfl_sync(0xffffffffu, valid, n);
+      const int stage = done & (stages - 1);       // stages: 1 or 2
+      const uint32_t st = ring + stage * TILE_BYTES, bar = bars + stage * 8, parity = done >> (stages - 1) & 1;
+      landed = mbar_try_wait(bar, parity) || wait_copy(bar, parity, p.limit_ns);
+      if (!__all_sync(0xffffffffu, landed)) {
+        landed = false;
+        break;
+      }
+      float c[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = exp2f(c[i] - base[i & 1]);
-    z[0] = z[0] * alpha[0] + w[0] + w[2];
-    z[1] = z[1] * alpha[1] + w[1] + w[3];
-    uint32_t hi[2], lo[2];                    // each weight as two bf16: 16 bits of it enter the product
+      for (int kk = 0; kk < 8; ++kk) {
+        uint32_t a0, a1, a2, a3;
+        ldmatrix_x4(swz<TILE>(st, (mi & 1) * 8 + rr, kk * 16 + (mi >> 1) * 8), a0, a1, a2, a3);
+        mma_bf16(kk & 1 ? c2 : c, a0, a1, a2, a3, q[kk][0], q[kk][1]);
+      }
+      /* token g, heads 2t, 2t + 1; token g + 8 */
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t u = pack_bf16(w[2 * i], w[2 * i + 1]);
-      hi[i] = movmatrix_trans(u);
-      lo[i] = movmatrix_trans(pack_bf16(w[2 * i] - __uint_as_float(u << 16), w[2 * i + 1] - __uint_as_float(u & 0xffff0000u)));
+      for (int i = 0; i < 4; ++i)
+        c[i] = g + 8 * (i >> 1) < have && 2 * t + (i & 1) < p.G ? (c[i] + c2[i]) * p.scale_log2 : -INFINITY;
+      if (masses) {
+        float *d = wsc + (n0 + n) * TILE * GP + g * GP + 2 * t;
+        *(float2 *)d = make_float2(c[0], c[1]);
+        *(float2 *)(d + 8 * GP) = make_float2(c[2], c[3]);
+      }
+      float mx[2] = {fmaxf(c[0], c[2]), fmaxf(c[1], c[3])};
+      if (__any_sync(0xffffffffu, mx[0] > lim[0] || mx[1] > lim[1])) {
+#pragma unroll
+        for (int s = 4; s < 32; s <<= 1)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], s));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          m[i] = fmaxf(m[i], mx[i]);
+          const float alpha = ex2(base[i] - max_base(m[i]));
+          base[i] = max_base(m[i]);
+          lim[i] = m[i] + SLACK;
+          z[i] *= alpha;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            o[j][i] *= alpha;
+            o[j][2 + i] *= alpha;
+          }
+        }
+      }
+      uint32_t hi[2], lo[2];
+      {
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = ex2(c[j] - base[j & 1]);
+        z[0] += x[0] + x[2];
+        z[1] += x[1] + x[3];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t u = pack_bf16(x[2 * j], x[2 * j + 1]);
+          hi[j] = movmatrix_trans(u);
+          lo[j] = movmatrix_trans(
+              pack_bf16(x[2 * j] - __uint_as_float(u << 16), x[2 * j + 1] - __uint_as_float(u & 0xffff0000u)));
+        }
+      }
+      /* V rows past the tile's tokens, whatever they hold: the last one again */
+      const int vrow = TILE + min((mi >> 1) * 8 + rr, have - 1);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t a0, a1, a2, a3;
+        ldmatrix_x4_trans(swz<TILE>(st, vrow, i * 16 + (mi & 1) * 8), a0, a1, a2, a3);
+        mma_bf16(o[i], a0, a1, a2, a3, hi[0], hi[1]);
+        mma_bf16(o[i], a0, a1, a2, a3, lo[0], lo[1]);
+      }
+      __syncwarp();
+      if (ahead) {                                   // refill the stage: its reads come before the copy
+        const int k = __ffs(ahead) - 1;
+        const int at_k = __shfl_sync(0xffffffffu, at, k), sub_k = __shfl_sync(0xffffffffu, sub, k);
+        if (lane == 0) {
+          fence_proxy_async_smem();
+          copy_tile(stage, at_k, sub_k);
+        }
+        ++issued;
+        ahead &= ahead - 1;
+      }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint4 *v = x.v + (i >> 2);
-      auto word = [&](int tok) { return ((const uint32_t *)&v[2 * tok])[i & 3]; };
-      const uint32_t a0 = __byte_perm(word(0), word(1), 0x5410), a1 = __byte_perm(word(0), word(1), 0x7632),
-                     a2 = __byte_perm(word(2), word(3), 0x5410), a3 = __byte_perm(word(2), word(3), 0x7632);
-      o[i][0] *= alpha[0];
-      o[i][1] *= alpha[1];
-      o[i][2] *= alpha[0];
-      o[i][3] *= alpha[1];
-      mma_bf16(o[i], a0, a1, a2, a3, hi[0], hi[1]);
-      mma_bf16(o[i], a0, a1, a2, a3, lo[0], lo[1]);
+  }
+  if (!landed) {                                     // what is in flight must land before the stages are reused
+    for (; done < issued; ++done) wait_copy(bars + (done & (stages - 1)) * 8, done >> (stages - 1) & 1, DRAIN_LIMIT_NS);
+    z[0] = z[1] = NAN;
+    if (p.status && lane == 0) {
+      atomicCAS(&p.status[ST_CODE], 0, (int)MD_ERR_DEVICE_TIMEOUT);
+      atomicExch(&p.status[ST_ABORT], 1);
     }
   }
 #pragma unroll
@@ -377,72 +508,131 @@ __global__ void __launch_bounds__(32 * AT_WARPS) attend_pages_kernel(const __gri
   if (g == 0)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      sm[warp][2 * t + i] = m[i];
-      sl[warp][2 * t + i] = z[i];
+      sm[warp * GP + 2 * t + i] = m[i];
+      sl[warp * GP + 2 * t + i] = z[i];
     }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {               // channels of o[i]: rows g and g + 8
-    const int d = (i >> 2) * 64 + 8 * g + 2 * (i & 3);
+  for (int i = 0; i < 8; ++i)                 // channels 16 i + g and + 8
 #pragma unroll
-    for (int k = 0; k < 2; ++k) *(float2 *)&so[warp][2 * t + k][d] = make_float2(o[i][k], o[i][2 + k]);
-  }
+    for (int j = 0; j < 4; ++j) so[warp * WARP_FLOATS + (2 * t + (j & 1)) * OS + 16 * i + g + 8 * (j >> 1)] = o[i][j];
   __syncthreads();
-  const int head = threadIdx.x >> 5;          // 8 warps: a head each, 4 channels per lane
-  {
-    float top = -INFINITY, sum = 0.f;
-    for (int w = 0; w < AT_WARPS; ++w) top = fmaxf(top, sm[w][head]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int w = 0; w < AT_WARPS; ++w) {
-      const float f = exp2f(sm[w][head] - base);
-      const float4 y = *(const float4 *)&so[w][head][4 * lane];
-      sum += f * sl[w][head];
-      acc.x += f * y.x;
-      acc.y += f * y.y;
-      acc.z += f * y.z;
-      acc.w += f * y.w;
-    }
-    const float r = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);   // no token: zeros; NaN stays
-    if (head < p.G)
-      *(uint2 *)(p.out + (q_row + head) * D + 4 * lane) =
-          make_uint2(pack_bf16(acc.x * r, acc.y * r), pack_bf16(acc.z * r, acc.w * r));
-    if (lane == 0) {
-      fm[head] = base;
-      fz[head] = head < p.G ? r : 0.f;
+  /* the CTA's sums: 4 channels of a head per thread, 8 / NW heads per warp */
+  const int slice = GP * D / C;
+  float4 acc[GP / NW];
+  float top[GP / NW], sum[GP / NW];
+#pragma unroll
+  for (int i = 0; i < GP / NW; ++i) {
+    const int head = warp + i * NW;
+    top[i] = -INFINITY;
+#pragma unroll
+    for (int y = 0; y < NW; ++y) top[i] = fmaxf(top[i], sm[y * GP + head]);
+    const float base = max_base(top[i]);
+    sum[i] = 0.f;
+    acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int y = 0; y < NW; ++y) {
+      const float f = ex2(sm[y * GP + head] - base);
+      const float4 e = *(const float4 *)&so[y * WARP_FLOATS + head * OS + 4 * lane];
+      sum[i] += f * sl[y * GP + head];
+      acc[i].x += f * e.x;
+      acc[i].y += f * e.y;
+      acc[i].z += f * e.z;
+      acc[i].w += f * e.w;
     }
   }
-  if (!p.mass && !p.mass_acc) return;
-  __syncthreads();
-  float *mass = p.mass + row * p.top * p.ps;
+  auto inverse = [](float s) { return s > 0.f ? 1.f / s : s == 0.f ? 0.f : s; };   // no token: zeros; NaN stays
+  if (C == 1) {
+#pragma unroll
+    for (int i = 0; i < GP / NW; ++i) {
+      const int head = warp + i * NW;
+      const float r = inverse(sum[i]);
+      if (head < p.G)
+        *(uint2 *)(p.out + (q_row + head) * D + 4 * lane) =
+            make_uint2(pack_bf16(acc[i].x * r, acc[i].y * r), pack_bf16(acc[i].z * r, acc[i].w * r));
+      if (lane == 0) {
+        fin[head] = max_base(top[i]);
+        fin[GP + head] = head < p.G ? r : 0.f;
+      }
+    }
+    if (!masses) return;
+    __syncthreads();
+  } else {
+    cluster_wait();                           // every CTA runs
+#pragma unroll
+    for (int i = 0; i < GP / NW; ++i) {
+      const int head = warp + i * NW, e = head * D + 4 * lane, to = e / slice;
+      st_cluster_v4(cluster_map(smem_u32(xo + rank * slice + e - to * slice), to), acc[i].x, acc[i].y, acc[i].z, acc[i].w);
+      if (lane < C) st_cluster_v2(cluster_map(smem_u32(xml + (rank * GP + head) * 2), lane), top[i], sum[i]);
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (threadIdx.x < GP) {
+      const int head = threadIdx.x;
+      float most = -INFINITY, s = 0.f;
+      for (int y = 0; y < C; ++y) most = fmaxf(most, xml[(y * GP + head) * 2]);
+      most = max_base(most);
+      for (int y = 0; y < C; ++y) s += ex2(xml[(y * GP + head) * 2] - most) * xml[(y * GP + head) * 2 + 1];
+      fin[head] = most;
+      fin[GP + head] = head < p.G ? inverse(s) : 0.f;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x * 4; e < slice; e += 32 * NW * 4) {
+      const int at_e = rank * slice + e, head = at_e / D;
+      const float r = fin[GP + head];
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < C; ++i) {
+        const float f = ex2(xml[(i * GP + head) * 2] - fin[head]);
+        const float4 x = *(const float4 *)&xo[i * slice + e];
+        y.x += f * x.x;
+        y.y += f * x.y;
+        y.z += f * x.z;
+        y.w += f * x.w;
+      }
+      if (head < p.G)
+        *(uint2 *)(p.out + q_row * D + at_e) =
+            make_uint2(pack_bf16(y.x * r, y.y * r), pack_bf16(y.z * r, y.w * r));
+    }
+    if (!masses) return;
+  }
+  /* the masses of this warp's tiles: a lane per token, two tiles at a time */
+  float fm[GP], fz[GP];
+#pragma unroll
+  for (int i = 0; i < GP; ++i) {
+    fm[i] = fin[i];
+    fz[i] = fin[GP + i];
+  }
   const uint64_t keep = policy_evict_last();
-  const float m0 = fm[2 * t], m1 = fm[2 * t + 1], r0 = fz[2 * t], r1 = fz[2 * t + 1];
-  for (int tile = warp; tile < tiles; tile += AT_WARPS) {
-    int valid;
-    const uint16_t *page = tile_at(tile, valid);
-    float w0 = 0.f, w1 = 0.f;
-    if (valid > 0) {
-      uint4 k[8];
-      float c[4];
-      load_k(page, valid, g, t, k);
-      tile_scores(k, q, p.scale_log2, valid, g, c);
-      w0 = (r0 != 0.f ? exp2f(c[0] - m0) * r0 : 0.f) + (r1 != 0.f ? exp2f(c[1] - m1) * r1 : 0.f);
-      w1 = (r0 != 0.f ? exp2f(c[2] - m0) * r0 : 0.f) + (r1 != 0.f ? exp2f(c[3] - m1) * r1 : 0.f);
+  const int tok = lane & 15;
+#pragma unroll 2
+  for (int n0 = 0; n0 < nt; n0 += 2) {
+    const int n = n0 + (lane >> 4), tile = w + W * n;
+    if (n >= nt) continue;
+    const int have = wsv[n];
+    const float4 *s = (const float4 *)(wsc + (n * TILE + tok) * GP);
+    float x = 0.f;
+    if (tok < have) {
+      const float4 u = s[0], v = s[1];
+      x = (ex2(u.x - fm[0]) * fz[0] + ex2(u.y - fm[1]) * fz[1]) + (ex2(u.z - fm[2]) * fz[2] + ex2(u.w - fm[3]) * fz[3]);
+      x += (ex2(v.x - fm[4]) * fz[4] + ex2(v.y - fm[5]) * fz[5]) + (ex2(v.z - fm[6]) * fz[6] + ex2(v.w - fm[7]) * fz[7]);
     }
-#pragma unroll
-    for (int s = 1; s < 4; s <<= 1) {
-      w0 += __shfl_xor_sync(0xffffffffu, w0, s);
-      w1 += __shfl_xor_sync(0xffffffffu, w1, s);
-    }
-    if (t == 0 && p.mass) {
-      mass[tile * TILE + g] = w0;
-      mass[tile * TILE + 8 + g] = w1;
-    }
-    if (t == 0 && p.mass_acc && valid > 0) {
-      unsigned long long *acc = p.mass_acc + (size_t)page_id(p, b, ids[tile / tpp]) * p.ps + tile % tpp * TILE;
-      if (g < valid) red_add_u64_hint(acc + g, __float2ull_rn(w0 * MASS_SCALE), keep);
-      if (g + 8 < valid) red_add_u64_hint(acc + g + 8, __float2ull_rn(w1 * MASS_SCALE), keep);
-    }
+    if (p.mass) p.mass[((size_t)row * tiles + tile) * TILE + tok] = x;
+    if (p.mass_acc && tok < have)
+      red_add_u64_hint(p.mass_acc + (size_t)page_id(p, b, p.ids[(size_t)row * p.top + (tile >> shift)]) * p.ps +
+                           (tile & shift) * TILE + tok,
+                       __float2ull_rn(x * MASS_SCALE), keep);
   }
+}
+
+/* Runs f (a kernel's attributes) once per device; KEY: the kernel. */
+template <int KEY, class F>
+cudaError_t once_per_device(F f) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && done.load() >> dev & 1)) return e;
+  e = f();
+  if (e == cudaSuccess && dev < 64) done.fetch_or(1ULL << dev);
+  return e;
 }
 
 }  // namespace
@@ -474,11 +664,67 @@ cudaError_t launch_page_scores(const PageScoresParams &p, cudaStream_t s) {
 }
 
 cudaError_t launch_page_top(const PageTopParams &p, cudaStream_t s) {
-  return launch_pdl(page_top_kernel, p.n_seqs * p.rows, TOP_THREADS, 0, s, p);
+  int most = 0;
+  for (int b = 0; b < p.n_seqs; ++b) most = p.n_pages[b] > most ? p.n_pages[b] : most;
+  if (most <= p.top) most = 0;                 // nothing to choose: no keys
+  static_assert((size_t)MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS / 16 * 4 <= 64 * 1024, "the longest row's keys");
+  const cudaError_t e = once_per_device<0>(
+      [] { return cudaFuncSetAttribute(page_top_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024); });
+  if (e != cudaSuccess) return e;
+  const int threads = most <= 1024 ? 256 : most <= 8192 ? 512 : 1024;
+  return launch_pdl(page_top_kernel, p.n_seqs * p.rows, threads, most * 4, s, p);
 }
 
-cudaError_t launch_attend_pages(const AttendPagesParams &p, cudaStream_t s) {
-  return launch_pdl(attend_pages_kernel, p.n_seqs * p.L * p.Hkv, 32 * AT_WARPS, 0, s, p);
+namespace {
+
+template <int NW>
+cudaError_t launch_attend(const AttendParams &p, const CUtensorMap &tmap, cudaStream_t s) {
+  const cudaError_t e = once_per_device<NW>([] {
+    const cudaError_t e =
+        cudaFuncSetAttribute(attend_pages_kernel<NW>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_ATTEND_SMEM);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(attend_pages_kernel<NW>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  });
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.n_seqs * p.L * p.Hkv * p.C));
+  cfg.blockDim = dim3(32 * NW);
+  cfg.dynamicSmemBytes = attend_smem(p.C, NW, p.stages, p.warp_tiles);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.C;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.C > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, attend_pages_kernel<NW>, p, tmap);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_pages(const AttendPagesParams &base, const CUtensorMap &tmap, cudaStream_t s) {
+  AttendParams p;
+  (AttendPagesParams &)p = base;
+  const long long rows = (long long)p.n_seqs * p.L * p.Hkv;
+  const int tiles = p.top * (p.ps / TILE);
+  int NW = 4;
+  p.C = 1;
+  p.stages = 1;
+  if (rows >= 128) {
+    NW = tiles <= 96 ? 4 : 8;
+  } else {
+    while (p.C < MAX_CLUSTER && rows * p.C * 4 < 600 && p.C * NW < tiles) p.C *= 2;
+    if (p.C * NW < tiles && rows * p.C * 8 < 1300) NW = 8;
+    p.stages = 2;
+  }
+  /* the scores' room, wanted or not: the split, and with it the result, does not depend on it */
+  auto room = [&] { return attend_smem(p.C, NW, p.stages, (tiles + p.C * NW - 1) / (p.C * NW)); };
+  if (room() > MAX_ATTEND_SMEM) p.stages = 1;
+  while (room() > MAX_ATTEND_SMEM && p.C < MAX_CLUSTER) p.C *= 2;
+  if (room() > MAX_ATTEND_SMEM) NW = 4;
+  p.warp_tiles = p.mass || p.mass_acc ? (tiles + p.C * NW - 1) / (p.C * NW) : 0;
+  return NW == 8 ? launch_attend<8>(p, tmap, s) : launch_attend<4>(p, tmap, s);
 }
 
 namespace {
@@ -491,7 +737,7 @@ bool page_set(PageSet &p, const int32_t *block_table, const int32_t *n_tokens, i
       P_max < 1 || P_phys < 1 || (long long)P_max * ps > (long long)MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS)
     return false;
   if (Hq && (Hq < Hkv || Hq % Hkv || Hq / Hkv > MD_MAX_GROUP)) return false;
-  if ((long long)L * P_phys * Hkv * 2 * ps >= (1LL << 31) || (long long)batch * L * Hkv >= (1LL << 31)) return false;
+  if ((long long)L * P_phys * Hkv * 2 * ps >= (1LL << 31) || (long long)batch * L * Hkv >= (1LL << 27)) return false;
   p.block_table = block_table;
   p.page_fill = nullptr;
   p.L = L;
@@ -508,6 +754,20 @@ bool page_set(PageSet &p, const int32_t *block_table, const int32_t *n_tokens, i
     p.n_pages[b] = (n_tokens[b] + ps - 1) / ps;
   }
   return true;
+}
+
+/* The driver's tensor-map encoder, looked up once per process. */
+void *tile_encoder() {
+  static std::atomic<void *> known{nullptr};
+  void *fn = known.load();
+  if (!fn) {
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      return nullptr;
+    known.store(fn);
+  }
+  return fn;
 }
 
 bool misaligned(const void *p) { return !p || ((uintptr_t)p & 15); }
@@ -588,12 +848,18 @@ MD_API md_status md_attend_pages(const void *q, const void *pool, const int32_t 
                 num_phys_pages))
     return MD_ERR_INVALID_ARG;
   p.q = (const uint16_t *)q;
-  p.pool = (const uint16_t *)pool;
   p.out = (uint16_t *)out;
   p.ids = page_ids;
   p.mass = mass;
   p.mass_acc = nullptr;
   p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
   p.top = top_pages;
-  return launch_attend_pages(p, (cudaStream_t)stream) == cudaSuccess ? MD_OK : MD_ERR_CUDA;
+  p.l0 = 0;
+  p.status = nullptr;
+  p.limit_ns = 2000000000LL;
+  void *encode = tile_encoder();
+  CUtensorMap tmap;
+  const size_t rows = (size_t)num_layers * num_phys_pages * num_kv_heads * 2 * page_size;
+  if (!encode || !encode_tile_map(encode, &tmap, (void *)pool, rows, page_size)) return MD_ERR_CUDA;
+  return launch_attend_pages(p, tmap, (cudaStream_t)stream) == cudaSuccess ? MD_OK : MD_ERR_CUDA;
 }

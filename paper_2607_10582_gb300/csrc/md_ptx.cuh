@@ -157,6 +157,12 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+/* 2^x, to about 2 ulp; results below 2^-126 are 0 */
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 /* two fp32 -> packed bf16x2 (round to nearest even); lo in the low half */
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
