@@ -8,6 +8,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/memdecay.h"
 
 namespace md {
@@ -328,6 +330,19 @@ cudaError_t launch_pdl(void (*kernel)(P), int grid, int threads, int smem, cudaS
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+/* Runs f (it sets kernel attributes) once per device; WHICH: for which kernels. */
+enum { ATTR_TOP, ATTR_ATTEND_4, ATTR_ATTEND_8, ATTR_ROWS };
+template <int WHICH, class F>
+cudaError_t once_per_device(F f) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && done.load() >> dev & 1)) return e;
+  e = f();
+  if (e == cudaSuccess && dev < 64) done.fetch_or(1ULL << dev);
+  return e;
 }
 
 /* --------------------------------------------------------------- init --- */

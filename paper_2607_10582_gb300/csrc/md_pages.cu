@@ -623,18 +623,6 @@ __global__ void __launch_bounds__(32 * NW)
   }
 }
 
-/* Runs f (a kernel's attributes) once per device; KEY: the kernel. */
-template <int KEY, class F>
-cudaError_t once_per_device(F f) {
-  static std::atomic<unsigned long long> done{0};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess || (dev < 64 && done.load() >> dev & 1)) return e;
-  e = f();
-  if (e == cudaSuccess && dev < 64) done.fetch_or(1ULL << dev);
-  return e;
-}
-
 }  // namespace
 
 cudaError_t launch_bounds(const BoundsParams &p, cudaStream_t s) {
@@ -668,7 +656,7 @@ cudaError_t launch_page_top(const PageTopParams &p, cudaStream_t s) {
   for (int b = 0; b < p.n_seqs; ++b) most = p.n_pages[b] > most ? p.n_pages[b] : most;
   if (most <= p.top) most = 0;                 // nothing to choose: no keys
   static_assert((size_t)MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS / 16 * 4 <= 64 * 1024, "the longest row's keys");
-  const cudaError_t e = once_per_device<0>(
+  const cudaError_t e = once_per_device<ATTR_TOP>(
       [] { return cudaFuncSetAttribute(page_top_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024); });
   if (e != cudaSuccess) return e;
   const int threads = most <= 1024 ? 256 : most <= 8192 ? 512 : 1024;
@@ -679,7 +667,7 @@ namespace {
 
 template <int NW>
 cudaError_t launch_attend(const AttendParams &p, const CUtensorMap &tmap, cudaStream_t s) {
-  const cudaError_t e = once_per_device<NW>([] {
+  const cudaError_t e = once_per_device<NW == 8 ? ATTR_ATTEND_8 : ATTR_ATTEND_4>([] {
     const cudaError_t e =
         cudaFuncSetAttribute(attend_pages_kernel<NW>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_ATTEND_SMEM);
     return e != cudaSuccess ? e : cudaFuncSetAttribute(attend_pages_kernel<NW>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);

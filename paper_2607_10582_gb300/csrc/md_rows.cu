@@ -5,6 +5,8 @@
 
 #include <string.h>
 
+#include <algorithm>
+
 #include "md_internal.h"
 #include "md_ptx.cuh"
 
@@ -12,150 +14,276 @@ namespace md {
 
 namespace {
 
+/* The rows of q, k and v: element (token, head, d) is at token * token_stride +
+ * head * head_stride + d. */
+struct Rows {
+  const void *in;
+  uint16_t *out;
+  const float *weight;        // null: no norm
+  long long in_token, in_head, out_token, out_head;
+  int heads, rotate;
+};
 struct RowsParams {
-  md_norm_rope_args a;
-  int parts, rows_per_part;   // a token's rows are split over `parts` half-warps
-  uint8_t axis[D / 2];
+  Rows set[3];
+  const float2 *table;
+  const int32_t *positions;
+  long long n_tokens;
+  int table_len, rotary_dim;
+  float eps;
+  int split_log;              // a token's rows are split over 2^split_log units (4 at least)
+  unsigned long long axes[2]; // the axis of pair q: 2 bits at 2 (q % 32) of word q / 32
 };
 
-/* 4 consecutive elements, as they are and as fp32 */
-template <class T>
-struct Raw {
-  typedef uint2 type;
-};
-template <>
-struct Raw<float> {
-  typedef float4 type;
-};
-__device__ __forceinline__ void widen(const uint2 &u, float (&x)[4], __nv_bfloat16) {
-  x[0] = __uint_as_float(u.x << 16);
-  x[1] = __uint_as_float(u.x & 0xffff0000u);
-  x[2] = __uint_as_float(u.y << 16);
-  x[3] = __uint_as_float(u.y & 0xffff0000u);
+/* ---- pairs of fp32 in one 64-bit register, two results per instruction ---- */
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
 }
-__device__ __forceinline__ void widen(const uint2 &u, float (&x)[4], __half) {
-  const float2 a = __half22float2(*(const __half2 *)&u.x), b = __half22float2(*(const __half2 *)&u.y);
-  x[0] = a.x;
-  x[1] = a.y;
-  x[2] = b.x;
-  x[3] = b.y;
+__device__ __forceinline__ float2 parts(f32x2 x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
 }
-__device__ __forceinline__ void widen(const float4 &u, float (&x)[4], float) {
-  x[0] = u.x;
-  x[1] = u.y;
-  x[2] = u.z;
-  x[3] = u.w;
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
-__device__ __forceinline__ void store4(uint16_t *p, const float (&x)[4]) {
-  *(uint2 *)p = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
 }
 
-/* A half-warp per token, or per part of a token's rows: what the rows share
- * (table entries, weights) is loaded once.  A row is eight elements per lane, two
- * groups of four, chosen so that a lane holds both channels of its four pairs:
- * 4j .. and R/2 + 4j .. for the pairs (i, i + R/2), 8j .. 8j + 7 for (2i, 2i + 1);
- * lanes past the rotated channels hold the rest.  Four rows are in flight. */
+/* Two consecutive elements as fp32. */
+__device__ __forceinline__ f32x2 load2(const __nv_bfloat16 *p) {
+  const uint32_t u = *(const uint32_t *)p;
+  return pair(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
+__device__ __forceinline__ f32x2 load2(const __half *p) {
+  const float2 f = __half22float2(*(const __half2 *)p);
+  return pair(f.x, f.y);
+}
+__device__ __forceinline__ f32x2 load2(const float *p) {
+  const float2 f = *(const float2 *)p;
+  return pair(f.x, f.y);
+}
+__device__ __forceinline__ uint32_t pack2(f32x2 x) {
+  const float2 f = parts(x);
+  return pack_bf16(f.x, f.y);
+}
+
+/* What a row's lane multiplies its elements with.  With n the norm's factor, w the
+ * weights (1 where there is none) and (c, s) the pair's table entry:
+ *   out_a = n (x_a (w_a c) + x_b (-w_b s)),  out_b = n (x_b (w_b c) + x_a (w_a s));
+ * the four products are made once per token. */
+
+/* 8 consecutive elements in registers, as they came */
 template <class T>
-__global__ void __launch_bounds__(256) norm_rope_kernel(const __grid_constant__ RowsParams p) {
-  typedef typename Raw<T>::type raw;
-  constexpr int FLIGHT = 4;
+struct Eight {
+  uint4 q[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = ((const uint4 *)p)[i];
+  }
+  __device__ __forceinline__ f32x2 two(int i) const { return load2((const T *)q + 2 * i); }
+};
+
+/* A unit of eight lanes per row, 16 elements per lane, two runs of eight that hold both
+ * channels of eight pairs: 8j .. and R/2 + 8j .. for the pairs (i, i + R/2), 16j ..
+ * for (2i, 2i + 1) (INTER); lanes past the rotated channels hold the rest.  A warp's
+ * four units take neighbouring rows of one token, every 2^split-th row each, and load
+ * the next row before they compute the one at hand. */
+constexpr int WARPS = 2;
+
+template <class T, bool INTER>
+__global__ void __launch_bounds__(32 * WARPS, 20 / WARPS) norm_rope_kernel(const __grid_constant__ RowsParams p) {
+  struct Row {
+    Eight<T> u, v;
+  };
+  __shared__ float4 entries[WARPS][32];                  // [4][8 lanes] the entries of two pairs
+  const int lane = threadIdx.x & 31, j = lane & 7;
+  float4 *cs = entries[threadIdx.x >> 5];
+  const unsigned lanes = 0xffu << (lane & 24);
+  const int R = p.rotary_dim, pairs = R / 2, split = p.split_log, step = 1 << split;   // split >= 2
+  const bool rot = 16 * j < R;
+  const int e0 = INTER || !rot ? 16 * j : 8 * j, e1 = INTER || !rot ? e0 + 8 : R / 2 + 8 * j;
+  const long long unit = ((long long)blockIdx.x * 32 * WARPS + threadIdx.x) >> 3;
+  const long long tok = unit >> split;
+  if (tok >= p.n_tokens) return;                         // the whole warp
+  int row = (int)unit & (step - 1);                      // of the token's q, k and v rows, in this order
+  const int h0 = p.set[0].heads, h1 = h0 + p.set[1].heads, h2 = h1 + p.set[2].heads;
   pdl_wait();
   pdl_trigger();
-  const md_norm_rope_args &a = p.a;
-  const int j = threadIdx.x & 15;
-  const long long unit = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
-  if (unit >= (long long)a.n_tokens * p.parts) return;   // whole half-warps; the shuffles stay inside them
-  const unsigned half = threadIdx.x & 16 ? 0xffff0000u : 0xffffu;
-  const long long tok = unit / p.parts;
-  const int first = (int)(unit - tok * p.parts) * p.rows_per_part;   // of the token's q, k and v rows, in this order
-  const int R = a.rotary_dim;
-  const bool rot = 8 * j < R;
-  const int e0 = a.interleaved || !rot ? 8 * j : 4 * j, e1 = a.interleaved || !rot ? e0 + 4 : R / 2 + 4 * j;
-  float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
-  if (rot) {
+  int pos[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int pos = a.positions[(size_t)p.axis[4 * j + i] * a.n_tokens + tok];
-      float2 cs = make_float2(NAN, NAN);
-      if (pos >= 0 && pos < a.table_len) cs = ((const float2 *)a.table)[(size_t)pos * (R / 2) + 4 * j + i];
-      c[i] = cs.x;
-      s[i] = cs.y;
-    }
+  for (int i = 0; i < 2; ++i) {
+    const int q = lane + 32 * i;
+    pos[i] = q < pairs ? p.positions[(long long)(p.axes[i] >> 2 * lane & 3) * p.n_tokens + tok] : -1;
   }
-  /* rows lo .. hi - 1 of one of q, k, v */
-  auto rows = [&](const void *in, int64_t in_token, int64_t in_head, void *out, int64_t out_token, int64_t out_head,
-                  const float *w, bool value, int lo, int hi) {
-    const T *src = (const T *)in + tok * in_token;
-    uint16_t *dst = (uint16_t *)out + tok * out_token;
-    float wx[4], wy[4];
-    if (w) {
-      widen(*(const float4 *)(w + e0), wx, 0.f);
-      widen(*(const float4 *)(w + e1), wy, 0.f);
-    }
-    for (int h0 = lo; h0 < hi; h0 += FLIGHT) {
-      raw u[FLIGHT], v[FLIGHT];
+  auto fetch = [&](Row &x, int at) {
+    if (at >= h2) return;
+    const T *src = at < h0   ? (const T *)p.set[0].in + tok * p.set[0].in_token + at * p.set[0].in_head
+                   : at < h1 ? (const T *)p.set[1].in + tok * p.set[1].in_token + (at - h0) * p.set[1].in_head
+                             : (const T *)p.set[2].in + tok * p.set[2].in_token + (at - h1) * p.set[2].in_head;
+    x.u.load(src + e0);
+    x.v.load(src + e1);
+  };
+  Row now, next;
+  fetch(now, row);
 #pragma unroll
-      for (int r = 0; r < FLIGHT; ++r) {
-        const T *x = src + min(h0 + r, hi - 1) * in_head;
-        u[r] = *(const raw *)(x + e0);
-        v[r] = *(const raw *)(x + e1);
+  for (int i = 0; i < 2; ++i) {
+    const int q = lane + 32 * i;
+    if (q < pairs)
+      ((float2 *)cs)[((q & 7) / 2 * 8 + q / 8) * 2 + (q & 1)] =
+          pos[i] >= 0 && pos[i] < p.table_len ? p.table[(size_t)pos[i] * pairs + q] : make_float2(NAN, NAN);
+  }
+  __syncwarp();
+  /* the factors of run u, and of run v, with their own and with the other channel */
+  f32x2 uu[4], uv[4], vv[4], vu[4];
+  auto factors = [&](const float *w) {
+    const float4 *e = cs + j;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float4 wu = make_float4(1.f, 1.f, 1.f, 1.f), wv = wu;
+      if (w) {
+        wu = *(const float4 *)(w + e0 + 4 * h);
+        wv = *(const float4 *)(w + e1 + 4 * h);
       }
 #pragma unroll
-      for (int r = 0; r < FLIGHT; ++r) {
-        if (h0 + r >= hi) break;
-        float x[4], y[4];
-        widen(u[r], x, T());
-        widen(v[r], y, T());
-        if (w) {
-          float sum = 0.f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sum += x[i] * x[i] + y[i] * y[i];
-#pragma unroll
-          for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(half, sum, o);
-          const float f = rsqrtf(sum * (1.f / D) + a.eps);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[i] *= f * wx[i];
-            y[i] *= f * wy[i];
-          }
+      for (int n = 0; n < 2; ++n) {
+        const int i = 2 * h + n;
+        const float2 a = n ? make_float2(wu.z, wu.w) : make_float2(wu.x, wu.y);
+        const float2 b = n ? make_float2(wv.z, wv.w) : make_float2(wv.x, wv.y);
+        uu[i] = pair(a.x, a.y);
+        vv[i] = pair(b.x, b.y);
+        if (!rot) continue;
+        if (INTER) {                                     // word i of run u is pair i, of run v pair i + 4
+          const float4 c = e[(i / 2) * 8], d = e[(i / 2 + 2) * 8];
+          const float2 x = i & 1 ? make_float2(c.z, c.w) : make_float2(c.x, c.y);
+          const float2 y = i & 1 ? make_float2(d.z, d.w) : make_float2(d.x, d.y);
+          uu[i] = pair(a.x * x.x, a.y * x.x);
+          uv[i] = pair(-a.y * x.y, a.x * x.y);
+          vv[i] = pair(b.x * y.x, b.y * y.x);
+          vu[i] = pair(-b.y * y.y, b.x * y.y);
+        } else {                                         // pairs 2i, 2i + 1
+          const float4 c = e[i * 8];
+          uu[i] = pair(a.x * c.x, a.y * c.z);
+          uv[i] = pair(-b.x * c.y, -b.y * c.w);
+          vv[i] = pair(b.x * c.x, b.y * c.z);
+          vu[i] = pair(a.x * c.y, a.y * c.w);
         }
-        if (rot && !value) {
-          float n[4], m[4];
-          if (a.interleaved) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              n[2 * i] = x[2 * i] * c[i] - x[2 * i + 1] * s[i];
-              n[2 * i + 1] = x[2 * i + 1] * c[i] + x[2 * i] * s[i];
-              m[2 * i] = y[2 * i] * c[i + 2] - y[2 * i + 1] * s[i + 2];
-              m[2 * i + 1] = y[2 * i + 1] * c[i + 2] + y[2 * i] * s[i + 2];
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              n[i] = x[i] * c[i] - y[i] * s[i];
-              m[i] = y[i] * c[i] + x[i] * s[i];
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[i] = n[i];
-            y[i] = m[i];
-          }
-        }
-        uint16_t *d = dst + (h0 + r) * out_head;
-        store4(d + e0, x);
-        store4(d + e1, y);
       }
     }
   };
-  const int last = first + p.rows_per_part, Hq = a.num_q_heads, Hkv = a.num_kv_heads;
-  auto clip = [&](int n, int at) { return max(0, min(n, at)); };
-  rows(a.q, a.q_token, a.q_head, a.q_out, a.q_out_token, a.q_out_head, a.q_weight, false, clip(Hq, first), clip(Hq, last));
-  rows(a.k, a.k_token, a.k_head, a.k_out, a.k_out_token, a.k_out_head, a.k_weight, false, clip(Hkv, first - Hq),
-       clip(Hkv, last - Hq));
-  if (a.v)
-    rows(a.v, a.v_token, a.v_head, a.v_out, a.v_out_token, a.v_out_head, nullptr, true, clip(Hkv, first - Hq - Hkv),
-         clip(Hkv, last - Hq - Hkv));
+  const float *have = (const float *)1;                  // whose factors are at hand: no weights' yet
+#pragma unroll 1
+  for (; row < h2; row += step, now = next) {
+    fetch(next, row + step);
+    uint4 u, v;
+    uint32_t *ou = &u.x, *ov = &v.x;
+    uint16_t *dst;
+    if (row >= h1) {                                     // a value row
+      dst = p.set[2].out + tok * p.set[2].out_token + (row - h1) * p.set[2].out_head;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        ou[i] = pack2(now.u.two(i));
+        ov[i] = pack2(now.v.two(i));
+      }
+    } else {
+      const bool is_q = row < h0;
+      dst = is_q ? p.set[0].out + tok * p.set[0].out_token + row * p.set[0].out_head
+                 : p.set[1].out + tok * p.set[1].out_token + (row - h0) * p.set[1].out_head;
+      const float *w = is_q ? p.set[0].weight : p.set[1].weight;
+      if (have != w) factors(w);
+      have = w;
+      f32x2 x[4], y[4], f = pair(1.f, 1.f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = now.u.two(i);
+        y[i] = now.v.two(i);
+      }
+      if (w) {
+        f32x2 s2 = mul2(x[0], x[0]), t2 = mul2(y[0], y[0]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) {
+          s2 = fma2(x[i], x[i], s2);
+          t2 = fma2(y[i], y[i], t2);
+        }
+        const float2 s = parts(s2), t = parts(t2);
+        float sum = (s.x + s.y) + (t.x + t.y);
+#pragma unroll
+        for (int o = 4; o; o >>= 1) sum += __shfl_xor_sync(lanes, sum, o);
+        const float n = rsqrtf(sum * (1.f / D) + p.eps);
+        f = pair(n, n);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x2 m = mul2(x[i], uu[i]), n = mul2(y[i], vv[i]);
+        if (rot) {
+          const float2 g = parts(x[i]), h = parts(y[i]);
+          m = fma2(INTER ? pair(g.y, g.x) : y[i], uv[i], m);
+          n = fma2(INTER ? pair(h.y, h.x) : x[i], vu[i], n);
+        }
+        ou[i] = pack2(mul2(m, f));
+        ov[i] = pack2(mul2(n, f));
+      }
+    }
+    *(uint4 *)(dst + e0) = u;
+    *(uint4 *)(dst + e1) = v;
+  }
+}
+
+/* Any layout that the call takes: 8-byte aligned rows, any multiple of 8 as
+ * rotary_dim.  A warp per row, two pairs (or four elements) per lane. */
+template <class T>
+__global__ void __launch_bounds__(256) norm_rope_any_kernel(const __grid_constant__ RowsParams p, int inter) {
+  pdl_wait();
+  pdl_trigger();
+  const int j = threadIdx.x & 31;
+  const int all = p.set[0].heads + p.set[1].heads + p.set[2].heads;
+  const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (unit >= p.n_tokens * all) return;
+  const long long tok = unit / all;
+  int k = 0, row = (int)(unit - tok * all);
+  while (row >= p.set[k].heads) row -= p.set[k++].heads;
+  const Rows &set = p.set[k];
+  const int R = p.rotary_dim;
+  const bool rot = 4 * j < R;
+  const int e0 = inter || !rot ? 4 * j : 2 * j, e1 = inter || !rot ? e0 + 2 : R / 2 + 2 * j;
+  const T *src = (const T *)set.in + tok * set.in_token + row * set.in_head;
+  uint16_t *dst = set.out + tok * set.out_token + row * set.out_head;
+  float2 x = parts(load2(src + e0)), y = parts(load2(src + e1));
+  if (set.weight) {
+    float sum = (x.x * x.x + x.y * x.y) + (y.x * y.x + y.y * y.y);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float n = rsqrtf(sum * (1.f / D) + p.eps);
+    x = make_float2(x.x * n * set.weight[e0], x.y * n * set.weight[e0 + 1]);
+    y = make_float2(y.x * n * set.weight[e1], y.y * n * set.weight[e1 + 1]);
+  }
+  if (rot && set.rotate) {
+    float2 cs[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int q = 2 * j + i;
+      const int pos = p.positions[(long long)((q < 32 ? p.axes[0] : p.axes[1]) >> 2 * (q & 31) & 3) * p.n_tokens + tok];
+      cs[i] = make_float2(NAN, NAN);
+      if (pos >= 0 && pos < p.table_len) cs[i] = p.table[(size_t)pos * (R / 2) + 2 * j + i];
+    }
+    const float2 u = x, v = y;
+    if (inter) {
+      x = make_float2(u.x * cs[0].x - u.y * cs[0].y, u.y * cs[0].x + u.x * cs[0].y);
+      y = make_float2(v.x * cs[1].x - v.y * cs[1].y, v.y * cs[1].x + v.x * cs[1].y);
+    } else {
+      x = make_float2(u.x * cs[0].x - v.x * cs[0].y, u.y * cs[1].x - v.y * cs[1].y);
+      y = make_float2(v.x * cs[0].x + u.x * cs[0].y, v.y * cs[1].x + u.y * cs[1].y);
+    }
+  }
+  *(uint32_t *)(dst + e0) = pack_bf16(x.x, x.y);
+  *(uint32_t *)(dst + e1) = pack_bf16(y.x, y.y);
 }
 
 struct TableParams {
@@ -176,7 +304,9 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const __grid_constant__
   }
 }
 
-constexpr int UNITS = 152 * 128;
+constexpr int ROUND = 152 * 3 * 32;   // units that run at once
+
+static_assert(MD_MAX_AXES <= 4 && D / 2 <= 64, "an axis is two bits");
 
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 bool rows_ok(const void *p, int64_t token, int64_t head, size_t align) {
@@ -210,9 +340,7 @@ MD_API md_status md_rope_table(const double *inv_freq, int rotary_dim, int table
 MD_API md_status md_norm_rope(const md_norm_rope_args *args) {
   using namespace md;
   if (!args) return MD_ERR_INVALID_ARG;
-  RowsParams p;
-  p.a = *args;
-  md_norm_rope_args &a = p.a;
+  const md_norm_rope_args &a = *args;
   if (a.n_tokens < 0 || a.num_q_heads < 0 || a.num_kv_heads < 0 || a.num_q_heads > 65535 || a.num_kv_heads > 65535 ||
       a.type < MD_TYPE_BF16 || a.type > MD_TYPE_F32 || a.rotary_dim < 0 || a.rotary_dim > D || a.rotary_dim % 8 ||
       !(a.eps >= 0.f))
@@ -227,30 +355,66 @@ MD_API md_status md_norm_rope(const md_norm_rope_args *args) {
       return MD_ERR_INVALID_ARG;
   }
   if (!aligned(a.q_weight, 16) || !aligned(a.k_weight, 16)) return MD_ERR_INVALID_ARG;
-  memset(p.axis, 0, sizeof(p.axis));
+  RowsParams p;
+  memset(&p, 0, sizeof(p));
   if (a.rotary_dim > 0) {
     if (!a.table || !aligned(a.table, 16) || !a.positions || a.num_axes < 1 || a.num_axes > MD_MAX_AXES || a.table_len < 1)
       return MD_ERR_INVALID_ARG;
     for (int i = 0; a.axis_host && i < a.rotary_dim / 2; ++i) {
       if (a.axis_host[i] >= a.num_axes) return MD_ERR_INVALID_ARG;
-      p.axis[i] = a.axis_host[i];
+      p.axes[i / 32] |= (unsigned long long)a.axis_host[i] << 2 * (i & 31);
     }
   }
-  const int rows = a.num_q_heads + a.num_kv_heads * (a.v ? 2 : 1);
+  const int values = a.v ? a.num_kv_heads : 0, rows = a.num_q_heads + a.num_kv_heads + values;
   if (a.n_tokens == 0 || rows == 0) return MD_OK;
-  /* as many parts as keep about UNITS half-warps busy */
-  p.parts = (int)(UNITS / a.n_tokens < 1 ? 1 : UNITS / a.n_tokens > rows ? rows : UNITS / a.n_tokens);
-  p.rows_per_part = (rows + p.parts - 1) / p.parts;
-  p.parts = (rows + p.rows_per_part - 1) / p.rows_per_part;
-  const long long blocks = ((long long)a.n_tokens * p.parts + 15) / 16;
-  if (blocks >= (1LL << 31)) return MD_ERR_INVALID_ARG;
+  p.set[0] = {a.q, (uint16_t *)a.q_out, a.q_weight, a.q_token, a.q_head, a.q_out_token, a.q_out_head, a.num_q_heads, 1};
+  p.set[1] = {a.k, (uint16_t *)a.k_out, a.k_weight, a.k_token, a.k_head, a.k_out_token, a.k_out_head, a.num_kv_heads, 1};
+  p.set[2] = {a.v, (uint16_t *)a.v_out, nullptr, a.v_token, a.v_head, a.v_out_token, a.v_out_head, values, 0};
+  p.table = (const float2 *)a.table;
+  p.positions = a.positions;
+  p.n_tokens = a.n_tokens;
+  p.table_len = a.table_len;
+  p.rotary_dim = a.rotary_dim;
+  p.eps = a.eps;
   const cudaStream_t s = (cudaStream_t)a.stream;
+  const int type = a.type;
+  const bool inter = a.interleaved != 0;
   cudaError_t e;
-  if (a.type == MD_TYPE_BF16)
-    e = launch_pdl(norm_rope_kernel<__nv_bfloat16>, (int)blocks, 256, 0, s, p);
-  else if (a.type == MD_TYPE_F16)
-    e = launch_pdl(norm_rope_kernel<__half>, (int)blocks, 256, 0, s, p);
-  else
-    e = launch_pdl(norm_rope_kernel<float>, (int)blocks, 256, 0, s, p);
+  bool wide = a.rotary_dim % 16 == 0;
+  for (const Rows &r : p.set) {
+    const long long to = type == MD_TYPE_F32 ? 4 : 8;    // elements in 16 bytes
+    if (r.heads)
+      wide = wide && aligned(r.in, 16) && aligned(r.out, 16) && r.in_token % to == 0 && r.in_head % to == 0 &&
+             r.out_token % 8 == 0 && r.out_head % 8 == 0;
+  }
+  if (wide) {
+    /* a unit per row while one round of blocks has room for them */
+    p.split_log = 2;
+    while (1 << p.split_log < rows && (long long)a.n_tokens << (p.split_log + 1) <= ROUND) ++p.split_log;
+    const long long blocks = (((long long)a.n_tokens << p.split_log) + 4 * WARPS - 1) / (4 * WARPS);
+    if (blocks >= (1LL << 31)) return MD_ERR_INVALID_ARG;
+    auto launch = [&](auto plain, auto interleaved) {
+      return launch_pdl(inter ? interleaved : plain, (int)blocks, 32 * WARPS, 0, s, p);
+    };
+    e = type == MD_TYPE_BF16  ? launch(norm_rope_kernel<__nv_bfloat16, false>, norm_rope_kernel<__nv_bfloat16, true>)
+        : type == MD_TYPE_F16 ? launch(norm_rope_kernel<__half, false>, norm_rope_kernel<__half, true>)
+                              : launch(norm_rope_kernel<float, false>, norm_rope_kernel<float, true>);
+  } else {
+    const long long blocks = ((long long)a.n_tokens * rows + 7) / 8;
+    if (blocks >= (1LL << 31)) return MD_ERR_INVALID_ARG;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(256);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    auto launch = [&](auto kernel) { return cudaLaunchKernelEx(&cfg, kernel, p, (int)inter); };
+    e = type == MD_TYPE_BF16  ? launch(norm_rope_any_kernel<__nv_bfloat16>)
+        : type == MD_TYPE_F16 ? launch(norm_rope_any_kernel<__half>)
+                              : launch(norm_rope_any_kernel<float>);
+  }
   return e == cudaSuccess ? MD_OK : MD_ERR_CUDA;
 }
