@@ -333,7 +333,7 @@ cudaError_t launch_pdl(void (*kernel)(P), int grid, int threads, int smem, cudaS
 }
 
 /* Runs f (it sets kernel attributes) once per device; WHICH: for which kernels. */
-enum { ATTR_TOP, ATTR_ATTEND_4, ATTR_ATTEND_8, ATTR_ROWS };
+enum { ATTR_ATTEND_4, ATTR_ATTEND_8 };
 template <int WHICH, class F>
 cudaError_t once_per_device(F f) {
   static std::atomic<unsigned long long> done{0};

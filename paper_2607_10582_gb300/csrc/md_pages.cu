@@ -5,6 +5,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "md_attn.cuh"
@@ -165,12 +166,15 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-/* A block per row.  The keys between the fixed first and last pages go to shared
- * memory; a histogram over the range that they span (not over fixed bits: the
- * scores of a row lie close together) finds the bin with the k-th largest, then
- * one over that bin, until a bin is taken whole or holds equal keys: two rounds
- * for most rows.  A thread then counts and writes a run of consecutive pages, so that
- * one scan over the threads gives all places. */
+/* A block per row, KEYS keys per thread in registers.  A histogram over the range
+ * that the row's keys span (not over fixed bits: the scores of a row lie close
+ * together) finds the bin with the k-th largest, then one over that bin, until a bin is
+ * taken whole or holds equal keys: two rounds for most rows.  The pages that are
+ * taken become bits, and one scan over the words of bits gives all places.
+ *
+ * Latency bounds it: barriers and round trips through shared memory.  2 rows of 2,048
+ * pages 5.6 us, 576 rows of 4,096 (keys in shared memory, a second pass over them
+ * for the places) 15.7. */
 constexpr int BINS = 2048, TOP_WARPS = 32;
 
 /* Sums of a and b over the threads before this one; every thread calls it. */
@@ -193,11 +197,11 @@ __device__ __forceinline__ int2 scan_before(int a, int b, int2 *warp_sum) {
   return make_int2(x - a + w.x, y - b + w.y);
 }
 
+template <int KEYS>
 __global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_constant__ PageTopParams p) {
-  extern __shared__ uint32_t keys[];
   __shared__ int hist[BINS];
   __shared__ int2 warp_sum[TOP_WARPS];
-  __shared__ uint32_t warp_lo[TOP_WARPS], warp_hi[TOP_WARPS];
+  __shared__ uint32_t warp_lo[TOP_WARPS], warp_hi[TOP_WARPS], above[TOP_WARPS * KEYS], equal[TOP_WARPS * KEYS];
   __shared__ int s_bin, s_left, s_in;
   pdl_wait();
   pdl_trigger();
@@ -215,13 +219,16 @@ __global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_c
   for (int i = tid; i < p.first; i += threads) out[i] = i;
   for (int i = tid; i < p.last; i += threads) out[p.top - p.last + i] = P - p.last + i;
   if (left == 0) return;
-  uint32_t lo = 0xffffffffu, hi = 0;
-#pragma unroll 4
-  for (int i = tid; i < n; i += threads) {
-    const uint32_t k = score_key(sc[i]);
-    keys[i] = k;
-    lo = min(lo, k);
-    hi = max(hi, k);
+  uint32_t k[KEYS], lo = 0xffffffffu, hi = 0;
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {
+    const int at = tid + i * threads;
+    k[i] = at < n ? score_key(sc[at]) : 0u;    // 0: the key of no score
+  }
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {
+    lo = min(lo, k[i] - 1);                    // past the end: 0xffffffff
+    hi = max(hi, k[i]);
   }
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
@@ -231,15 +238,15 @@ __global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_c
   }
   for (int i = tid; i < BINS; i += threads) hist[i] = 0;
   __syncthreads();
-  lo = __reduce_min_sync(0xffffffffu, lane < warps ? warp_lo[lane] : 0xffffffffu);
+  lo = __reduce_min_sync(0xffffffffu, lane < warps ? warp_lo[lane] : 0xffffffffu) + 1;
   hi = __reduce_max_sync(0xffffffffu, lane < warps ? warp_hi[lane] : 0u);
   /* keys above hi are taken, and `left` of those in [lo, hi] */
   while (true) {
-    const int bits = 32 - __clz(hi - lo), shift = bits > 11 ? bits - 11 : 0;
-    for (int i = tid; i < n; i += threads) {
-      const uint32_t k = keys[i];
-      if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1);
-    }
+    const uint32_t span = hi - lo;
+    const int bits = 32 - __clz(span), shift = bits > 11 ? bits - 11 : 0;
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i)
+      if (k[i] - lo <= span) atomicAdd(&hist[(k[i] - lo) >> shift], 1);
     __syncthreads();
     const int each = BINS / threads;           // bins per thread, from the top down
     int sum = 0;
@@ -260,20 +267,25 @@ __global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_c
     for (int i = tid; i < BINS; i += threads) hist[i] = 0;
     __syncthreads();
   }
-  const int run = (n + threads - 1) / threads | 1;   // odd: no bank conflicts
-  const int r0 = min(n, tid * run), r1 = min(n, r0 + run);
-  int above = 0, equal = 0;
-  for (int i = r0; i < r1; ++i) {
-    above += keys[i] > hi;
-    equal += keys[i] >= lo && keys[i] <= hi;
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {             // word w: pages 32 w ..
+    const unsigned gt = __ballot_sync(0xffffffffu, k[i] > hi), eq = __ballot_sync(0xffffffffu, k[i] - lo <= hi - lo);
+    if (lane == 0) {
+      above[warp + i * warps] = gt;
+      equal[warp + i * warps] = eq;
+    }
   }
-  const int2 at = scan_before(above, equal, warp_sum);
+  __syncthreads();
+  const bool mine = tid < KEYS * warps;        // a word per thread
+  uint32_t gt = mine ? above[tid] : 0u, eq = mine ? equal[tid] : 0u;
+  const int2 at = scan_before(__popc(gt), __popc(eq), warp_sum);
   int a = at.x, e = at.y;
-  for (int i = r0; i < r1; ++i) {
-    const bool gt = keys[i] > hi, eq = !gt && keys[i] >= lo;
-    if (gt || (eq && e < left)) out[p.first + a + min(e, left)] = p.first + i;
-    a += gt;
-    e += eq;
+  for (uint32_t any = gt | eq; any; any &= any - 1) {
+    const uint32_t bit = any & (0u - any);
+    const bool is_gt = gt & bit;
+    if (is_gt || e < left) out[p.first + a + min(e, left)] = p.first + 32 * tid + __ffs(bit) - 1;
+    a += is_gt;
+    e += !is_gt;
   }
 }
 
@@ -654,13 +666,13 @@ cudaError_t launch_page_scores(const PageScoresParams &p, cudaStream_t s) {
 cudaError_t launch_page_top(const PageTopParams &p, cudaStream_t s) {
   int most = 0;
   for (int b = 0; b < p.n_seqs; ++b) most = p.n_pages[b] > most ? p.n_pages[b] : most;
-  if (most <= p.top) most = 0;                 // nothing to choose: no keys
-  static_assert((size_t)MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS / 16 * 4 <= 64 * 1024, "the longest row's keys");
-  const cudaError_t e = once_per_device<ATTR_TOP>(
-      [] { return cudaFuncSetAttribute(page_top_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024); });
-  if (e != cudaSuccess) return e;
-  const int threads = most <= 1024 ? 256 : most <= 8192 ? 512 : 1024;
-  return launch_pdl(page_top_kernel, p.n_seqs * p.rows, threads, most * 4, s, p);
+  static_assert(MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS / 16 <= 16 * 32 * TOP_WARPS, "the longest row has its keys");
+  const int rows = p.n_seqs * p.rows;
+  return most <= 1024   ? launch_pdl(page_top_kernel<4>, rows, 256, 0, s, p)
+         : most <= 2048 ? launch_pdl(page_top_kernel<8>, rows, 256, 0, s, p)
+         : most <= 4096 ? launch_pdl(page_top_kernel<8>, rows, 512, 0, s, p)
+         : most <= 8192 ? launch_pdl(page_top_kernel<8>, rows, 1024, 0, s, p)
+                        : launch_pdl(page_top_kernel<16>, rows, 1024, 0, s, p);
 }
 
 namespace {
@@ -691,28 +703,80 @@ cudaError_t launch_attend(const AttendParams &p, const CUtensorMap &tmap, cudaSt
 
 }  // namespace
 
+namespace {
+
+struct AttendForm {
+  int C = 0, warps = 0, stages = 0;
+};
+
+/* How many CTAs and warps per row, and how many tiles in flight per warp: the least
+ * of these costs in us.  Their constants were fitted to 70 launches timed on a GB300
+ * in up to 20 forms each (1 to 64 sequences, 1 to 36 layers, 2 to 600 tiles per
+ * list, 2 to 1,472 rows): the choice takes 1.8% longer than the best form of each
+ * on average, 20% at worst.  n: tiles of a warp, N: CTAs, hbm: K/V bytes at 6.8
+ * TB/s, slots: CTAs that run at once (a cluster of 8 or 16 leaves parts of the
+ * chip unused, and more so with one CTA per SM).
+ *   Shared memory is counted with the scores' room whether masses are wanted or
+ * not: the split, and with it the rounding of a result, does not depend on it.
+ *   One row pair of 64 tiles (one layer of one sequence): 4.6 us with 16 x 4 warps,
+ * 8.4 with 8 warps; 288 rows of 256: 101 us with 8 warps per row (two rounds of one
+ * CTA per SM), 126 and more with the other forms at one tile in flight but 4 x 4. */
+AttendForm attend_form(const AttendPagesParams &p) {
+  constexpr float SMS = 152.f;
+  const int tpp = p.ps / TILE, listed = p.top * tpp;
+  long long sum = 0;
+  int T = 1;
+  for (int b = 0; b < p.n_seqs; ++b) {
+    const int t = (p.n_pages[b] < p.top ? p.n_pages[b] : p.top) * tpp;
+    sum += t;
+    T = t > T ? t : T;
+  }
+  const float rows = (float)p.n_seqs * p.L * p.Hkv, hbm = (float)sum * p.L * p.Hkv * (TILE_BYTES / 6.8e6f);
+  AttendForm best;
+  float least = INFINITY;
+  for (int lg = 0; lg < 5; ++lg)
+    for (int warps = 4; warps <= 8; warps += 4)
+      for (int stages = 1; stages <= STAGES; ++stages) {
+        const int C = 1 << lg, W = C * warps;
+        if (W > 2 * listed && W > 8) continue;
+        const size_t smem = attend_smem(C, warps, stages, (listed + W - 1) / W);
+        if (smem > MAX_ATTEND_SMEM) continue;
+        const int per_sm = std::min(16 / warps, (int)(228 * 1024 / (smem + 1024)));
+        const float part = C <= 2 ? 1.f : per_sm > 1 ? (C == 4 ? 0.97f : C == 8 ? 0.93f : 0.72f)
+                                                     : (C == 4 ? 0.94f : C == 8 ? 0.78f : 0.6f);
+        const float slots = per_sm * SMS * part, N = rows * C;
+        const float cta = 5.4f + (C > 1 ? 0.9f : 0.f) + (C == 16 ? 0.15f : 0.f) + (warps == 8 ? 0.24f : 0.f) +
+                          (float)((T + W - 1) / W) * (stages == 1 ? 0.98f : 0.57f);
+        float cost;
+        if (N <= slots)
+          cost = std::max(cta, hbm * 1.1f + 1.9f) + 0.0026f * N;
+        else
+          cost = std::max(hbm * 1.1f + 1.9f + 0.46f * cta, 0.9f * N / slots * cta) + 0.0026f * slots +
+                 (C > 1 ? 0.014f * N : 0.f);
+        if (cost < least) {
+          least = cost;
+          best.C = C;
+          best.warps = warps;
+          best.stages = stages;
+        }
+      }
+  return best;
+}
+
+}  // namespace
+
 cudaError_t launch_attend_pages(const AttendPagesParams &base, const CUtensorMap &tmap, cudaStream_t s) {
   AttendParams p;
   (AttendPagesParams &)p = base;
-  const long long rows = (long long)p.n_seqs * p.L * p.Hkv;
-  const int tiles = p.top * (p.ps / TILE);
-  int NW = 4;
-  p.C = 1;
-  p.stages = 1;
-  if (rows >= 128) {
-    NW = tiles <= 96 ? 4 : 8;
-  } else {
-    while (p.C < MAX_CLUSTER && rows * p.C * 4 < 600 && p.C * NW < tiles) p.C *= 2;
-    if (p.C * NW < tiles && rows * p.C * 8 < 1300) NW = 8;
-    p.stages = 2;
-  }
-  /* the scores' room, wanted or not: the split, and with it the result, does not depend on it */
-  auto room = [&] { return attend_smem(p.C, NW, p.stages, (tiles + p.C * NW - 1) / (p.C * NW)); };
-  if (room() > MAX_ATTEND_SMEM) p.stages = 1;
-  while (room() > MAX_ATTEND_SMEM && p.C < MAX_CLUSTER) p.C *= 2;
-  if (room() > MAX_ATTEND_SMEM) NW = 4;
-  p.warp_tiles = p.mass || p.mass_acc ? (tiles + p.C * NW - 1) / (p.C * NW) : 0;
-  return NW == 8 ? launch_attend<8>(p, tmap, s) : launch_attend<4>(p, tmap, s);
+  const AttendForm f = attend_form(base);
+  if (f.C == 0) return cudaErrorInvalidConfiguration;   // MD_MAX_TOP_TOKENS fit 16 CTAs of 4 warps
+  static_assert(attend_smem(MAX_CLUSTER, 4, 1, MD_MAX_TOP_TOKENS / TILE / (4 * MAX_CLUSTER)) <= MAX_ATTEND_SMEM,
+                "the longest list has a form");
+  const int W = f.C * f.warps;
+  p.C = f.C;
+  p.stages = f.stages;
+  p.warp_tiles = p.mass || p.mass_acc ? (p.top * (p.ps / TILE) + W - 1) / W : 0;
+  return f.warps == 8 ? launch_attend<8>(p, tmap, s) : launch_attend<4>(p, tmap, s);
 }
 
 namespace {

@@ -1,8 +1,9 @@
 """md_sparse_enable: decode steps of a handle over selected pages.
 
 With contiguous pages a step's output is that of the page calls on the handle's own pool
-and table, bit for bit, and its mass their masses' sum; tests/test_pages.py holds those
-calls to their formulas.  Region-aligned pages are held to the formulas directly, with the
+and table, bit for bit, and its mass their masses' sum (for a layer-by-layer step, calls of
+one layer each: how a row is split, and so its rounding, goes by a launch's size);
+tests/test_pages.py holds those calls to their formulas.  Region-aligned pages are held to the formulas directly, with the
 tolerances given there."""
 import ctypes
 import math
@@ -70,7 +71,7 @@ class Loop:
     def pages(self):
         return [self.c.query(md.MD_QUERY_PAGES, b) for b in range(self.B)]
 
-    def by_page_calls(self, q, top, first, last):
+    def by_page_calls(self, q, top, first, last, each_layer):
         """The step just run, by the page calls: output, and mass per slot."""
         pool, bt, n = self.c.get_state(md.MD_STATE_POOL), self.c.get_state(md.MD_STATE_BLOCK_TABLE), self.tokens()
         L, P, W, rows = self.L, pool.shape[1], bt.shape[1], (self.B, self.L, self.Hkv)
@@ -81,7 +82,11 @@ class Loop:
         md.md_page_bounds(pool, bt, n, bounds)
         md.md_page_scores(q, bounds, bt, n, scores, page_size=self.ps)
         md.md_page_top(scores, n, ids, page_size=self.ps, first=first, last=last)
-        md.md_attend_pages(q, pool, bt, n, ids, out, mass=mass)
+        for l in range(L) if each_layer else [slice(None)]:
+            part = slice(l, l + 1) if each_layer else l
+            o, m = torch.empty_like(q[:, part]).contiguous(), torch.empty_like(mass[:, part]).contiguous()
+            md.md_attend_pages(q[:, part].contiguous(), pool[part], bt, n, ids[:, part].contiguous(), o, mass=m)
+            out[:, part], mass[:, part] = o, m
         acc = torch.zeros(P * self.ps, dtype=torch.float64, device="cuda")
         for b in range(self.B):
             i = ids[b].long()
@@ -93,7 +98,7 @@ class Loop:
     def check(self, how, top, first=1, last=1):
         q, out = self.step(how)
         mass = self.c.get_state(md.MD_STATE_MASS).double() * UNIT
-        want, acc = self.by_page_calls(q, top, first, last)
+        want, acc = self.by_page_calls(q, top, first, last, how == "layers")
         assert torch.equal(out, want)
         # each addend is rounded to 2^-48
         assert (mass - acc).abs().max() <= self.L * self.Hkv * 2.0 ** -48 + 2.0 ** -50 * self.L * self.Hq
