@@ -318,9 +318,9 @@ cudaError_t launch_attend_pages(const AttendPagesParams &p, const CUtensorMap &t
 /* Launch of a kernel taking one parameter struct, with programmatic stream
  * serialization (the kernel calls pdl_wait() before touching global memory). */
 template <class P>
-cudaError_t launch_pdl(void (*kernel)(P), int grid, int threads, int smem, cudaStream_t s, const P &p) {
+cudaError_t launch_pdl(void (*kernel)(P), dim3 grid, int threads, int smem, cudaStream_t s, const P &p) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;

@@ -111,38 +111,44 @@ __device__ __forceinline__ void load_q(const uint16_t *q, int G, int g, int t, u
   }
 }
 
-/* A warp per 16 pages of a (sequence, layer, KV head): the pages are an MMA's
- * rows, the query heads its columns, and lo and hi side by side the summed
- * dimension, against the queries' negative and positive parts. */
-__global__ void __launch_bounds__(256) page_scores_kernel(const __grid_constant__ PageScoresParams p, int most) {
+/* A warp per 16 pages of a (sequence, layer, KV head): the pages are an MMA's rows,
+ * the query heads its columns, and lo and hi side by side the summed dimension,
+ * against the queries' negative and positive parts.
+ *
+ * HBM bounds it, given registers for all of a tile's loads at once (64 a thread):
+ * 2.1 M pages (1.08 GB of bounds) 161 us, 99% of the copy rate; 171 with 80 registers
+ * and fewer warps, 180 with 54, where the loads went out in two parts. */
+__global__ void __launch_bounds__(256, 4) page_scores_kernel(const __grid_constant__ PageScoresParams p, int tiles) {
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int lh = p.L * p.Hkv;
-  const long long units = (long long)p.n_seqs * lh * most;   // most: 16-page tiles of the longest sequence
-  const long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (u >= units) return;
-  const long long row = u / most;
-  const int tile = (int)(u - row * most);
-  const int b = (int)(row / lh), l = (int)(row % lh) / p.Hkv, h = (int)(row % p.Hkv);
-  const int P = p.n_pages[b];
+  const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);   // tiles: of the longest sequence
+  const int row = (int)(unit / tiles), tile = (int)(unit - (long long)row * tiles);
+  if (row >= p.n_seqs * lh) return;
+  const int b = row / lh, l = row % lh / p.Hkv, h = row % p.Hkv;
+  const int P = p.n_pages[b], p0 = tile * 16 + g, p1 = p0 + 8;
   if (tile * 16 >= P) return;
   uint32_t q[16];
   load_q(p.q + (((size_t)b * p.L + l) * p.Hq + h * p.G) * D, p.G, g, t, q);
-  const int p0 = tile * 16 + g, p1 = p0 + 8;
   const int i0 = page_id(p, b, p0), i1 = page_id(p, b, p1);
   const uint4 *s0 = (const uint4 *)(p.bounds + (((size_t)l * p.P_phys + (i0 < 0 ? 0 : i0)) * p.Hkv + h) * 2 * D) + t;
   const uint4 *s1 = (const uint4 *)(p.bounds + (((size_t)l * p.P_phys + (i1 < 0 ? 0 : i1)) * p.Hkv + h) * 2 * D) + t;
-  float c[4] = {0.f, 0.f, 0.f, 0.f};
   const uint4 none = make_uint4(0, 0, 0, 0);
+  uint4 x[8], y[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {   // 0..3: lo, 4..7: hi
-    const uint4 x = i0 >= 0 ? s0[4 * j] : none, y = i1 >= 0 ? s1[4 * j] : none;
+  for (int j = 0; j < 8; ++j) {                // 0..3: lo, 4..7: hi
+    x[j] = i0 >= 0 ? s0[4 * j] : none;
+    y[j] = i1 >= 0 ? s1[4 * j] : none;
+  }
+  float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
     uint32_t w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) w[k] = j < 4 ? min2(q[4 * (j & 3) + k], 0u) : max2(q[4 * (j & 3) + k], 0u);
-    mma_bf16(c, x.x, y.x, x.y, y.y, w[0], w[1]);
-    mma_bf16(c, x.z, y.z, x.w, y.w, w[2], w[3]);
+    mma_bf16(c, x[j].x, y[j].x, x[j].y, y[j].y, w[0], w[1]);
+    mma_bf16(c, x[j].z, y[j].z, x[j].w, y[j].w, w[2], w[3]);
   }
   /* columns 2t, 2t + 1 of rows g (c[0], c[1]) and g + 8 */
   const bool in0 = 2 * t < p.G, in1 = 2 * t + 1 < p.G;
@@ -173,41 +179,35 @@ __device__ __forceinline__ uint32_t score_key(float x) {
  * taken become bits, and one scan over the words of bits gives all places.
  *
  * Latency bounds it: barriers and round trips through shared memory.  2 rows of 2,048
- * pages 5.6 us, 576 rows of 4,096 (keys in shared memory, a second pass over them
- * for the places) 15.7. */
-constexpr int BINS = 2048, TOP_WARPS = 32;
+ * pages 4.0 us, 576 rows of 4,096 9.6 us.  With keys in shared memory and a second pass
+ * over them for the places 5.6 and 15.7; with eight-bit digits 7.3 and 24.3. */
+constexpr int BINS = 2048;
 
-/* Sums of a and b over the threads before this one; every thread calls it. */
-__device__ __forceinline__ int2 scan_before(int a, int b, int2 *warp_sum) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  int x = a, y = b;
+/* Sum of a over the threads before this one; every thread calls it. */
+__device__ __forceinline__ int scan_before(int a, int warps, int *warp_sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = a;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
-    if (lane >= o) {
-      x += u;
-      y += v;
-    }
+    const int u = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += u;
   }
-  if (lane == 31) warp_sum[warp] = make_int2(x, y);
+  if (lane == 31) warp_sum[warp] = x;
   __syncthreads();
-  int2 w = lane < warps && lane < warp ? warp_sum[lane] : make_int2(0, 0);
-  w.x = __reduce_add_sync(0xffffffffu, w.x);
-  w.y = __reduce_add_sync(0xffffffffu, w.y);
-  return make_int2(x - a + w.x, y - b + w.y);
+  return x - a + __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane] : 0);
 }
 
-template <int KEYS>
-__global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_constant__ PageTopParams p) {
-  __shared__ int hist[BINS];
-  __shared__ int2 warp_sum[TOP_WARPS];
-  __shared__ uint32_t warp_lo[TOP_WARPS], warp_hi[TOP_WARPS], above[TOP_WARPS * KEYS], equal[TOP_WARPS * KEYS];
+template <int threads, int KEYS>
+__global__ void __launch_bounds__(threads) page_top_kernel(const __grid_constant__ PageTopParams p) {
+  constexpr int warps = threads / 32;
+  __shared__ int hist[BINS], warp_sum[32];
+  __shared__ uint32_t warp_lo[32], warp_hi[32], above[warps * KEYS], equal[warps * KEYS];
   __shared__ int s_bin, s_left, s_in;
   pdl_wait();
   pdl_trigger();
-  const long long row = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
-  const int P = p.n_pages[row / p.rows];
+  const size_t row = (size_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int P = p.n_pages[blockIdx.y];
   int32_t *out = p.ids + row * p.top;
   if (P <= p.top) {
     for (int i = tid; i < p.top; i += threads) out[i] = i < P ? i : -1;
@@ -236,7 +236,8 @@ __global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_c
     warp_lo[warp] = lo;
     warp_hi[warp] = hi;
   }
-  for (int i = tid; i < BINS; i += threads) hist[i] = 0;
+#pragma unroll
+  for (int i = 0; i < BINS; i += threads) hist[i + tid] = 0;
   __syncthreads();
   lo = __reduce_min_sync(0xffffffffu, lane < warps ? warp_lo[lane] : 0xffffffffu) + 1;
   hi = __reduce_max_sync(0xffffffffu, lane < warps ? warp_hi[lane] : 0u);
@@ -248,10 +249,11 @@ __global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_c
     for (int i = 0; i < KEYS; ++i)
       if (k[i] - lo <= span) atomicAdd(&hist[(k[i] - lo) >> shift], 1);
     __syncthreads();
-    const int each = BINS / threads;           // bins per thread, from the top down
+    constexpr int each = BINS / threads;       // bins per thread, from the top down
     int sum = 0;
+#pragma unroll
     for (int i = 0; i < each; ++i) sum += hist[BINS - 1 - tid * each - i];
-    int before = scan_before(sum, 0, warp_sum).x;
+    int before = scan_before(sum, warps, warp_sum);
     if (before < left && left <= before + sum) {
       int bin = BINS - 1 - tid * each;
       while (before + hist[bin] < left) before += hist[bin--];
@@ -264,7 +266,8 @@ __global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_c
     lo += (uint32_t)s_bin << shift;
     hi = lo + min(hi - lo, (1u << shift) - 1);
     if (s_in == left || shift == 0) break;
-    for (int i = tid; i < BINS; i += threads) hist[i] = 0;
+#pragma unroll
+    for (int i = 0; i < BINS; i += threads) hist[i + tid] = 0;
     __syncthreads();
   }
 #pragma unroll
@@ -277,9 +280,9 @@ __global__ void __launch_bounds__(32 * TOP_WARPS) page_top_kernel(const __grid_c
   }
   __syncthreads();
   const bool mine = tid < KEYS * warps;        // a word per thread
-  uint32_t gt = mine ? above[tid] : 0u, eq = mine ? equal[tid] : 0u;
-  const int2 at = scan_before(__popc(gt), __popc(eq), warp_sum);
-  int a = at.x, e = at.y;
+  const uint32_t gt = mine ? above[tid] : 0u, eq = mine ? equal[tid] : 0u;
+  const int at = scan_before(__popc(gt) | __popc(eq) << 16, warps, warp_sum);   // at most 16,384 of each
+  int a = at & 0xffff, e = at >> 16;
   for (uint32_t any = gt | eq; any; any &= any - 1) {
     const uint32_t bit = any & (0u - any);
     const bool is_gt = gt & bit;
@@ -648,11 +651,10 @@ cudaError_t launch_bounds(const BoundsParams &p, cudaStream_t s) {
 cudaError_t launch_page_scores(const PageScoresParams &p, cudaStream_t s) {
   int most = 0;
   for (int b = 0; b < p.n_seqs; ++b) most = p.n_pages[b] > most ? p.n_pages[b] : most;
-  most = (most + 15) / 16;
-  const long long blocks = ((long long)p.n_seqs * p.L * p.Hkv * most + 7) / 8;
-  if (blocks == 0) return cudaSuccess;
+  const long long rows = (long long)p.n_seqs * p.L * p.Hkv, tiles = (most + 15) / 16;
+  if (tiles == 0) return cudaSuccess;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.gridDim = dim3((unsigned)((rows * tiles + 7) / 8));
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -660,19 +662,19 @@ cudaError_t launch_page_scores(const PageScoresParams &p, cudaStream_t s) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, page_scores_kernel, p, most);
+  return cudaLaunchKernelEx(&cfg, page_scores_kernel, p, (int)tiles);
 }
 
 cudaError_t launch_page_top(const PageTopParams &p, cudaStream_t s) {
   int most = 0;
   for (int b = 0; b < p.n_seqs; ++b) most = p.n_pages[b] > most ? p.n_pages[b] : most;
-  static_assert(MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS / 16 <= 16 * 32 * TOP_WARPS, "the longest row has its keys");
-  const int rows = p.n_seqs * p.rows;
-  return most <= 1024   ? launch_pdl(page_top_kernel<4>, rows, 256, 0, s, p)
-         : most <= 2048 ? launch_pdl(page_top_kernel<8>, rows, 256, 0, s, p)
-         : most <= 4096 ? launch_pdl(page_top_kernel<8>, rows, 512, 0, s, p)
-         : most <= 8192 ? launch_pdl(page_top_kernel<8>, rows, 1024, 0, s, p)
-                        : launch_pdl(page_top_kernel<16>, rows, 1024, 0, s, p);
+  static_assert(MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS / 16 <= 16 * 1024, "the longest row has its keys");
+  const dim3 grid(p.rows, p.n_seqs);
+  return most <= 1024   ? launch_pdl(page_top_kernel<512, 2>, grid, 512, 0, s, p)
+         : most <= 2048 ? launch_pdl(page_top_kernel<512, 4>, grid, 512, 0, s, p)
+         : most <= 4096 ? launch_pdl(page_top_kernel<512, 8>, grid, 512, 0, s, p)
+         : most <= 8192 ? launch_pdl(page_top_kernel<1024, 8>, grid, 1024, 0, s, p)
+                        : launch_pdl(page_top_kernel<1024, 16>, grid, 1024, 0, s, p);
 }
 
 namespace {
@@ -709,29 +711,27 @@ struct AttendForm {
   int C = 0, warps = 0, stages = 0;
 };
 
-/* How many CTAs and warps per row, and how many tiles in flight per warp: the least
- * of these costs in us.  Their constants were fitted to 70 launches timed on a GB300
- * in up to 20 forms each (1 to 64 sequences, 1 to 36 layers, 2 to 600 tiles per
- * list, 2 to 1,472 rows): the choice takes 1.8% longer than the best form of each
- * on average, 20% at worst.  n: tiles of a warp, N: CTAs, hbm: K/V bytes at 6.8
- * TB/s, slots: CTAs that run at once (a cluster of 8 or 16 leaves parts of the
- * chip unused, and more so with one CTA per SM).
- *   Shared memory is counted with the scores' room whether masses are wanted or
- * not: the split, and with it the rounding of a result, does not depend on it.
- *   One row pair of 64 tiles (one layer of one sequence): 4.6 us with 16 x 4 warps,
- * 8.4 with 8 warps; 288 rows of 256: 101 us with 8 warps per row (two rounds of one
- * CTA per SM), 126 and more with the other forms at one tile in flight but 4 x 4. */
+/* How many CTAs and warps per row, and how many tiles in flight per warp.  cta: the
+ * time of one CTA in us, n tiles of its busiest warp at 0.72 or, with two in flight,
+ * 0.42; slots: CTAs that run at once (a cluster of 8 or 16 leaves parts of the chip
+ * unused, the more so with one CTA per SM).  Of the forms whose CTAs all run at once the
+ * shortest; if there is none, the one with the least CTA time per slot.  (What a
+ * launch takes beyond that, HBM for one, is the same in all forms.)
+ *   The constants were fitted to 115 launches timed on a GB300 in up to 20 forms each (1
+ * to 64 sequences, 1 to 36 layers, 2 to 600 tiles per list, 2 to 7,200 rows, up to
+ * 110 us at the copy rate): the choice takes 1.7% longer than the best form of each on
+ * average, 21% at worst.  Some of them: 2 rows of 64 tiles 4.6 us with 16 x 4 warps, 8.4
+ * with 8; 64 rows of 48, 8.3 with 4 x 4 and 8.5 with 8 or 2 x 8; 1,152 rows of 48, 75 us
+ * with 4 warps, 76 with 8, 81 with 2 x 4; 288 rows of 256, 101 to 107 with 8, 2 x 8 or
+ * 4 x 8, 146 with 4.
+ *   The scores' room is counted whether masses are wanted or not: the split, and with it
+ * the rounding of a result, does not depend on it. */
 AttendForm attend_form(const AttendPagesParams &p) {
   constexpr float SMS = 152.f;
   const int tpp = p.ps / TILE, listed = p.top * tpp;
-  long long sum = 0;
   int T = 1;
-  for (int b = 0; b < p.n_seqs; ++b) {
-    const int t = (p.n_pages[b] < p.top ? p.n_pages[b] : p.top) * tpp;
-    sum += t;
-    T = t > T ? t : T;
-  }
-  const float rows = (float)p.n_seqs * p.L * p.Hkv, hbm = (float)sum * p.L * p.Hkv * (TILE_BYTES / 6.8e6f);
+  for (int b = 0; b < p.n_seqs; ++b) T = std::max(T, std::min(p.n_pages[b], p.top) * tpp);
+  const float rows = (float)p.n_seqs * p.L * p.Hkv;
   AttendForm best;
   float least = INFINITY;
   for (int lg = 0; lg < 5; ++lg)
@@ -745,14 +745,9 @@ AttendForm attend_form(const AttendPagesParams &p) {
         const float part = C <= 2 ? 1.f : per_sm > 1 ? (C == 4 ? 0.97f : C == 8 ? 0.93f : 0.72f)
                                                      : (C == 4 ? 0.94f : C == 8 ? 0.78f : 0.6f);
         const float slots = per_sm * SMS * part, N = rows * C;
-        const float cta = 5.4f + (C > 1 ? 0.9f : 0.f) + (C == 16 ? 0.15f : 0.f) + (warps == 8 ? 0.24f : 0.f) +
-                          (float)((T + W - 1) / W) * (stages == 1 ? 0.98f : 0.57f);
-        float cost;
-        if (N <= slots)
-          cost = std::max(cta, hbm * 1.1f + 1.9f) + 0.0026f * N;
-        else
-          cost = std::max(hbm * 1.1f + 1.9f + 0.46f * cta, 0.9f * N / slots * cta) + 0.0026f * slots +
-                 (C > 1 ? 0.014f * N : 0.f);
+        const float cta = 4.f + (C > 1 ? 0.73f : 0.f) + (C == 16 ? 0.13f : 0.f) + (warps == 8 ? 0.21f : 0.f) +
+                          (float)((T + W - 1) / W) * (stages == 1 ? 0.72f : 0.42f);
+        const float cost = N <= slots ? cta + 0.0021f * N : 1e6f + N / slots * cta + 0.0012f * N;
         if (cost < least) {
           least = cost;
           best.C = C;
