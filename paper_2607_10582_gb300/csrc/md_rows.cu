@@ -75,11 +75,6 @@ __device__ __forceinline__ uint32_t pack2(f32x2 x) {
   return pack_bf16(f.x, f.y);
 }
 
-/* What a row's lane multiplies its elements with.  With n the norm's factor, w the
- * weights (1 where there is none) and (c, s) the pair's table entry:
- *   out_a = n (x_a (w_a c) + x_b (-w_b s)),  out_b = n (x_b (w_b c) + x_a (w_a s));
- * the four products are made once per token. */
-
 /* 8 consecutive elements in registers, as they came */
 template <class T>
 struct Eight {
@@ -123,11 +118,17 @@ __global__ void __launch_bounds__(32 * WARPS, 20 / WARPS) norm_rope_kernel(const
     const int q = lane + 32 * i;
     pos[i] = q < pairs ? p.positions[(long long)(p.axes[i] >> 2 * lane & 3) * p.n_tokens + tok] : -1;
   }
+  /* most rows are query rows, a step apart; key and value rows are looked up */
+  const T *q_src = (const T *)p.set[0].in + tok * p.set[0].in_token + row * p.set[0].in_head;
+  uint16_t *q_dst = p.set[0].out + tok * p.set[0].out_token + row * p.set[0].out_head;
+  const long long src_step = step * p.set[0].in_head, dst_step = step * p.set[0].out_head;
   auto fetch = [&](Row &x, int at) {
     if (at >= h2) return;
-    const T *src = at < h0   ? (const T *)p.set[0].in + tok * p.set[0].in_token + at * p.set[0].in_head
-                   : at < h1 ? (const T *)p.set[1].in + tok * p.set[1].in_token + (at - h0) * p.set[1].in_head
-                             : (const T *)p.set[2].in + tok * p.set[2].in_token + (at - h1) * p.set[2].in_head;
+    const T *src = q_src;
+    q_src += src_step;
+    if (at >= h0)
+      src = at < h1 ? (const T *)p.set[1].in + tok * p.set[1].in_token + (at - h0) * p.set[1].in_head
+                    : (const T *)p.set[2].in + tok * p.set[2].in_token + (at - h1) * p.set[2].in_head;
     x.u.load(src + e0);
     x.v.load(src + e1);
   };
@@ -141,50 +142,37 @@ __global__ void __launch_bounds__(32 * WARPS, 20 / WARPS) norm_rope_kernel(const
           pos[i] >= 0 && pos[i] < p.table_len ? p.table[(size_t)pos[i] * pairs + q] : make_float2(NAN, NAN);
   }
   __syncwarp();
-  /* the factors of run u, and of run v, with their own and with the other channel */
-  f32x2 uu[4], uv[4], vv[4], vu[4];
-  auto factors = [&](const float *w) {
+  /* (cos, sin) as the channels of runs u and v want them: INTER, word i: a pair's
+   * cos twice, its -sin and sin; else the cosines and the sines of pairs 2i, 2i + 1 */
+  f32x2 cu[4], su[4], cv[4], sv[4], wu[4], wv[4];
+  if (rot) {
     const float4 *e = cs + j;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float4 wu = make_float4(1.f, 1.f, 1.f, 1.f), wv = wu;
-      if (w) {
-        wu = *(const float4 *)(w + e0 + 4 * h);
-        wv = *(const float4 *)(w + e1 + 4 * h);
-      }
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int i = 2 * h + n;
-        const float2 a = n ? make_float2(wu.z, wu.w) : make_float2(wu.x, wu.y);
-        const float2 b = n ? make_float2(wv.z, wv.w) : make_float2(wv.x, wv.y);
-        uu[i] = pair(a.x, a.y);
-        vv[i] = pair(b.x, b.y);
-        if (!rot) continue;
-        if (INTER) {                                     // word i of run u is pair i, of run v pair i + 4
-          const float4 c = e[(i / 2) * 8], d = e[(i / 2 + 2) * 8];
-          const float2 x = i & 1 ? make_float2(c.z, c.w) : make_float2(c.x, c.y);
-          const float2 y = i & 1 ? make_float2(d.z, d.w) : make_float2(d.x, d.y);
-          uu[i] = pair(a.x * x.x, a.y * x.x);
-          uv[i] = pair(-a.y * x.y, a.x * x.y);
-          vv[i] = pair(b.x * y.x, b.y * y.x);
-          vu[i] = pair(-b.y * y.y, b.x * y.y);
-        } else {                                         // pairs 2i, 2i + 1
-          const float4 c = e[i * 8];
-          uu[i] = pair(a.x * c.x, a.y * c.z);
-          uv[i] = pair(-b.x * c.y, -b.y * c.w);
-          vv[i] = pair(b.x * c.x, b.y * c.z);
-          vu[i] = pair(a.x * c.y, a.y * c.w);
-        }
+    for (int i = 0; i < 4; ++i) {
+      if (INTER) {                                       // word i of run u is pair i, of run v pair i + 4
+        const float4 c = e[(i / 2) * 8], d = e[(i / 2 + 2) * 8];
+        const float2 x = i & 1 ? make_float2(c.z, c.w) : make_float2(c.x, c.y);
+        const float2 y = i & 1 ? make_float2(d.z, d.w) : make_float2(d.x, d.y);
+        cu[i] = pair(x.x, x.x);
+        su[i] = pair(-x.y, x.y);
+        cv[i] = pair(y.x, y.x);
+        sv[i] = pair(-y.y, y.y);
+      } else {
+        const float4 c = e[i * 8];
+        cu[i] = cv[i] = pair(c.x, c.z);
+        sv[i] = pair(c.y, c.w);
+        su[i] = pair(-c.y, -c.w);
       }
     }
-  };
-  const float *have = (const float *)1;                  // whose factors are at hand: no weights' yet
+  }
+  const float *have = nullptr;                           // whose weights are at hand
 #pragma unroll 1
   for (; row < h2; row += step, now = next) {
     fetch(next, row + step);
     uint4 u, v;
     uint32_t *ou = &u.x, *ov = &v.x;
-    uint16_t *dst;
+    uint16_t *dst = q_dst;
+    q_dst += dst_step;
     if (row >= h1) {                                     // a value row
       dst = p.set[2].out + tok * p.set[2].out_token + (row - h1) * p.set[2].out_head;
 #pragma unroll
@@ -193,19 +181,29 @@ __global__ void __launch_bounds__(32 * WARPS, 20 / WARPS) norm_rope_kernel(const
         ov[i] = pack2(now.v.two(i));
       }
     } else {
-      const bool is_q = row < h0;
-      dst = is_q ? p.set[0].out + tok * p.set[0].out_token + row * p.set[0].out_head
-                 : p.set[1].out + tok * p.set[1].out_token + (row - h0) * p.set[1].out_head;
-      const float *w = is_q ? p.set[0].weight : p.set[1].weight;
-      if (have != w) factors(w);
-      have = w;
-      f32x2 x[4], y[4], f = pair(1.f, 1.f);
+      const float *w = p.set[0].weight;
+      if (row >= h0) {
+        dst = p.set[1].out + tok * p.set[1].out_token + (row - h0) * p.set[1].out_head;
+        w = p.set[1].weight;
+      }
+      f32x2 x[4], y[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         x[i] = now.u.two(i);
         y[i] = now.v.two(i);
       }
       if (w) {
+        if (have != w) {
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const float4 a = *(const float4 *)(w + e0 + 2 * i), b = *(const float4 *)(w + e1 + 2 * i);
+            wu[i] = pair(a.x, a.y);
+            wu[i + 1] = pair(a.z, a.w);
+            wv[i] = pair(b.x, b.y);
+            wv[i + 1] = pair(b.z, b.w);
+          }
+          have = w;
+        }
         f32x2 s2 = mul2(x[0], x[0]), t2 = mul2(y[0], y[0]);
 #pragma unroll
         for (int i = 1; i < 4; ++i) {
@@ -217,18 +215,23 @@ __global__ void __launch_bounds__(32 * WARPS, 20 / WARPS) norm_rope_kernel(const
 #pragma unroll
         for (int o = 4; o; o >>= 1) sum += __shfl_xor_sync(lanes, sum, o);
         const float n = rsqrtf(sum * (1.f / D) + p.eps);
-        f = pair(n, n);
+        const f32x2 f = pair(n, n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = mul2(mul2(x[i], f), wu[i]);
+          y[i] = mul2(mul2(y[i], f), wv[i]);
+        }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        f32x2 m = mul2(x[i], uu[i]), n = mul2(y[i], vv[i]);
+        f32x2 m = x[i], n = y[i];
         if (rot) {
           const float2 g = parts(x[i]), h = parts(y[i]);
-          m = fma2(INTER ? pair(g.y, g.x) : y[i], uv[i], m);
-          n = fma2(INTER ? pair(h.y, h.x) : x[i], vu[i], n);
+          m = fma2(INTER ? pair(g.y, g.x) : y[i], su[i], mul2(x[i], cu[i]));
+          n = fma2(INTER ? pair(h.y, h.x) : x[i], sv[i], mul2(y[i], cv[i]));
         }
-        ou[i] = pack2(mul2(m, f));
-        ov[i] = pack2(mul2(n, f));
+        ou[i] = pack2(m);
+        ov[i] = pack2(n);
       }
     }
     *(uint4 *)(dst + e0) = u;
