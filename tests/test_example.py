@@ -15,5 +15,5 @@ def test_sparse_decode_example(capsys):
     spec = importlib.util.spec_from_file_location("sparse_decode", os.path.join(ROOT, "examples", "sparse_decode.py"))
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
-    r = m.main(["--tokens", "2500", "--steps", "4", "--top", "8", "--layers", "2"])
+    r = m.main(["--agents", "3", "--tokens", "2500", "--steps", "4", "--top", "8", "--layers", "2"])
     assert set(r) == {0, 8} and "nan" not in capsys.readouterr().out
