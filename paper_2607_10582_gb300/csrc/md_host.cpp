@@ -79,7 +79,7 @@ struct md_ctx {
   struct {                   // md_sparse_enable
     int top = 0, first = 0, last = 0;   // top 0: off
     uint8_t *buf = nullptr;
-    std::vector<int> bounded;           // leading pages of each sequence whose bounds are made
+    int bounded[MD_MAX_BATCH] = {0};    // leading pages of each sequence whose bounds are made
   } sparse;
   int device = 0;
   int pageable_access = 0;   // the device reads and writes pageable host memory coherently
@@ -916,6 +916,7 @@ md_status run_sparse(md_ctx *c, int batch, int l0, int L, const void *q_dev, voi
   if (e == cudaSuccess) {
     PageScoresParams sp;
     (PageSet &)sp = set;
+    for (int b = 0; b < batch; ++b) sp.n_pages[b] -= 1;   // the page being written needs no score
     sp.q = (const uint16_t *)q_dev;
     sp.bounds = bounds;
     sp.scores = (float *)(c->sparse.buf + sl.scores);
@@ -1417,7 +1418,7 @@ MD_API md_status md_set_state(md_ctx *c, int what, const void *src, size_t bytes
   size_t off, n;
   state_array(c, what, &off, &n);
   if (bytes != n) return fail(c, MD_ERR_INVALID_ARG, "state array is %zu bytes, not %zu", n, bytes);
-  if (what == MD_STATE_BLOCK_TABLE || what == MD_STATE_PAGE_FILL) c->sparse.bounded.assign(c->sparse.bounded.size(), 0);
+  if (what == MD_STATE_BLOCK_TABLE || what == MD_STATE_PAGE_FILL) std::fill(c->sparse.bounded, c->sparse.bounded + MD_MAX_BATCH, 0);
   cudaError_t e = cudaMemcpyAsync(c->ws + off, src, n, cudaMemcpyDeviceToDevice, c->stream);
   return e == cudaSuccess ? MD_OK : cuda_fail(c, e, "state copy");
 }
@@ -1536,7 +1537,7 @@ MD_API md_status md_load_state(md_ctx *c, const void *src_dev, const void *host_
   memcpy(c->tokens_exact.data(), h, B);
   h += B;
   c->calib_on = *h != 0;
-  c->sparse.bounded.assign(c->sparse.bounded.size(), 0);
+  std::fill(c->sparse.bounded, c->sparse.bounded + MD_MAX_BATCH, 0);
   /* a checkpoint holds no pending step mass; clear whatever the live state
    * had accumulated, or the next step would add to it */
   cudaError_t e = cudaMemsetAsync(c->ws + c->lay.mass_acc, 0, c->lay.slots * 8, c->stream);
@@ -1567,7 +1568,7 @@ MD_API md_status md_sparse_enable(md_ctx *c, int top, int first, int last, void 
   c->sparse.first = first;
   c->sparse.last = last;
   c->sparse.buf = (uint8_t *)buf;
-  c->sparse.bounded.assign(c->cfg.max_batch, 0);
+  std::fill(c->sparse.bounded, c->sparse.bounded + MD_MAX_BATCH, 0);
   return MD_OK;
 }
 

@@ -348,6 +348,8 @@ MD_API md_status md_norm_rope(const md_norm_rope_args *args) {
       a.type < MD_TYPE_BF16 || a.type > MD_TYPE_F32 || a.rotary_dim < 0 || a.rotary_dim > D || a.rotary_dim % 8 ||
       !(a.eps >= 0.f))
     return MD_ERR_INVALID_ARG;
+  const int values = a.v ? a.num_kv_heads : 0, rows = a.num_q_heads + a.num_kv_heads + values;
+  if (a.n_tokens == 0 || rows == 0) return MD_OK;
   const size_t in = a.type == MD_TYPE_F32 ? 16 : 8;
   if (a.num_q_heads > 0 && (!rows_ok(a.q, a.q_token, a.q_head, in) || !rows_ok(a.q_out, a.q_out_token, a.q_out_head, 8)))
     return MD_ERR_INVALID_ARG;
@@ -368,8 +370,6 @@ MD_API md_status md_norm_rope(const md_norm_rope_args *args) {
       p.axes[i / 32] |= (unsigned long long)a.axis_host[i] << 2 * (i & 31);
     }
   }
-  const int values = a.v ? a.num_kv_heads : 0, rows = a.num_q_heads + a.num_kv_heads + values;
-  if (a.n_tokens == 0 || rows == 0) return MD_OK;
   p.set[0] = {a.q, (uint16_t *)a.q_out, a.q_weight, a.q_token, a.q_head, a.q_out_token, a.q_out_head, a.num_q_heads, 1};
   p.set[1] = {a.k, (uint16_t *)a.k_out, a.k_weight, a.k_token, a.k_head, a.k_out_token, a.k_out_head, a.num_kv_heads, 1};
   p.set[2] = {a.v, (uint16_t *)a.v_out, nullptr, a.v_token, a.v_head, a.v_out_token, a.v_out_head, values, 0};

@@ -142,6 +142,44 @@ def test_infinities_and_positions_outside_the_table():
 
 
 @gpu
+def test_no_tokens_and_no_rotation():
+    _need_gpu()
+    x, y = (torch.ones((0, 4, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = md.md_rope_table(_freq(64), 8)
+    md.md_norm_rope(x, None, None, y, None, None, positions=torch.zeros(0, dtype=torch.int32, device="cuda"), table=table)
+    x = torch.randn((6, 4, D), device="cuda")
+    y = torch.empty((6, 4, D), dtype=torch.bfloat16, device="cuda")
+    md.md_norm_rope(x, None, None, y, None, None, positions=None, table=None)        # a rounding copy
+    assert torch.equal(y, x.bfloat16())
+
+
+@gpu
+def test_unaligned_rows():
+    """Rows at 8-byte addresses and odd multiples of 4 elements apart, and rotary_dim = 8 mod 16,
+    take another kernel: the same values."""
+    _need_gpu()
+    T, H = 37, 5
+    g = torch.Generator(device="cuda").manual_seed(8)
+    big = torch.randn((T, H * 132 + 4), generator=g, device="cuda").bfloat16()
+    off = big[:, 4:].view(T, H * 132)[:, :H * 132].unflatten(1, (H, 132))[..., :D]    # head stride 132, base + 8 bytes
+    even = off.contiguous()
+    table, w = md.md_rope_table(_freq(64), 99), 1 + 0.1 * torch.randn(D, generator=g, device="cuda")
+    pos = torch.randint(0, 99, (2, T), generator=g, device="cuda", dtype=torch.int32)
+    axes = np.arange(64, dtype=np.uint8) % 2
+    for inter in (False, True):
+        for weight in (None, w):
+            a, b = (torch.empty((T, H, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            md.md_norm_rope(off, None, None, a, None, None, positions=pos, table=table, q_weight=weight, axes=axes,
+                            interleaved=inter)
+            md.md_norm_rope(even, None, None, b, None, None, positions=pos, table=table, q_weight=weight, axes=axes,
+                            interleaved=inter)
+            for y in (a, b):
+                ref, size = _ref(even.double().cpu().numpy(), None if weight is None else w.double().cpu().numpy(), 1e-6,
+                                 pos.cpu().numpy(), _freq(64), axes, inter)
+                _check(y, ref, size)
+
+
+@gpu
 def test_calls_without_the_c_module_are_the_same(monkeypatch):
     """Where Python's headers are missing every call goes through ctypes."""
     _need_gpu()

@@ -238,6 +238,28 @@ def test_region_aligned_pages(ps):
 
 
 @gpu
+def test_wait_limit_shorter_than_a_copy():
+    """A copy that does not land within the handle's limit ends the step with a status, and what
+    was in flight lands before the launch ends: a new handle works."""
+    s = Loop(2, 16, 2, 32, [3000, 500], seed=10)
+    s.c.sparse_enable(40)
+    s.c.debug_set(md.MD_DEBUG_SPIN_LIMIT_NS, 1000)
+    statuses = set()
+    for _ in range(30):
+        s.step()
+        statuses.add(s.c.sync())
+        if md.MD_ERR_DEVICE_TIMEOUT in statuses:
+            break
+    assert statuses <= {md.MD_OK, md.MD_ERR_DEVICE_TIMEOUT}
+    if md.MD_ERR_DEVICE_TIMEOUT in statuses:
+        with pytest.raises(md.MemDecayError):
+            s.step()
+    t = Loop(2, 16, 2, 32, [3000, 500], seed=10)
+    t.c.sparse_enable(40)
+    t.check("step", 40)
+
+
+@gpu
 def test_refusals_leave_the_handle_as_it_was():
     s = Loop(2, 16, 2, 16, [400], seed=9)
     for top, first, last in ((-1, 1, 1), (5000, 1, 1), (4, 1, 0), (4, -1, 1), (4, 3, 2), (4, 5, 1)):
