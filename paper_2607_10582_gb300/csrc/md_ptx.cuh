@@ -109,11 +109,16 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
       : "memory");
 }
 
-/* ---- cp.async: 16 bytes global -> shared, past L1 ---- */
+/* ---- cp.async: 16 bytes global -> shared ---- */
 /* A thread's copies are visible to itself after its own wait; no barrier is
- * needed where each thread reads only what it copied. */
+ * needed where each thread reads only what it copied.  HALVES: the other half of a
+ * 32-byte sector comes by another copy, so the sector is kept in L1; else past it. */
+template <bool HALVES>
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"((uint64_t)src) : "memory");
+  if (HALVES)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst), "l"((uint64_t)src) : "memory");
+  else
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"((uint64_t)src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>   // all but the last N groups are complete

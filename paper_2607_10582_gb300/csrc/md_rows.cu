@@ -75,172 +75,212 @@ __device__ __forceinline__ uint32_t pack2(f32x2 x) {
   return pack_bf16(f.x, f.y);
 }
 
-/* 8 consecutive elements in registers, as they came */
-template <class T>
-struct Eight {
-  uint4 q[sizeof(T) / 2];
-  __device__ __forceinline__ void load(const T *p) {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = ((const uint4 *)p)[i];
-  }
-  __device__ __forceinline__ f32x2 two(int i) const { return load2((const T *)q + 2 * i); }
-};
-
-/* A unit of eight lanes per row, 16 elements per lane, two runs of eight that hold both
- * channels of eight pairs: 8j .. and R/2 + 8j .. for the pairs (i, i + R/2), 16j ..
- * for (2i, 2i + 1) (INTER); lanes past the rotated channels hold the rest.  A warp's
- * four units take neighbouring rows of one token, every 2^split-th row each, and load
- * the next row before they compute the one at hand. */
-constexpr int WARPS = 2;
+/* Eight lanes per row, 16 elements per lane in two runs of eight, such that a lane holds
+ * both channels of its pairs: channels 8j .. and R/2 + 8j .. for the pairs
+ * (i, i + R/2), 8j .. and 64 + 8j .. for (2i, 2i + 1) (INTER).  A warp takes four
+ * neighbouring rows of a token at a time, of every 2^split, then its next token.
+ *
+ * HBM bounds it where there are many tokens, as long as enough is in flight and little
+ * is computed per row.  A lane copies its 16-byte pieces of the rows ahead into slots of
+ * its own in shared memory, DEPTH rows deep: no registers, no barriers.  The warp fetches
+ * the table entries of its next token together while it computes this one, and the
+ * positions of the one after it.  Two fp32 operations go in one instruction.
+ *   30,000 tokens of 20 rows (323 MB) 55.6 us, 5.8 TB/s, 86% of the copy rate; 8,191
+ * tokens 19.2; one token of 16 rows 1.8.  Steps: loads into registers a row ahead 69.9
+ * and 21.7; the lanes fetching their own table entries 85; the axes in an indexed array
+ * of the launch parameters 72; 16 lanes per row with one operation per instruction 78. */
+constexpr int WARPS = 4, DEPTH = 3;
 
 template <class T, bool INTER>
-__global__ void __launch_bounds__(32 * WARPS, 20 / WARPS) norm_rope_kernel(const __grid_constant__ RowsParams p) {
-  struct Row {
-    Eight<T> u, v;
-  };
+__global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) norm_rope_kernel(const __grid_constant__ RowsParams p) {
+  constexpr int PIECES = sizeof(T);                      // 16-byte pieces of a lane's 16 elements
+  __shared__ uint4 rows_ahead[WARPS][DEPTH][PIECES][32];
   __shared__ float4 entries[WARPS][32];                  // [4][8 lanes] the entries of two pairs
   const int lane = threadIdx.x & 31, j = lane & 7;
   float4 *cs = entries[threadIdx.x >> 5];
+  uint4 *ring = &rows_ahead[threadIdx.x >> 5][0][0][lane];   // this lane's slots: piece i of slot s at (s PIECES + i) 32
   const unsigned lanes = 0xffu << (lane & 24);
   const int R = p.rotary_dim, pairs = R / 2, split = p.split_log, step = 1 << split;   // split >= 2
-  const bool rot = 16 * j < R;
-  const int e0 = INTER || !rot ? 16 * j : 8 * j, e1 = INTER || !rot ? e0 + 8 : R / 2 + 8 * j;
-  const long long unit = ((long long)blockIdx.x * 32 * WARPS + threadIdx.x) >> 3;
-  const long long tok = unit >> split;
-  if (tok >= p.n_tokens) return;                         // the whole warp
-  int row = (int)unit & (step - 1);                      // of the token's q, k and v rows, in this order
+  /* this lane's runs; lanes past R / 16 of the pairs (i, i + R / 2) hold what is not rotated */
+  const int past = j - R / 16;
+  const int e0 = INTER || past < 0 ? 8 * j : R + 8 * past;
+  const int e1 = INTER ? D / 2 + 8 * j : past < 0 ? R / 2 + 8 * j : R + (D - R) / 2 + 8 * past;
+  const bool rot_u = INTER ? e0 < R : past < 0, rot_v = INTER ? e1 < R : past < 0;
+  /* items: a token's warps, 2^(split - 2) of them */
+  const long long items = p.n_tokens << (split - 2), stride = (long long)gridDim.x * WARPS;
+  long long item = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
+  if (item >= items) return;
+  const int first = (int)((unsigned)item << 2 & (step - 1)) + (lane >> 3);   // of the token's q, k and v rows, in this order
   const int h0 = p.set[0].heads, h1 = h0 + p.set[1].heads, h2 = h1 + p.set[2].heads;
   pdl_wait();
   pdl_trigger();
-  int pos[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int q = lane + 32 * i;
-    pos[i] = q < pairs ? p.positions[(long long)(p.axes[i] >> 2 * lane & 3) * p.n_tokens + tok] : -1;
-  }
-  /* most rows are query rows, a step apart; key and value rows are looked up */
-  const T *q_src = (const T *)p.set[0].in + tok * p.set[0].in_token + row * p.set[0].in_head;
-  uint16_t *q_dst = p.set[0].out + tok * p.set[0].out_token + row * p.set[0].out_head;
-  const long long src_step = step * p.set[0].in_head, dst_step = step * p.set[0].out_head;
-  auto fetch = [&](Row &x, int at) {
-    if (at >= h2) return;
-    const T *src = q_src;
-    q_src += src_step;
-    if (at >= h0)
-      src = at < h1 ? (const T *)p.set[1].in + tok * p.set[1].in_token + (at - h0) * p.set[1].in_head
-                    : (const T *)p.set[2].in + tok * p.set[2].in_token + (at - h1) * p.set[2].in_head;
-    x.u.load(src + e0);
-    x.v.load(src + e1);
+  auto position = [&](long long it, int i) {             // of pair lane + 32 i
+    return it < items && lane + 32 * i < pairs
+               ? p.positions[(long long)(p.axes[i] >> 2 * lane & 3) * p.n_tokens + (it >> (split - 2))]
+               : -1;
   };
-  Row now, next;
-  fetch(now, row);
+  auto entry = [&](int pos, int i) {
+    return pos >= 0 && pos < p.table_len && lane + 32 * i < pairs ? p.table[(size_t)pos * pairs + lane + 32 * i]
+                                                                  : make_float2(NAN, NAN);
+  };
+  int pos0 = position(item, 0), pos1 = position(item, 1);
+  const T *q_src;
+  const long long src_step = step * p.set[0].in_head, dst_step = step * p.set[0].out_head;
+  auto rows_of = [&](long long tok) { q_src = (const T *)p.set[0].in + tok * p.set[0].in_token + first * p.set[0].in_head; };
+  /* the rows ahead; most are query rows, a step apart, key and value rows are looked up */
+  long long f_item = item;
+  int f_row = first;
+  rows_of(item >> (split - 2));
+  auto fetch = [&](int slot) {
+    if (f_row < h2 && f_item < items) {
+      const T *src = q_src;
+      q_src += src_step;
+      if (f_row >= h0) {
+        const long long tok = f_item >> (split - 2);
+        src = f_row < h1 ? (const T *)p.set[1].in + tok * p.set[1].in_token + (f_row - h0) * p.set[1].in_head
+                         : (const T *)p.set[2].in + tok * p.set[2].in_token + (f_row - h1) * p.set[2].in_head;
+      }
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int q = lane + 32 * i;
-    if (q < pairs)
-      ((float2 *)cs)[((q & 7) / 2 * 8 + q / 8) * 2 + (q & 1)] =
-          pos[i] >= 0 && pos[i] < p.table_len ? p.table[(size_t)pos[i] * pairs + q] : make_float2(NAN, NAN);
-  }
-  __syncwarp();
-  /* (cos, sin) as the channels of runs u and v want them: INTER, word i: a pair's
-   * cos twice, its -sin and sin; else the cosines and the sines of pairs 2i, 2i + 1 */
-  f32x2 cu[4], su[4], cv[4], sv[4], wu[4], wv[4];
-  if (rot) {
-    const float4 *e = cs + j;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (INTER) {                                       // word i of run u is pair i, of run v pair i + 4
-        const float4 c = e[(i / 2) * 8], d = e[(i / 2 + 2) * 8];
-        const float2 x = i & 1 ? make_float2(c.z, c.w) : make_float2(c.x, c.y);
-        const float2 y = i & 1 ? make_float2(d.z, d.w) : make_float2(d.x, d.y);
-        cu[i] = pair(x.x, x.x);
-        su[i] = pair(-x.y, x.y);
-        cv[i] = pair(y.x, y.x);
-        sv[i] = pair(-y.y, y.y);
-      } else {
-        const float4 c = e[i * 8];
-        cu[i] = cv[i] = pair(c.x, c.z);
-        sv[i] = pair(c.y, c.w);
-        su[i] = pair(-c.y, -c.w);
+      for (int i = 0; i < PIECES / 2; ++i) {
+        cp_async16<PIECES == 4>(smem_u32(ring + (slot * PIECES + i) * 32), (const uint4 *)(src + e0) + i);
+        cp_async16<PIECES == 4>(smem_u32(ring + (slot * PIECES + PIECES / 2 + i) * 32), (const uint4 *)(src + e1) + i);
+      }
+      f_row += step;
+      if (f_row >= h2) {
+        f_row = first;
+        f_item += stride;
+        rows_of(f_item >> (split - 2));
       }
     }
-  }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < DEPTH; ++i) fetch(i);
+  int slot = 0;
+  float2 t0 = entry(pos0, 0), t1 = entry(pos1, 1);
+  pos0 = position(item + stride, 0);
+  pos1 = position(item + stride, 1);
+  f32x2 cu[4], su[4], cv[4], sv[4], wu[4], wv[4];
   const float *have = nullptr;                           // whose weights are at hand
 #pragma unroll 1
-  for (; row < h2; row += step, now = next) {
-    fetch(next, row + step);
-    uint4 u, v;
-    uint32_t *ou = &u.x, *ov = &v.x;
-    uint16_t *dst = q_dst;
-    q_dst += dst_step;
-    if (row >= h1) {                                     // a value row
-      dst = p.set[2].out + tok * p.set[2].out_token + (row - h1) * p.set[2].out_head;
+  for (; item < items; item += stride) {
+    const long long tok = item >> (split - 2);
+    __syncwarp();                                        // the entries before have been read
+    auto put = [&](int q, float2 e) {                    // where lane j finds its eight pairs
+      const int at = INTER ? (q / 32 * 2 + (q & 3) / 2) * 8 + (q & 31) / 4 : (q & 7) / 2 * 8 + q / 8;
+      ((float2 *)cs)[at * 2 + (q & 1)] = e;
+    };
+    put(lane, t0);
+    put(lane + 32, t1);
+    __syncwarp();
+    t0 = entry(pos0, 0);                                 // of the next token, and positions of the one after it
+    t1 = entry(pos1, 1);
+    pos0 = position(item + 2 * stride, 0);
+    pos1 = position(item + 2 * stride, 1);
+    /* (cos, sin) as the channels of runs u and v want them: INTER, word i: a pair's
+     * cos twice, its -sin and sin; else the cosines and the sines of pairs 2i, 2i + 1 */
+    if (rot_u) {                                           // rot_v: only with rot_u
+      const float4 *e = cs + j;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        ou[i] = pack2(now.u.two(i));
-        ov[i] = pack2(now.v.two(i));
-      }
-    } else {
-      const float *w = p.set[0].weight;
-      if (row >= h0) {
-        dst = p.set[1].out + tok * p.set[1].out_token + (row - h0) * p.set[1].out_head;
-        w = p.set[1].weight;
-      }
-      f32x2 x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[i] = now.u.two(i);
-        y[i] = now.v.two(i);
-      }
-      if (w) {
-        if (have != w) {
-#pragma unroll
-          for (int i = 0; i < 4; i += 2) {
-            const float4 a = *(const float4 *)(w + e0 + 2 * i), b = *(const float4 *)(w + e1 + 2 * i);
-            wu[i] = pair(a.x, a.y);
-            wu[i + 1] = pair(a.z, a.w);
-            wv[i] = pair(b.x, b.y);
-            wv[i + 1] = pair(b.z, b.w);
-          }
-          have = w;
+        if (INTER) {                                       // word i of a run is a pair
+          const float4 c = e[(i / 2) * 8], d = e[(i / 2 + 2) * 8];
+          const float2 x = i & 1 ? make_float2(c.z, c.w) : make_float2(c.x, c.y);
+          const float2 y = i & 1 ? make_float2(d.z, d.w) : make_float2(d.x, d.y);
+          cu[i] = pair(x.x, x.x);
+          su[i] = pair(-x.y, x.y);
+          cv[i] = pair(y.x, y.x);
+          sv[i] = pair(-y.y, y.y);
+        } else {
+          const float4 c = e[i * 8];
+          cu[i] = cv[i] = pair(c.x, c.z);
+          sv[i] = pair(c.y, c.w);
+          su[i] = pair(-c.y, -c.w);
         }
-        f32x2 s2 = mul2(x[0], x[0]), t2 = mul2(y[0], y[0]);
-#pragma unroll
-        for (int i = 1; i < 4; ++i) {
-          s2 = fma2(x[i], x[i], s2);
-          t2 = fma2(y[i], y[i], t2);
-        }
-        const float2 s = parts(s2), t = parts(t2);
-        float sum = (s.x + s.y) + (t.x + t.y);
-#pragma unroll
-        for (int o = 4; o; o >>= 1) sum += __shfl_xor_sync(lanes, sum, o);
-        const float n = rsqrtf(sum * (1.f / D) + p.eps);
-        const f32x2 f = pair(n, n);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[i] = mul2(mul2(x[i], f), wu[i]);
-          y[i] = mul2(mul2(y[i], f), wv[i]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f32x2 m = x[i], n = y[i];
-        if (rot) {
-          const float2 g = parts(x[i]), h = parts(y[i]);
-          m = fma2(INTER ? pair(g.y, g.x) : y[i], su[i], mul2(x[i], cu[i]));
-          n = fma2(INTER ? pair(h.y, h.x) : x[i], sv[i], mul2(y[i], cv[i]));
-        }
-        ou[i] = pack2(m);
-        ov[i] = pack2(n);
       }
     }
-    *(uint4 *)(dst + e0) = u;
-    *(uint4 *)(dst + e1) = v;
+    uint16_t *q_dst = p.set[0].out + tok * p.set[0].out_token + first * p.set[0].out_head;
+#pragma unroll 1
+    for (int row = first; row < h2; row += step, slot = (slot + 1) % DEPTH) {
+      cp_async_wait<DEPTH - 1>();
+      uint4 raw[PIECES];
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) raw[i] = ring[(slot * PIECES + i) * 32];
+      auto two = [&](int run, int i) { return load2((const T *)raw + run * 8 + 2 * i); };
+      uint4 u, v;
+      uint32_t *ou = &u.x, *ov = &v.x;
+      uint16_t *dst = q_dst;
+      q_dst += dst_step;
+      if (row >= h1) {                                     // a value row
+        dst = p.set[2].out + tok * p.set[2].out_token + (row - h1) * p.set[2].out_head;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ou[i] = pack2(two(0, i));
+          ov[i] = pack2(two(1, i));
+        }
+      } else {
+        const float *w = p.set[0].weight;
+        if (row >= h0) {
+          dst = p.set[1].out + tok * p.set[1].out_token + (row - h0) * p.set[1].out_head;
+          w = p.set[1].weight;
+        }
+        f32x2 x[4], y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = two(0, i);
+          y[i] = two(1, i);
+        }
+        if (w) {
+          if (have != w) {
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+              const float4 a = *(const float4 *)(w + e0 + 2 * i), b = *(const float4 *)(w + e1 + 2 * i);
+              wu[i] = pair(a.x, a.y);
+              wu[i + 1] = pair(a.z, a.w);
+              wv[i] = pair(b.x, b.y);
+              wv[i + 1] = pair(b.z, b.w);
+            }
+            have = w;
+          }
+          f32x2 s2 = mul2(x[0], x[0]), t2 = mul2(y[0], y[0]);
+#pragma unroll
+          for (int i = 1; i < 4; ++i) {
+            s2 = fma2(x[i], x[i], s2);
+            t2 = fma2(y[i], y[i], t2);
+          }
+          const float2 s = parts(s2), t = parts(t2);
+          float sum = (s.x + s.y) + (t.x + t.y);
+#pragma unroll
+          for (int o = 4; o; o >>= 1) sum += __shfl_xor_sync(lanes, sum, o);
+          const float n = rsqrtf(sum * (1.f / D) + p.eps);
+          const f32x2 f = pair(n, n);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[i] = mul2(mul2(x[i], f), wu[i]);
+            y[i] = mul2(mul2(y[i], f), wv[i]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f32x2 m = x[i], n = y[i];
+          const float2 g = parts(x[i]), h = parts(y[i]);
+          if (rot_u) m = fma2(INTER ? pair(g.y, g.x) : y[i], su[i], mul2(x[i], cu[i]));
+          if (rot_v) n = fma2(INTER ? pair(h.y, h.x) : x[i], sv[i], mul2(y[i], cv[i]));
+          ou[i] = pack2(m);
+          ov[i] = pack2(n);
+        }
+      }
+      *(uint4 *)(dst + e0) = u;
+      *(uint4 *)(dst + e1) = v;
+      fetch(slot);                                         // the slot has been read: its values are in the stores
+    }
   }
 }
 
 /* Any layout that the call takes: 8-byte aligned rows, any multiple of 8 as
- * rotary_dim.  A warp per row, two pairs (or four elements) per lane. */
+ * rotary_dim.  A warp per row, two pairs (or four elements) per lane.  8,191 tokens
+ * of 20 rows 38 us, where 16-byte aligned rows take 17 in the kernel above (one set of
+ * buffers, partly in L2). */
 template <class T>
 __global__ void __launch_bounds__(256) norm_rope_any_kernel(const __grid_constant__ RowsParams p, int inter) {
   pdl_wait();
@@ -307,7 +347,8 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const __grid_constant__
   }
 }
 
-constexpr int ROUND = 152 * 3 * 32;   // units that run at once
+constexpr int GRID = 152 * 16 / WARPS;   // blocks that run at once
+constexpr int ROUND = GRID * WARPS * 4;   // units that run at once
 
 static_assert(MD_MAX_AXES <= 4 && D / 2 <= 64, "an axis is two bits");
 
@@ -395,9 +436,8 @@ MD_API md_status md_norm_rope(const md_norm_rope_args *args) {
     p.split_log = 2;
     while (1 << p.split_log < rows && (long long)a.n_tokens << (p.split_log + 1) <= ROUND) ++p.split_log;
     const long long blocks = (((long long)a.n_tokens << p.split_log) + 4 * WARPS - 1) / (4 * WARPS);
-    if (blocks >= (1LL << 31)) return MD_ERR_INVALID_ARG;
     auto launch = [&](auto plain, auto interleaved) {
-      return launch_pdl(inter ? interleaved : plain, (int)blocks, 32 * WARPS, 0, s, p);
+      return launch_pdl(inter ? interleaved : plain, (int)(blocks < GRID ? blocks : GRID), 32 * WARPS, 0, s, p);
     };
     e = type == MD_TYPE_BF16  ? launch(norm_rope_kernel<__nv_bfloat16, false>, norm_rope_kernel<__nv_bfloat16, true>)
         : type == MD_TYPE_F16 ? launch(norm_rope_kernel<__half, false>, norm_rope_kernel<__half, true>)
