@@ -551,11 +551,14 @@ md_status md_page_top(const float *scores_dev, const int32_t *n_tokens_host, int
 
 /* Attention over the cached tokens of the listed pages, for every layer and
  * query head, with md_decode_step's arithmetic but for the softmax weights, which
- * enter the product with V as two bf16 terms each; entries outside a sequence's
- * pages (-1) are skipped, and a row that lists no token yields zeros.
+ * enter the product with V as two bf16 terms each (an infinite value may turn
+ * NaN); entries outside a sequence's pages (-1) are skipped, and a row that lists
+ * no token yields zeros.  How a row is split over CTAs goes by the launch's shape:
+ * calls of the same shape give the same bits, others may round differently.  The
+ * kernel's waits for its own copies are bounded (2 s); a row that gives up is NaN.
  *   page_ids_dev  int32 [batch][L][Hkv][top_pages], each page at most once
  *   q_dev         bf16 [batch][L][Hq][128] (16-byte aligned)
- *   out_dev       bf16 [batch][L][Hq][128] (written)
+ *   out_dev       bf16 [batch][L][Hq][128] (8-byte aligned, written)
  *   mass_dev      fp32 [batch][L][Hkv][top_pages][page_size], or NULL: for every
  *                 token of the listed pages, the sum over the KV head's query
  *                 heads of their softmax weight on it; 0 at entries and slots

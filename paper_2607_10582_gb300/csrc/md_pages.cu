@@ -737,16 +737,17 @@ AttendForm attend_form(const AttendPagesParams &p) {
   for (int lg = 0; lg < 5; ++lg)
     for (int warps = 4; warps <= 8; warps += 4)
       for (int stages = 1; stages <= STAGES; ++stages) {
-        const int C = 1 << lg, W = C * warps;
+        const int C = 1 << lg, lgW = lg + (warps == 8 ? 3 : 2), W = 1 << lgW;
         if (W > 2 * listed && W > 8) continue;
-        const size_t smem = attend_smem(C, warps, stages, (listed + W - 1) / W);
+        const size_t smem = attend_smem(C, warps, stages, (listed + W - 1) >> lgW);
         if (smem > MAX_ATTEND_SMEM) continue;
-        const int per_sm = std::min(16 / warps, (int)(228 * 1024 / (smem + 1024)));
+        int per_sm = 1;                      // by shared memory, and by registers
+        while (per_sm < 16 / warps && (per_sm + 1) * (smem + 1024) <= 228 * 1024) ++per_sm;
         const float part = C <= 2 ? 1.f : per_sm > 1 ? (C == 4 ? 0.97f : C == 8 ? 0.93f : 0.72f)
                                                      : (C == 4 ? 0.94f : C == 8 ? 0.78f : 0.6f);
         const float slots = per_sm * SMS * part, N = rows * C;
         const float cta = 4.f + (C > 1 ? 0.73f : 0.f) + (C == 16 ? 0.13f : 0.f) + (warps == 8 ? 0.21f : 0.f) +
-                          (float)((T + W - 1) / W) * (stages == 1 ? 0.72f : 0.42f);
+                          (float)((T + W - 1) >> lgW) * (stages == 1 ? 0.72f : 0.42f);
         const float cost = N <= slots ? cta + 0.0021f * N : 1e6f + N / slots * cta + 0.0012f * N;
         if (cost < least) {
           least = cost;
