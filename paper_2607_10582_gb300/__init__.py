@@ -236,10 +236,9 @@ def _ops():
     if _torch_calls is None:
         import torch
         b = _binding()
-        b.load_torch((torch.bfloat16, torch.float16, torch.float32, torch.int16, torch.int32),
-                     getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
-                     getattr(torch._C, "_cuda_getCurrentRawStream",
-                             lambda d: torch.cuda.current_stream(d).cuda_stream))
+        d = os.path.join(os.path.dirname(torch.__file__), "lib")
+        b.load_torch(torch.Tensor, torch.nn.Parameter, os.path.join(d, "libtorch_cpu.so"),
+                     os.path.join(d, "libtorch_cuda.so"))
         _torch_calls = b
     return _torch_calls
 

@@ -18,7 +18,7 @@
 
 #include "../../include/memdecay.h"
 
-static PyObject *s_data_ptr, *s_is_cuda, *s_is_contiguous, *s_shape, *s_stride, *s_dtype, *s_get_device;
+static PyObject *s_data_ptr, *s_is_cuda, *s_is_contiguous, *s_cdata;
 static md_status (*f_decode_step)(md_ctx *, int, const void *, const void *, const void *, const uint8_t *, void *);
 static md_status (*f_decode_step_host)(md_ctx *, int, const void *, const void *, const void *, const uint8_t *,
                                        void *);
@@ -34,9 +34,6 @@ static md_status (*f_page_scores)(const void *, const void *, const int32_t *, c
 static md_status (*f_page_top)(const float *, const int32_t *, int32_t *, int, int, int, int, int, int, int, int, void *);
 static md_status (*f_attend_pages)(const void *, const void *, const int32_t *, const int32_t *, const int32_t *, void *,
                                    float *, int, int, int, int, int, int, int, int, void *);
-/* torch's dtypes bfloat16, float16, float32, int16, int32, and its functions for
- * the current device and the raw current stream of a device (load_torch) */
-static PyObject *t_types[5], *t_device, *t_stream;
 
 static PyObject *load(PyObject *self, PyObject *path) {
   const char *s = PyUnicode_AsUTF8(path);
@@ -231,61 +228,108 @@ static PyObject *get_state(PyObject *self, PyObject *const *a, Py_ssize_t n) {
  * shape, layout or device, an argument missing) they leave to the caller, by
  * None, who converts it or says what is wrong ---- */
 
-/* load_torch(types, current_device, current_raw_stream) */
-static PyObject *load_torch(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-  if (arity(n, 3)) return NULL;
-  if (!PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 5) {
-    PyErr_SetString(PyExc_TypeError, "five types expected");
-    return NULL;
-  }
-  for (int i = 0; i < 5; ++i) Py_XSETREF(t_types[i], Py_NewRef(PyTuple_GET_ITEM(a[0], i)));
-  Py_XSETREF(t_device, Py_NewRef(a[1]));
-  Py_XSETREF(t_stream, Py_NewRef(a[2]));
-  Py_RETURN_NONE;
-}
-
+/* A tensor's address, type, shape, strides and device come from torch's C interface
+ * (exported by its libraries, the same across versions), which takes the address of
+ * a pointer to the tensor's implementation: one attribute of the Python object.
+ * Through the object's attributes instead, a call with ten tensors took 2.5 us longer. */
 enum { T_BF16, T_F16, T_F32, T_I16, T_I32, T_OTHER };
 #define MAX_DIMS 6
+
+static struct {
+  PyObject *tensor, *parameter;      /* torch.Tensor, torch.nn.Parameter; tensor NULL: not loaded */
+  int32_t types[T_OTHER], cuda;
+  int32_t (*get_data_ptr)(void *, void **);
+  int32_t (*get_dim)(void *, int64_t *);
+  int32_t (*get_sizes)(void *, int64_t **);
+  int32_t (*get_strides)(void *, int64_t **);
+  int32_t (*get_dtype)(void *, int32_t *);
+  int32_t (*get_device_type)(void *, int32_t *);
+  int32_t (*get_device_index)(void *, int32_t *);
+  int32_t (*current_device)(int32_t *);
+  int32_t (*current_stream)(int32_t, void **);
+} torch_c;
+
+/* load_torch(Tensor, Parameter, path of libtorch_cpu, of libtorch_cuda) -> whether
+ * the calls below take tensors; the libraries are the ones torch has loaded */
+static PyObject *load_torch(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  if (arity(n, 4)) return NULL;
+  const char *cpu = PyUnicode_AsUTF8(a[2]), *cuda = cpu ? PyUnicode_AsUTF8(a[3]) : NULL;
+  if (!cuda) return NULL;
+  void *l = dlopen(cpu, RTLD_NOW | RTLD_NOLOAD), *g = dlopen(cuda, RTLD_NOW | RTLD_NOLOAD);
+  if (!l || !g) Py_RETURN_FALSE;
+  static const char *const kinds[T_OTHER] = {"aoti_torch_dtype_bfloat16", "aoti_torch_dtype_float16",
+                                             "aoti_torch_dtype_float32", "aoti_torch_dtype_int16",
+                                             "aoti_torch_dtype_int32"};
+  int32_t (*kind)(void);
+  for (int i = 0; i < T_OTHER; ++i) {
+    *(void **)&kind = dlsym(l, kinds[i]);
+    if (!kind) Py_RETURN_FALSE;
+    torch_c.types[i] = kind();
+  }
+  *(void **)&kind = dlsym(l, "aoti_torch_device_type_cuda");
+  if (!kind) Py_RETURN_FALSE;
+  torch_c.cuda = kind();
+  *(void **)&torch_c.get_data_ptr = dlsym(l, "aoti_torch_get_data_ptr");
+  *(void **)&torch_c.get_dim = dlsym(l, "aoti_torch_get_dim");
+  *(void **)&torch_c.get_sizes = dlsym(l, "aoti_torch_get_sizes");
+  *(void **)&torch_c.get_strides = dlsym(l, "aoti_torch_get_strides");
+  *(void **)&torch_c.get_dtype = dlsym(l, "aoti_torch_get_dtype");
+  *(void **)&torch_c.get_device_type = dlsym(l, "aoti_torch_get_device_type");
+  *(void **)&torch_c.get_device_index = dlsym(l, "aoti_torch_get_device_index");
+  *(void **)&torch_c.current_device = dlsym(l, "aoti_torch_get_current_device_index");
+  *(void **)&torch_c.current_stream = dlsym(g, "aoti_torch_get_current_cuda_stream");
+  if (!torch_c.get_data_ptr || !torch_c.get_dim || !torch_c.get_sizes || !torch_c.get_strides || !torch_c.get_dtype ||
+      !torch_c.get_device_type || !torch_c.get_device_index || !torch_c.current_device || !torch_c.current_stream)
+    Py_RETURN_FALSE;
+  Py_XSETREF(torch_c.parameter, Py_NewRef(a[1]));
+  Py_XSETREF(torch_c.tensor, Py_NewRef(a[0]));
+  Py_RETURN_TRUE;
+}
 
 typedef struct {
   void *p;
   int dims, type;
-  long long n[MAX_DIMS];
+  int32_t device;
+  int64_t n[MAX_DIMS], stride[MAX_DIMS];
 } tensor;
 
-/* Integers of a tuple: their number, or -1. */
-static int tuple_of(PyObject *t, long long *out) {
-  if (!t || !PyTuple_Check(t) || PyTuple_GET_SIZE(t) > MAX_DIMS) return -1;
-  const int n = (int)PyTuple_GET_SIZE(t);
-  for (int i = 0; i < n; ++i) out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
-  return n;
-}
-
-static int is_true(PyObject *v) {
-  const int r = v == Py_True;
-  Py_XDECREF(v);
-  return r;
-}
-
-/* A device tensor's address, type and shape: 1, or 0 (an exception may be set). */
+/* A tensor on a GPU (not of a subclass, which may be something else): 1, or 0 (an
+ * exception may be set). */
 static int device_tensor(PyObject *o, tensor *t) {
-  if (o == Py_None || !is_true(PyObject_GetAttr(o, s_is_cuda))) return 0;
-  PyObject *v = PyObject_GetAttr(o, s_shape);
-  t->dims = tuple_of(v, t->n);
-  Py_XDECREF(v);
-  if (t->dims < 0) return 0;
-  v = PyObject_GetAttr(o, s_dtype);
-  for (t->type = 0; t->type < T_OTHER && v != t_types[t->type]; ++t->type) {
+  if (!torch_c.tensor || ((PyObject *)Py_TYPE(o) != torch_c.tensor && (PyObject *)Py_TYPE(o) != torch_c.parameter)) return 0;
+  PyObject *v = PyObject_GetAttr(o, s_cdata);
+  if (!v) return 0;
+  void *impl = PyLong_AsVoidPtr(v);
+  Py_DECREF(v);
+  if (!impl) return 0;
+  int32_t kind, type;
+  int64_t dims, *n, *stride;
+  if (torch_c.get_device_type(&impl, &kind) || kind != torch_c.cuda || torch_c.get_device_index(&impl, &t->device) ||
+      torch_c.get_dtype(&impl, &type) || torch_c.get_dim(&impl, &dims) || dims > MAX_DIMS ||
+      torch_c.get_sizes(&impl, &n) || torch_c.get_strides(&impl, &stride) || torch_c.get_data_ptr(&impl, &t->p))
+    return 0;
+  t->dims = (int)dims;
+  for (int i = 0; i < dims; ++i) {
+    t->n[i] = n[i];
+    t->stride[i] = stride[i];
   }
-  Py_XDECREF(v);
-  return v && dev_ptr(o, &t->p) == 0;
+  for (t->type = 0; t->type < T_OTHER && torch_c.types[t->type] != type; ++t->type) {
+  }
+  return 1;
 }
 
 static int two_bytes(const tensor *t) { return t->type == T_BF16 || t->type == T_I16; }
 
 /* A contiguous one. */
 static int dense_tensor(PyObject *o, tensor *t) {
-  return device_tensor(o, t) && is_true(PyObject_CallMethodNoArgs(o, s_is_contiguous));
+  if (!device_tensor(o, t)) return 0;
+  int64_t want = 1;
+  for (int i = t->dims - 1; i >= 0; --i) {
+    if (t->n[i] == 0) return 1;
+    if (t->n[i] > 1 && t->stride[i] != want) return 0;
+    want *= t->n[i];
+  }
+  return 1;
 }
 
 static int has_shape(const tensor *t, int dims, long long a, long long b, long long c, long long d, long long e) {
@@ -296,23 +340,12 @@ static int has_shape(const tensor *t, int dims, long long a, long long b, long l
   return 1;
 }
 
-/* The stream of a call on tensor x: an address, or None for the current one.  x
- * has to lie on the current device (the others are taken to lie there too). */
-static int call_stream(PyObject *x, PyObject *o, void **out) {
-  PyObject *dev = PyObject_CallNoArgs(t_device), *own = dev ? PyObject_CallMethodNoArgs(x, s_get_device) : NULL;
-  const int here = own && PyLong_AsLong(own) == PyLong_AsLong(dev);
-  Py_XDECREF(own);
-  int ok = here;
-  if (here && o == Py_None) {
-    PyObject *s = PyObject_CallOneArg(t_stream, dev);
-    *out = s ? (void *)(uintptr_t)PyLong_AsUnsignedLongLongMask(s) : NULL;
-    ok = s && !PyErr_Occurred();
-    Py_XDECREF(s);
-  } else if (here) {
-    ok = dev_ptr(o, out) == 0;
-  }
-  Py_XDECREF(dev);
-  return ok;
+/* The stream of a call whose tensors lie on `device`, which has to be the current
+ * one: an address, or None for the current stream. */
+static int call_stream(int32_t device, PyObject *o, void **out) {
+  int32_t now;
+  if (torch_c.current_device(&now) || now != device) return 0;
+  return o == Py_None ? torch_c.current_stream(device, out) == 0 : dev_ptr(o, out) == 0;
 }
 
 static PyObject *leave(void) {
@@ -330,14 +363,9 @@ static int count_view(PyObject *o, long long batch, Py_buffer *view) {
 
 /* Rows [tokens][heads][128] with their strides over tokens and heads. */
 static int row_tensor(PyObject *o, tensor *t, int64_t *token, int64_t *head) {
-  long long s[MAX_DIMS];
-  if (!device_tensor(o, t) || t->dims != 3 || t->n[2] != MD_HEAD_DIM) return 0;
-  PyObject *v = PyObject_CallMethodNoArgs(o, s_stride);
-  const int n = tuple_of(v, s);
-  Py_XDECREF(v);
-  if (n != 3 || s[2] != 1) return 0;
-  *token = t->n[0] > 1 ? s[0] : 0;
-  *head = t->n[1] > 1 ? s[1] : 0;
+  if (!device_tensor(o, t) || t->dims != 3 || t->n[2] != MD_HEAD_DIM || t->stride[2] != 1) return 0;
+  *token = t->n[0] > 1 ? t->stride[0] : 0;
+  *head = t->n[1] > 1 ? t->stride[1] : 0;
   return 1;
 }
 
@@ -355,7 +383,8 @@ static PyObject *norm_rope(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     if (a[i] == Py_None) continue;
     if (!row_tensor(a[i], &x[i], in[i][0], in[i][1]) || !row_tensor(a[3 + i], &y[i], out[i][0], out[i][1]))
       return leave();
-    if (x[i].type != x[first].type || x[i].n[0] != x[first].n[0] || !two_bytes(&y[i]) || y[i].n[0] != x[i].n[0] ||
+    if (x[i].device != x[first].device || y[i].device != x[first].device || x[i].type != x[first].type ||
+        x[i].n[0] != x[first].n[0] || !two_bytes(&y[i]) || y[i].n[0] != x[i].n[0] ||
         y[i].n[1] != x[i].n[1])
       return leave();
   }
@@ -368,23 +397,25 @@ static PyObject *norm_rope(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   if (hv) r.v = x[2].p, r.v_out = y[2].p;
   for (int i = 0; i < 2; ++i) {
     if (a[8 + i] == Py_None || a[i] == Py_None) continue;
-    if (!dense_tensor(a[8 + i], &t) || t.type != T_F32 || !has_shape(&t, 1, MD_HEAD_DIM, 0, 0, 0, 0)) return leave();
+    if (!dense_tensor(a[8 + i], &t) || t.type != T_F32 || !has_shape(&t, 1, MD_HEAD_DIM, 0, 0, 0, 0) ||
+        t.device != x[first].device)
+      return leave();
     *(i ? &r.k_weight : &r.q_weight) = (const float *)t.p;
   }
   Py_buffer axes = {0};
   const double eps = PyFloat_AsDouble(a[10]);
-  if (PyErr_Occurred() || !call_stream(a[first], a[13], &r.stream)) return leave();
+  if (PyErr_Occurred() || !call_stream(x[first].device, a[13], &r.stream)) return leave();
   r.eps = (float)eps;
   r.interleaved = a[12] != Py_False;
   if (a[7] != Py_None) {
     if (!dense_tensor(a[7], &t) || t.type != T_F32 || t.dims != 3 || t.n[2] != 2 || t.n[0] > INT32_MAX ||
-        t.n[1] > MD_HEAD_DIM / 2)
+        t.n[1] > MD_HEAD_DIM / 2 || t.device != x[first].device)
       return leave();
     r.table = (const float *)t.p;
     r.table_len = (int)t.n[0];
     r.rotary_dim = 2 * (int)t.n[1];
     if (!dense_tensor(a[6], &t) || t.type != T_I32 || t.dims < 1 || t.dims > 2 || t.n[t.dims - 1] != r.n_tokens ||
-        (t.dims == 2 && t.n[0] > MD_MAX_AXES))
+        (t.dims == 2 && t.n[0] > MD_MAX_AXES) || t.device != x[first].device)
       return leave();
     r.positions = (const int32_t *)t.p;
     r.num_axes = t.dims == 2 ? (int)t.n[0] : 1;
@@ -422,7 +453,8 @@ static PyObject *page_bounds(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   if (arity(n, 6)) return NULL;
   if (!pool_tensor(a[0], &pool) || !block_table_tensor(a[1], &table) || !dense_tensor(a[4], &bounds) ||
       !two_bytes(&bounds) || !has_shape(&bounds, 5, pool.n[0], pool.n[1], pool.n[2], 2, MD_HEAD_DIM) ||
-      !call_stream(a[0], a[5], &s) || !count_view(a[2], table.n[0], &count))
+      table.device != pool.device || bounds.device != pool.device || !call_stream(pool.device, a[5], &s) ||
+      !count_view(a[2], table.n[0], &count))
     return leave();
   if (a[3] != Py_None && !count_view(a[3], table.n[0], &first)) {
     PyBuffer_Release(&count);
@@ -450,7 +482,8 @@ static PyObject *page_scores(PyObject *self, PyObject *const *a, Py_ssize_t n) {
       bounds.n[2] > INT32_MAX || bounds.n[3] != 2 || bounds.n[4] != MD_HEAD_DIM || !block_table_tensor(a[2], &table) ||
       !has_shape(&q, 4, table.n[0], bounds.n[0], q.n[2], MD_HEAD_DIM, 0) || !dense_tensor(a[4], &scores) ||
       scores.type != T_F32 || !has_shape(&scores, 4, table.n[0], bounds.n[0], bounds.n[2], table.n[1], 0) ||
-      as_int(a[5], &ps) || !call_stream(a[0], a[6], &s) || !count_view(a[3], table.n[0], &count))
+      as_int(a[5], &ps) || bounds.device != q.device || table.device != q.device || scores.device != q.device ||
+      !call_stream(q.device, a[6], &s) || !count_view(a[3], table.n[0], &count))
     return leave();
   int st;
   Py_BEGIN_ALLOW_THREADS
@@ -472,7 +505,8 @@ static PyObject *page_top(PyObject *self, PyObject *const *a, Py_ssize_t n) {
       scores.n[1] > 255 || scores.n[2] > INT32_MAX || scores.n[3] > INT32_MAX || !dense_tensor(a[2], &ids) ||
       ids.type != T_I32 || ids.dims != 4 || ids.n[3] > INT32_MAX ||
       !has_shape(&ids, 4, scores.n[0], scores.n[1], scores.n[2], ids.n[3], 0) || as_int(a[3], &ps) ||
-      as_int(a[4], &first) || as_int(a[5], &last) || !call_stream(a[0], a[6], &s) || !count_view(a[1], scores.n[0], &count))
+      as_int(a[4], &first) || as_int(a[5], &last) || ids.device != scores.device ||
+      !call_stream(scores.device, a[6], &s) || !count_view(a[1], scores.n[0], &count))
     return leave();
   int st;
   Py_BEGIN_ALLOW_THREADS
@@ -499,7 +533,9 @@ static PyObject *attend_pages(PyObject *self, PyObject *const *a, Py_ssize_t n) 
       (!dense_tensor(a[6], &mass) || mass.type != T_F32 ||
        !has_shape(&mass, 4, table.n[0], pool.n[0], pool.n[2], ids.n[3] * pool.n[4], 0)))
     return leave();
-  if (!call_stream(a[0], a[7], &s) || !count_view(a[3], table.n[0], &count)) return leave();
+  if (pool.device != q.device || table.device != q.device || ids.device != q.device || out.device != q.device ||
+      (mass.p && mass.device != q.device) || !call_stream(q.device, a[7], &s) || !count_view(a[3], table.n[0], &count))
+    return leave();
   int st;
   Py_BEGIN_ALLOW_THREADS
   st = f_attend_pages(q.p, pool.p, table.p, count.buf, ids.p, out.p, mass.p, (int)table.n[0], (int)pool.n[0],
@@ -530,9 +566,6 @@ PyMODINIT_FUNC PyInit__calls(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_is_cuda = PyUnicode_InternFromString("is_cuda");
   s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-  s_shape = PyUnicode_InternFromString("shape");
-  s_stride = PyUnicode_InternFromString("stride");
-  s_dtype = PyUnicode_InternFromString("dtype");
-  s_get_device = PyUnicode_InternFromString("get_device");
-  return s_data_ptr && s_is_cuda && s_is_contiguous && s_shape && s_stride && s_dtype && s_get_device ? PyModule_Create(&module) : NULL;
+  s_cdata = PyUnicode_InternFromString("_cdata");
+  return s_data_ptr && s_is_cuda && s_is_contiguous && s_cdata ? PyModule_Create(&module) : NULL;
 }
