@@ -231,7 +231,9 @@ static PyObject *get_state(PyObject *self, PyObject *const *a, Py_ssize_t n) {
 /* A tensor's address, type, shape, strides and device come from torch's C interface
  * (exported by its libraries, the same across versions), which takes the address of
  * a pointer to the tensor's implementation: one attribute of the Python object.
- * Through the object's attributes instead, a call with ten tensors took 2.5 us longer. */
+ * Against reading the object's attributes, on a Grace core, a call: norm_rope of one
+ * token (ten tensors) 6.4 -> 4.0 us, bounds of 32 pages 4.4 -> 3.5, scores of one row
+ * 4.7 -> 3.5, attention of one row over one layer 5.9 -> 4.9. */
 enum { T_BF16, T_F16, T_F32, T_I16, T_I32, T_OTHER };
 #define MAX_DIMS 6
 
@@ -553,7 +555,7 @@ static PyMethodDef methods[] = {
     {"decode_layer", (PyCFunction)(void (*)(void))decode_layer, METH_FASTCALL, "md_decode_layer"},
     {"evict", (PyCFunction)(void (*)(void))evict, METH_FASTCALL, "md_evict"},
     {"get_state", (PyCFunction)(void (*)(void))get_state, METH_FASTCALL, "md_get_state"},
-    {"load_torch", (PyCFunction)(void (*)(void))load_torch, METH_FASTCALL, "load_torch(types, device, stream)"},
+    {"load_torch", (PyCFunction)(void (*)(void))load_torch, METH_FASTCALL, "load_torch(Tensor, Parameter, libtorch_cpu, libtorch_cuda)"},
     {"norm_rope", (PyCFunction)(void (*)(void))norm_rope, METH_FASTCALL, "md_norm_rope"},
     {"page_bounds", (PyCFunction)(void (*)(void))page_bounds, METH_FASTCALL, "md_page_bounds"},
     {"page_scores", (PyCFunction)(void (*)(void))page_scores, METH_FASTCALL, "md_page_scores"},
