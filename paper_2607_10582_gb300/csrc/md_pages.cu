@@ -459,9 +459,10 @@ __global__ void __launch_bounds__(32 * NW)
           for (int i = 0; i < 2; ++i) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], s));
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+          const float last = m[i];                   // -inf: nothing to rescale
           m[i] = fmaxf(m[i], mx[i]);
-          const float alpha = ex2(base[i] - max_base(m[i]));
           base[i] = max_base(m[i]);
+          const float alpha = ex2(last - base[i]);
           lim[i] = m[i] + SLACK;
           z[i] *= alpha;
 #pragma unroll

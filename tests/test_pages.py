@@ -255,6 +255,24 @@ def test_flat_and_steep_softmax(scale):
 
 
 @gpu
+@pytest.mark.parametrize("lengths,top", [([16], 1), ([700, 3000], 188), ([3000] * 40, 60)])
+@pytest.mark.parametrize("low,high", [(-10.0, -10.0), (-60.0, -9.0), (-60.0, 60.0), (40.0, -40.0)])
+def test_logits_far_from_zero(lengths, top, low, high):
+    """All logits of a list, or of its parts, at +-100 to +-680: the weights' base moves as far."""
+    _need_gpu()
+    c = Case(2, 16, 2, 16, lengths, seed=11)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    s = torch.where(torch.rand(D, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    c.q = (s * (1 + 0.02 * torch.randn((c.B, c.L, c.Hq, D), generator=g, device="cuda"))).bfloat16()
+    level = torch.where(torch.rand(c.P, generator=g, device="cuda") < 0.5, low, high)[:, None, None, None]
+    noise = 0.05 * torch.randn((c.L, c.P, c.Hkv, c.ps, D), generator=g, device="cuda")
+    k = c.pool[:, :, :, 0]
+    c.pool[:, :, :, 0] = torch.where(k.isnan(), k, (s * level + noise).bfloat16())
+    ids = _pick(c, top, 13)
+    c.check_attend(ids, *c.attend(ids))
+
+
+@gpu
 def test_infinite_and_nan_tokens_stay_in_their_heads():
     _need_gpu()
     c = Case(1, 4, 2, 16, [200, 100], seed=9)
