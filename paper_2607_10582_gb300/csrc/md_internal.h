@@ -333,7 +333,7 @@ cudaError_t launch_pdl(void (*kernel)(P), dim3 grid, int threads, int smem, cuda
 }
 
 /* Runs f (it sets kernel attributes) once per device; WHICH: for which kernels. */
-enum { ATTR_ATTEND_4, ATTR_ATTEND_8 };
+enum { ATTR_ATTEND_4, ATTR_ATTEND_8 = ATTR_ATTEND_4 + 3 };   // three kernels each
 template <int WHICH, class F>
 cudaError_t once_per_device(F f) {
   static std::atomic<unsigned long long> done{0};

@@ -306,9 +306,14 @@ __global__ void __launch_bounds__(threads) page_top_kernel(const __grid_constant
  * score exceeds it by SLACK: most tiles then need no exchange between lanes and
  * no rescaling.
  *
- * Scores stay in shared memory for the masses, which need the final maxima and
- * sums.  Each CTA pushes those, and its part of the others' slices of O, into the
- * others' shared memory; after one cluster barrier each has all it needs.
+ * The masses need the scores again with the final maxima and sums.  A row of one CTA
+ * keeps them in tensor memory, four columns per tile in its warp's lanes: the shared
+ * memory is left to the tiles, and up to four CTAs share an SM where their scores would
+ * leave room for one (4 x 65,536 tokens, 36 layers: 105 -> 96 us).  A cluster keeps them
+ * in shared memory: a row's tiles are spread over more warps there, and no CTA waits for
+ * columns while another waits for it.  Each of its CTAs pushes its maxima and sums, and
+ * its part of the others' slices of O, into the others' shared memory; after one cluster
+ * barrier each has all it needs.
  *
  * A copy that does not land within the limit makes its row NaN (and is reported
  * in the status words, where there are any). */
@@ -320,13 +325,23 @@ constexpr int OS = D + 4;                    // padded row of a warp's O
 constexpr int MAX_ATTEND_SMEM = 227 * 1024;
 static_assert(GP * OS * 4 <= TILE_BYTES, "a warp's O fits a stage");
 constexpr size_t attend_smem(int C, int warps, int stages, int warp_tiles) {
-  return 1024 + (size_t)warps * (stages * TILE_BYTES + warp_tiles * (SCORE_BYTES + 4)) + 2 * warps * GP * 4 + 2 * GP * 4 +
-         (C > 1 ? (MAX_CLUSTER * GP * 2 + GP * D) * 4 : 0) + warps * STAGES * 8;
+  return 1024 + (size_t)warps * (stages * TILE_BYTES + warp_tiles * (4 + (C > 1 ? SCORE_BYTES : 0))) + 2 * warps * GP * 4 +
+         2 * GP * 4 + (C > 1 ? (MAX_CLUSTER * GP * 2 + GP * D) * 4 : 0) + warps * STAGES * 8 + 8;
+}
+
+/* Columns of tensor memory that hold the scores of a CTA's warps (of C = 1): a power of
+ * two, 32 at least; above TM_COLUMNS there is no room.  Warps w and w + 4 share lanes. */
+constexpr int TM_COLUMNS = 512;
+constexpr int attend_columns(int warps, int warp_tiles) {
+  int n = 32;
+  while (n < 4 * warp_tiles * (warps / 4)) n *= 2;
+  return n;
 }
 
 struct AttendParams : AttendPagesParams {
   int C, stages;       // CTAs per row; tiles in flight per warp
   int warp_tiles;      // most tiles of a warp whose scores are kept
+  int columns;         // of tensor memory (C = 1), where scores are kept
 };
 
 /* Bounded wait on an mbarrier phase. */
@@ -340,23 +355,55 @@ __device__ __noinline__ bool wait_copy(uint32_t bar, uint32_t parity, long long 
 /* The maxima against which weights are taken: 0 where nothing but -inf was seen. */
 __device__ __forceinline__ float max_base(float m) { return m == -INFINITY ? 0.f : m; }
 
-template <int NW>
+/* ---- tensor memory ---- */
+__device__ __forceinline__ void tm_alloc(uint32_t smem, int columns) {      // a whole warp
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem), "r"(columns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tm_free(uint32_t at, int columns) {         // the same warp
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+}
+__device__ __forceinline__ void tm_before_barrier() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tm_after_barrier() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tm_store4(uint32_t at, const float (&x)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(__float_as_uint(x[0])),
+               "r"(__float_as_uint(x[1])), "r"(__float_as_uint(x[2])), "r"(__float_as_uint(x[3]))
+               : "memory");
+}
+__device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_load8(uint32_t at, float (&x)[8]) {
+  uint32_t u[8];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+      : "r"(at)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(u[i]);
+}
+
+/* ONE: C is 1.  TM: scores are kept, in tensor memory.  A kernel with masses and one
+ * without, as the SM starts no second CTA of a kernel with tm_alloc before the first has
+ * got that far: with both in one kernel, calls without masses took up to 1.9 times as long. */
+template <int NW, bool ONE, bool TM>
 __global__ void __launch_bounds__(32 * NW)
     attend_pages_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ CUtensorMap tmap) {
   extern __shared__ uint8_t smem_raw[];
   const int stages = p.stages, WARP_FLOATS = stages * TILE_BYTES / 4;
   float *so = (float *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);   // [NW] the warps' stages, later their O [8][OS]
-  float *sc = so + NW * WARP_FLOATS;                 // [NW][warp_tiles][16][8] scores
-  float *sm = sc + NW * p.warp_tiles * TILE * GP;    // [NW][8] maxima, then sums
+  float *sc = so + NW * WARP_FLOATS;                 // [NW][warp_tiles][16][8] scores (not ONE)
+  float *sm = sc + (ONE ? 0 : NW * p.warp_tiles * TILE * GP);   // [NW][8] maxima, then sums
   float *sl = sm + NW * GP;
   float *fin = sl + NW * GP;                         // [8] final maxima, [8] 1 / sums
   float *xo = fin + 2 * GP;                          // [C][1024 / C] every CTA's part of this one's slice
-  float *xml = xo + (p.C > 1 ? GP * D : 0);          // [C][8][2]
-  uint64_t *full = (uint64_t *)(xml + (p.C > 1 ? MAX_CLUSTER * GP * 2 : 0));   // [NW][STAGES]
-  int *sv = (int *)(full + NW * STAGES);             // [NW][warp_tiles] tokens per tile
+  float *xml = xo + (ONE ? 0 : GP * D);              // [C][8][2]
+  uint64_t *full = (uint64_t *)(xml + (ONE ? 0 : MAX_CLUSTER * GP * 2));   // [NW][STAGES]
+  uint32_t *columns = (uint32_t *)(full + NW * STAGES);   // address of the tensor memory (ONE)
+  int *sv = (int *)(columns + 2);                    // [NW][warp_tiles] tokens per tile
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int mi = lane >> 3, rr = lane & 7;           // ldmatrix: matrix and row of this lane's address
-  const int C = p.C, row = blockIdx.x / C, rank = blockIdx.x - row * C;
+  const int C = ONE ? 1 : p.C, row = blockIdx.x / C, rank = blockIdx.x - row * C;
   const uint32_t ring = smem_u32(so) + warp * stages * TILE_BYTES, bars = smem_u32(full + warp * STAGES);
   if (lane < STAGES) {
     mbar_init(bars + lane * 8, 1);
@@ -364,7 +411,7 @@ __global__ void __launch_bounds__(32 * NW)
   }
   if (lane == 0) tma_prefetch_desc(&tmap);
   __syncwarp();
-  if (C > 1) cluster_arrive();                       // this CTA runs: the others may write its shared memory
+  if (!ONE) cluster_arrive();                        // this CTA runs: the others may write its shared memory
   const int lh = p.L * p.Hkv;
   const int b = row / lh, l = row % lh / p.Hkv, h = row % p.Hkv;
   const int shift = p.ps / TILE - 1, tiles = p.top << shift;   // tiles per page: 1 or 2
@@ -373,10 +420,16 @@ __global__ void __launch_bounds__(32 * NW)
   const int nt = tiles > w ? (tiles - w + W - 1) / W : 0;
   float *wsc = sc + warp * p.warp_tiles * TILE * GP;
   int *wsv = sv + warp * p.warp_tiles;
-  const bool masses = p.mass || p.mass_acc;
+  const bool masses = ONE ? TM : p.mass || p.mass_acc;
   const uint64_t stream = policy_evict_first();
   pdl_wait();
-  pdl_trigger();
+  /* Columns are taken after the launch before has freed its own, and before the next one may
+   * start: whoever waits for columns holds up none of those who have them. */
+  if (TM) {
+    if (warp == 0) tm_alloc(smem_u32(columns), p.columns);
+  } else {
+    pdl_trigger();
+  }
   /* tile n0 + lane of this warp: its page's row of the tensor map, its rows' offset there, its tokens */
   auto tile_info = [&](int n0, int &at, int &sub, int &valid) {
     at = sub = valid = 0;
@@ -412,19 +465,30 @@ __global__ void __launch_bounds__(32 * NW)
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   int done = 0, issued = 0;                          // tiles of this warp, across the lists of 32
+  unsigned todo, ahead;                              // of a list: tiles to compute, to copy
   bool landed = true;
-  for (int n0 = 0; n0 < nt && landed; n0 += 32) {
-    if (n0) tile_info(n0, at, sub, valid);
+  auto begin = [&](int n0) {                         // the first tiles of a list, a lane each
     if (masses && n0 + lane < nt) wsv[n0 + lane] = valid;
-    const unsigned some = __ballot_sync(0xffffffffu, valid > 0);
-    unsigned todo = some, ahead = some;              // tiles to compute, to copy
-    /* the first tiles, a lane each */
-    {
-      if (n0) fence_proxy_async_smem();              // behind the reads of the tiles before
-      const int i = __popc(some & ((1u << lane) - 1));
-      if (valid > 0 && i < stages) copy_tile((done + i) & (stages - 1), at, sub);
-      issued += min(__popc(some), stages);
-      for (int k = 0; k < stages; ++k) ahead &= ahead - 1;
+    todo = ahead = __ballot_sync(0xffffffffu, valid > 0);
+    const int i = __popc(todo & ((1u << lane) - 1));
+    if (valid > 0 && i < stages) copy_tile((done + i) & (stages - 1), at, sub);
+    issued += min(__popc(todo), stages);
+    for (int k = 0; k < stages; ++k) ahead &= ahead - 1;
+  };
+  begin(0);
+  uint32_t tm = 0;                                   // this warp's columns, four per tile
+  if (TM) {
+    tm_before_barrier();
+    __syncthreads();
+    tm_after_barrier();
+    pdl_trigger();
+    tm = *columns + (warp >> 2) * (p.columns / (NW / 4)) + ((warp & 3) << 21);   // lanes 32 (warp % 4) ..
+  }
+  for (int n0 = 0; n0 < nt; n0 += 32) {
+    if (n0) {
+      tile_info(n0, at, sub, valid);
+      fence_proxy_async_smem();                      // behind the reads of the tiles before
+      begin(n0);
     }
     for (; todo; todo &= todo - 1, ++done) {
       const int n = __ffs(todo) - 1, have = __shfl_sync(0xffffffffu, valid, n);
@@ -446,7 +510,9 @@ __global__ void __launch_bounds__(32 * NW)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         c[i] = g + 8 * (i >> 1) < have && 2 * t + (i & 1) < p.G ? (c[i] + c2[i]) * p.scale_log2 : -INFINITY;
-      if (masses) {
+      if (TM) {
+        tm_store4(tm + (n0 + n) * 4, c);
+      } else if (masses) {
         float *d = wsc + (n0 + n) * TILE * GP + g * GP + 2 * t;
         *(float2 *)d = make_float2(c[0], c[1]);
         *(float2 *)(d + 8 * GP) = make_float2(c[2], c[3]);
@@ -508,6 +574,7 @@ __global__ void __launch_bounds__(32 * NW)
         ahead &= ahead - 1;
       }
     }
+    if (!landed) break;
   }
   if (!landed) {                                     // what is in flight must land before the stages are reused
     for (; done < issued; ++done) wait_copy(bars + (done & (stages - 1)) * 8, done >> (stages - 1) & 1, DRAIN_LIMIT_NS);
@@ -557,7 +624,7 @@ __global__ void __launch_bounds__(32 * NW)
     }
   }
   auto inverse = [](float s) { return s > 0.f ? 1.f / s : s == 0.f ? 0.f : s; };   // no token: zeros; NaN stays
-  if (C == 1) {
+  if (ONE) {
 #pragma unroll
     for (int i = 0; i < GP / NW; ++i) {
       const int head = warp + i * NW;
@@ -610,32 +677,61 @@ __global__ void __launch_bounds__(32 * NW)
     }
     if (!masses) return;
   }
-  /* the masses of this warp's tiles: a lane per token, two tiles at a time */
-  float fm[GP], fz[GP];
-#pragma unroll
-  for (int i = 0; i < GP; ++i) {
-    fm[i] = fin[i];
-    fz[i] = fin[GP + i];
-  }
+  /* the masses of this warp's tiles, two at a time: a lane per token */
   const uint64_t keep = policy_evict_last();
-  const int tok = lane & 15;
-#pragma unroll 2
-  for (int n0 = 0; n0 < nt; n0 += 2) {
-    const int n = n0 + (lane >> 4), tile = w + W * n;
-    if (n >= nt) continue;
-    const int have = wsv[n];
-    const float4 *s = (const float4 *)(wsc + (n * TILE + tok) * GP);
-    float x = 0.f;
-    if (tok < have) {
-      const float4 u = s[0], v = s[1];
-      x = (ex2(u.x - fm[0]) * fz[0] + ex2(u.y - fm[1]) * fz[1]) + (ex2(u.z - fm[2]) * fz[2] + ex2(u.w - fm[3]) * fz[3]);
-      x += (ex2(v.x - fm[4]) * fz[4] + ex2(v.y - fm[5]) * fz[5]) + (ex2(v.z - fm[6]) * fz[6] + ex2(v.w - fm[7]) * fz[7]);
-    }
+  auto put = [&](int n, int tok, bool in, float x) {
+    const int tile = w + W * n;
     if (p.mass) p.mass[((size_t)row * tiles + tile) * TILE + tok] = x;
-    if (p.mass_acc && tok < have)
+    if (p.mass_acc && in)
       red_add_u64_hint(p.mass_acc + (size_t)page_id(p, b, p.ids[(size_t)row * p.top + (tile >> shift)]) * p.ps +
                            (tile & shift) * TILE + tok,
                        __float2ull_rn(x * MASS_SCALE), keep);
+  };
+  if constexpr (ONE) {
+    const float m0 = fin[2 * t], m1 = fin[2 * t + 1], z0 = fin[GP + 2 * t], z1 = fin[GP + 2 * t + 1];
+    tm_store_wait();
+    for (int n0 = 0; n0 < nt; n0 += 2) {
+      float c[8], x[4];                              // tokens g, g + 8 of tile n0, of the next: heads 2t, 2t + 1
+      tm_load8(tm + n0 * 4, c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = ex2(c[2 * i] - m0) * z0 + ex2(c[2 * i + 1] - m1) * z1;
+        x[i] += __shfl_xor_sync(0xffffffffu, x[i], 1);
+        x[i] += __shfl_xor_sync(0xffffffffu, x[i], 2);
+      }
+      const int n = n0 + (t >> 1), tok = g + 8 * (t & 1);
+      if (n < nt) {
+        const bool in = tok < wsv[n];
+        put(n, tok, in, in ? (t & 2 ? (t & 1 ? x[3] : x[2]) : (t & 1 ? x[1] : x[0])) : 0.f);
+      }
+      __syncwarp();
+    }
+    tm_before_barrier();
+    __syncthreads();
+    tm_after_barrier();
+    if (warp == 0) tm_free(*columns, p.columns);
+  } else {
+    float fm[GP], fz[GP];
+#pragma unroll
+    for (int i = 0; i < GP; ++i) {
+      fm[i] = fin[i];
+      fz[i] = fin[GP + i];
+    }
+    const int tok = lane & 15;
+#pragma unroll 2
+    for (int n0 = 0; n0 < nt; n0 += 2) {
+      const int n = n0 + (lane >> 4);
+      if (n >= nt) continue;
+      const int have = wsv[n];
+      const float4 *s = (const float4 *)(wsc + (n * TILE + tok) * GP);
+      float x = 0.f;
+      if (tok < have) {
+        const float4 u = s[0], v = s[1];
+        x = (ex2(u.x - fm[0]) * fz[0] + ex2(u.y - fm[1]) * fz[1]) + (ex2(u.z - fm[2]) * fz[2] + ex2(u.w - fm[3]) * fz[3]);
+        x += (ex2(v.x - fm[4]) * fz[4] + ex2(v.y - fm[5]) * fz[5]) + (ex2(v.z - fm[6]) * fz[6] + ex2(v.w - fm[7]) * fz[7]);
+      }
+      put(n, tok, tok < have, x);
+    }
   }
 }
 
@@ -680,18 +776,22 @@ cudaError_t launch_page_top(const PageTopParams &p, cudaStream_t s) {
 
 namespace {
 
-template <int NW>
+template <int NW, bool ONE, bool TM>
 cudaError_t launch_attend(const AttendParams &p, const CUtensorMap &tmap, cudaStream_t s) {
-  const cudaError_t e = once_per_device<NW == 8 ? ATTR_ATTEND_8 : ATTR_ATTEND_4>([] {
-    const cudaError_t e =
-        cudaFuncSetAttribute(attend_pages_kernel<NW>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_ATTEND_SMEM);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(attend_pages_kernel<NW>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  constexpr int which = (NW == 8 ? ATTR_ATTEND_8 : ATTR_ATTEND_4) + (TM ? 2 : ONE ? 1 : 0);
+  const cudaError_t e = once_per_device<which>([] {
+    const auto kernel = attend_pages_kernel<NW, ONE, TM>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_ATTEND_SMEM);
+    return e != cudaSuccess || ONE ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.n_seqs * p.L * p.Hkv * p.C));
   cfg.blockDim = dim3(32 * NW);
   cfg.dynamicSmemBytes = attend_smem(p.C, NW, p.stages, p.warp_tiles);
+  /* no more CTAs on an SM than there are columns for: none waits for them */
+  if (TM)
+    cfg.dynamicSmemBytes = std::max<size_t>(cfg.dynamicSmemBytes, 228 * 1024 / (TM_COLUMNS / p.columns + 1));
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -700,8 +800,8 @@ cudaError_t launch_attend(const AttendParams &p, const CUtensorMap &tmap, cudaSt
   attr[1].val.clusterDim.x = p.C;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = p.C > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, attend_pages_kernel<NW>, p, tmap);
+  cfg.numAttrs = ONE ? 1 : 2;
+  return cudaLaunchKernelEx(&cfg, attend_pages_kernel<NW, ONE, TM>, p, tmap);
 }
 
 }  // namespace
@@ -720,43 +820,49 @@ struct AttendForm {
  * launch takes beyond that, HBM for one, is the same in all forms.)
  *   The constants were fitted to 115 launches timed on a GB300 in up to 20 forms each (1
  * to 64 sequences, 1 to 36 layers, 2 to 600 tiles per list, 2 to 7,200 rows, up to
- * 110 us at the copy rate): the choice takes 1.7% longer than the best form of each on
- * average, 21% at worst.  Some of them: 2 rows of 64 tiles 4.6 us with 16 x 4 warps, 8.4
- * with 8; 64 rows of 48, 8.3 with 4 x 4 and 8.5 with 8 or 2 x 8; 1,152 rows of 48, 75 us
- * with 4 warps, 76 with 8, 81 with 2 x 4; 288 rows of 256, 101 to 107 with 8, 2 x 8 or
- * 4 x 8, 146 with 4.
- *   The scores' room is counted whether masses are wanted or not: the split, and with it
- * the rounding of a result, does not depend on it. */
+ * 110 us at the copy rate).  Of 150 launches of 15 us and more at the copy rate, those
+ * with masses take 1.7% longer than with the best form of each on average, 23% at worst;
+ * all 2.3%, and 57% at worst: rows of a few tiles under lists of hundreds, without masses.
+ * Some forms: 2 rows of 64 tiles 4.6 us with 16 x 4 warps, 8.4 with 8; 64 rows of 48, 8.3
+ * with 4 x 4 and 8.5 with 8 or 2 x 8; 288 rows of 256, 96 with 8 or 4, 106 with 2 x 8.
+ *   The scores' room counts whether masses are wanted or not: the split, and with it the
+ * rounding of a result, does not depend on it.  The tiles in flight do. */
 AttendForm attend_form(const AttendPagesParams &p) {
   constexpr float SMS = 152.f;
   const int tpp = p.ps / TILE, listed = p.top * tpp;
   int T = 1;
   for (int b = 0; b < p.n_seqs; ++b) T = std::max(T, std::min(p.n_pages[b], p.top) * tpp);
   const float rows = (float)p.n_seqs * p.L * p.Hkv;
+  auto cost = [&](int C, int warps, int stages, bool scores) {
+    const int W = C * warps, warp_tiles = scores ? (listed + W - 1) / W : 0;
+    const size_t smem = attend_smem(C, warps, stages, warp_tiles);
+    const int columns = C == 1 ? attend_columns(warps, warp_tiles) : 32;
+    if (smem > MAX_ATTEND_SMEM || columns > TM_COLUMNS) return INFINITY;
+    int per_sm = 1;                          // by shared memory, tensor memory and registers
+    while (per_sm < std::min(16 / warps, TM_COLUMNS / columns) && (per_sm + 1) * (smem + 1024) <= 228 * 1024) ++per_sm;
+    const float part = C <= 2 ? 1.f : per_sm > 1 ? (C == 4 ? 0.97f : C == 8 ? 0.93f : 0.72f)
+                                                 : (C == 4 ? 0.94f : C == 8 ? 0.78f : 0.6f);
+    const float slots = per_sm * SMS * part, N = rows * C;
+    const float cta = 4.f + (C > 1 ? 0.73f : 0.f) + (C == 16 ? 0.13f : 0.f) + (warps == 8 ? 0.21f : 0.f) +
+                      (float)((T + W - 1) / W) * (stages == 1 ? 0.72f : 0.42f);
+    return N <= slots ? cta + 0.0021f * N : 1e6f + N / slots * cta + 0.0012f * N;
+  };
   AttendForm best;
   float least = INFINITY;
-  for (int lg = 0; lg < 5; ++lg)
+  for (int C = 1; C <= MAX_CLUSTER; C *= 2)
     for (int warps = 4; warps <= 8; warps += 4)
       for (int stages = 1; stages <= STAGES; ++stages) {
-        const int C = 1 << lg, lgW = lg + (warps == 8 ? 3 : 2), W = 1 << lgW;
-        if (W > 2 * listed && W > 8) continue;
-        const size_t smem = attend_smem(C, warps, stages, (listed + W - 1) >> lgW);
-        if (smem > MAX_ATTEND_SMEM) continue;
-        int per_sm = 1;                      // by shared memory, and by registers
-        while (per_sm < 16 / warps && (per_sm + 1) * (smem + 1024) <= 228 * 1024) ++per_sm;
-        const float part = C <= 2 ? 1.f : per_sm > 1 ? (C == 4 ? 0.97f : C == 8 ? 0.93f : 0.72f)
-                                                     : (C == 4 ? 0.94f : C == 8 ? 0.78f : 0.6f);
-        const float slots = per_sm * SMS * part, N = rows * C;
-        const float cta = 4.f + (C > 1 ? 0.73f : 0.f) + (C == 16 ? 0.13f : 0.f) + (warps == 8 ? 0.21f : 0.f) +
-                          (float)((T + W - 1) >> lgW) * (stages == 1 ? 0.72f : 0.42f);
-        const float cost = N <= slots ? cta + 0.0021f * N : 1e6f + N / slots * cta + 0.0012f * N;
-        if (cost < least) {
-          least = cost;
+        if (C * warps > 2 * listed && C * warps > 8) continue;
+        const float x = cost(C, warps, stages, true);
+        if (x < least) {
+          least = x;
           best.C = C;
           best.warps = warps;
           best.stages = stages;
         }
       }
+  if (best.C && !p.mass && !p.mass_acc)
+    best.stages = cost(best.C, best.warps, 2, false) < cost(best.C, best.warps, 1, false) ? 2 : 1;
   return best;
 }
 
@@ -773,7 +879,11 @@ cudaError_t launch_attend_pages(const AttendPagesParams &base, const CUtensorMap
   p.C = f.C;
   p.stages = f.stages;
   p.warp_tiles = p.mass || p.mass_acc ? (p.top * (p.ps / TILE) + W - 1) / W : 0;
-  return f.warps == 8 ? launch_attend<8>(p, tmap, s) : launch_attend<4>(p, tmap, s);
+  p.columns = attend_columns(f.warps, p.warp_tiles);
+  auto launch = [&](auto eight, auto four) { return f.warps == 8 ? eight(p, tmap, s) : four(p, tmap, s); };
+  return f.C > 1         ? launch(launch_attend<8, false, false>, launch_attend<4, false, false>)
+         : p.warp_tiles  ? launch(launch_attend<8, true, true>, launch_attend<4, true, true>)
+                         : launch(launch_attend<8, true, false>, launch_attend<4, true, false>);
 }
 
 namespace {
