@@ -574,7 +574,10 @@ __global__ void __launch_bounds__(32 * NW)
         ahead &= ahead - 1;
       }
     }
-    if (!landed) break;
+    if (!landed) {                                   // the lists that are left have no tokens
+      for (int n = n0 + 32 + lane; masses && n < nt; n += 32) wsv[n] = 0;
+      break;
+    }
   }
   if (!landed) {                                     // what is in flight must land before the stages are reused
     for (; done < issued; ++done) wait_copy(bars + (done & (stages - 1)) * 8, done >> (stages - 1) & 1, DRAIN_LIMIT_NS);

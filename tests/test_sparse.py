@@ -260,6 +260,23 @@ def test_wait_limit_shorter_than_a_copy():
 
 
 @gpu
+def test_wait_limit_with_lists_of_many_tiles():
+    """A row that gives up early in a list of hundreds, most entries of which are no pages: its
+    masses go to tokens of the list only, and a new handle works."""
+    lengths = [6000] * 30 + [40, 17]
+    s = Loop(2, 16, 2, 16, lengths, seed=12)
+    s.c.sparse_enable(300)
+    s.c.debug_set(md.MD_DEBUG_SPIN_LIMIT_NS, 1000)
+    for _ in range(30):
+        s.step()
+        if s.c.sync() == md.MD_ERR_DEVICE_TIMEOUT:
+            break
+    t = Loop(2, 16, 2, 16, lengths, seed=12)
+    t.c.sparse_enable(300)
+    t.check("step", 300)
+
+
+@gpu
 def test_refusals_leave_the_handle_as_it_was():
     s = Loop(2, 16, 2, 16, [400], seed=9)
     for top, first, last in ((-1, 1, 1), (5000, 1, 1), (4, 1, 0), (4, -1, 1), (4, 3, 2), (4, 5, 1)):
