@@ -383,9 +383,9 @@ __device__ __forceinline__ void tm_load8(uint32_t at, float (&x)[8]) {
   for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(u[i]);
 }
 
-/* ONE: C is 1.  TM: scores are kept, in tensor memory.  A kernel with masses and one
- * without, as the SM starts no second CTA of a kernel with tm_alloc before the first has
- * got that far: with both in one kernel, calls without masses took up to 1.9 times as long. */
+/* ONE: C is 1.  TM: scores are kept, in tensor memory.  With and without masses are two
+ * kernels: in one, CTAs without masses, which never came to tm_alloc, ran as if there were
+ * one per SM, and their calls took up to 3 times as long. */
 template <int NW, bool ONE, bool TM>
 __global__ void __launch_bounds__(32 * NW)
     attend_pages_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ CUtensorMap tmap) {

@@ -310,6 +310,26 @@ def test_results_repeat_and_streams_are_kept():
 
 
 @gpu
+def test_launches_on_several_streams_at_once():
+    """Rows of one CTA each, with masses and without, in flight together."""
+    _need_gpu()
+    c = Case(4, 16, 2, 16, [3000] * 40, seed=14)
+    ids = _pick(c, 188, 15)
+    out, mass = c.attend(ids)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    torch.cuda.synchronize()
+    for i in range(12):
+        o = torch.empty_like(out)
+        m = torch.empty_like(mass) if i % 4 else None
+        got.append((o, m))
+        md.md_attend_pages(c.q, c.pool, c.bt, c.n, ids, o, mass=m, stream=streams[i % 3])
+    torch.cuda.synchronize()
+    for o, m in got:
+        assert torch.equal(o, out) and (m is None or torch.equal(m, mass))
+
+
+@gpu
 def test_calls_without_the_c_module_are_the_same(monkeypatch):
     _need_gpu()
     c = Case(2, 16, 2, 16, [700, 40, 0], seed=15)
