@@ -578,6 +578,8 @@ md_status md_attend_pages(const void *q_dev, const void *kv_pool_dev, const int3
  * its other pages, top_pages in all; steps of shorter sequences are unchanged.
  * top_pages = 0 turns it off.  last_pages >= 1: the page being written is always
  * attended.
+ * Queries that are not 16-byte aligned, and outputs that are not 8-byte aligned,
+ * go through the workspace, one more copy each.
  * The step's mass is that of the tokens attended: the others receive none, and
  * md_evict observes that.  Evicted pages are gone; pages that are not selected
  * stay, and any later step may select them.

@@ -963,8 +963,23 @@ md_status run_attention(md_ctx *c, int batch, int l0, int L, int q_layers, const
                         const void *k_new, const void *v_new, void *out_dev) {
   const md_config &cf = c->cfg;
   if (sparse_step(c, batch)) {
-    const md_status st = k_new ? append_step(c, batch, l0, L, k_new, v_new, nullptr, nullptr, 0) : MD_OK;
-    return st == MD_OK ? run_sparse(c, batch, l0, L, q_dev, out_dev) : st;
+    /* the page kernels read queries 16 bytes and write outputs 8 bytes at a time: rows
+     * at other addresses go through the workspace */
+    const size_t bytes = (size_t)batch * L * cf.num_q_heads * D * 2;
+    void *out = (uintptr_t)out_dev & 7 ? c->ws + c->lay.io_out : out_dev;
+    cudaError_t e = cudaSuccess;
+    if ((uintptr_t)q_dev & 15) {
+      e = cudaMemcpyAsync(c->ws + c->lay.io_q, q_dev, bytes, cudaMemcpyDeviceToDevice, c->stream);
+      q_dev = c->ws + c->lay.io_q;
+    }
+    if (e != cudaSuccess) return cuda_fail(c, e, "query copy");
+    md_status st = k_new ? append_step(c, batch, l0, L, k_new, v_new, nullptr, nullptr, 0) : MD_OK;
+    if (st == MD_OK) st = run_sparse(c, batch, l0, L, q_dev, out);
+    if (st == MD_OK && out != out_dev) {
+      e = cudaMemcpyAsync(out_dev, out, bytes, cudaMemcpyDeviceToDevice, c->stream);
+      if (e != cudaSuccess) return cuda_fail(c, e, "output copy");
+    }
+    return st;
   }
   AttnBase base;
   memset(&base, 0, sizeof(base));

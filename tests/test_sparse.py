@@ -277,6 +277,32 @@ def test_wait_limit_with_lists_of_many_tiles():
 
 
 @gpu
+@pytest.mark.parametrize("how", ["step", "layers"])
+def test_queries_and_outputs_at_any_address(how):
+    """Rows that start at any 2-byte address give the same bits, and nothing around the outputs
+    is written."""
+    want = None
+    for q_shift, out_shift in ((0, 0), (0, 1), (0, 2), (0, 4), (1, 0), (2, 4), (4, 3), (8, 8)):
+        s = Loop(2, 16, 2, 16, [700, 90, 1300], seed=16)
+        s.c.sparse_enable(9)
+        q, k, v = s.rand(3, 2, 16, D), s.rand(3, 2, 2, D), s.rand(3, 2, 2, D)
+        outs = []
+        for l in range(2) if how == "layers" else [slice(None)]:
+            x, kk, vv = (y[:, l].contiguous() for y in (q, k, v))
+            src = torch.zeros(x.numel() + 16, dtype=torch.bfloat16, device="cuda")
+            src[q_shift:q_shift + x.numel()] = x.flatten()
+            dst = torch.zeros(x.numel() + 16, dtype=torch.int16, device="cuda")
+            at = (src.data_ptr() + 2 * q_shift, kk, vv, [6] * 3, dst.data_ptr() + 2 * out_shift)
+            s.c.decode_layer(l, 3, *at) if how == "layers" else s.c.decode_step(3, *at)
+            assert s.c.sync() == md.MD_OK
+            assert not dst[:out_shift].any() and not dst[out_shift + x.numel():].any()
+            outs.append(dst[out_shift:out_shift + x.numel()])
+        outs = torch.cat(outs)
+        want = outs if want is None else want
+        assert torch.equal(outs, want) and outs.any()
+
+
+@gpu
 def test_refusals_leave_the_handle_as_it_was():
     s = Loop(2, 16, 2, 16, [400], seed=9)
     for top, first, last in ((-1, 1, 1), (5000, 1, 1), (4, 1, 0), (4, -1, 1), (4, 3, 2), (4, 5, 1)):
