@@ -336,7 +336,7 @@ def md_norm_rope(q, k, v, q_out, k_out, v_out, *, positions, table, q_weight=Non
         _bad(f"rows of {first.dtype}")
     if v is not None and (k is None or v.shape != k.shape):
         _bad("v must have k's shape")
-    a.n_tokens, a.type, a.eps, a.interleaved = T, types[first.dtype], eps, int(interleaved)
+    a.n_tokens, a.type, a.eps, a.interleaved = T, types[first.dtype], eps, int(bool(interleaved))
     a.num_q_heads = q.shape[1] if q is not None else 0
     a.num_kv_heads = k.shape[1] if k is not None else 0
     if q is not None and q_weight is not None:

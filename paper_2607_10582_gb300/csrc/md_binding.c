@@ -408,7 +408,8 @@ static PyObject *norm_rope(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   const double eps = PyFloat_AsDouble(a[10]);
   if (PyErr_Occurred() || !call_stream(x[first].device, a[13], &r.stream)) return leave();
   r.eps = (float)eps;
-  r.interleaved = a[12] != Py_False;
+  r.interleaved = PyObject_IsTrue(a[12]);
+  if (r.interleaved < 0) return leave();
   if (a[7] != Py_None) {
     if (!dense_tensor(a[7], &t) || t.type != T_F32 || t.dims != 3 || t.n[2] != 2 || t.n[0] > INT32_MAX ||
         t.n[1] > MD_HEAD_DIM / 2 || t.device != x[first].device)

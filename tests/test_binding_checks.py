@@ -1,0 +1,60 @@
+"""What the Python side of the row and page calls lets through, with stand-ins for device
+tensors and for the library: no GPU."""
+import types
+
+import numpy as np
+import pytest
+
+import paper_2607_10582_gb300 as md
+
+torch = pytest.importorskip("torch")
+D = 128
+
+
+class Stub:
+    """What the checks read of a device tensor."""
+
+    def __init__(self, *shape, dtype=torch.bfloat16, device=0):
+        self.t = torch.empty(shape, dtype=dtype, device="meta")
+        self.shape, self.dtype, self.device, self.is_cuda = self.t.shape, dtype, torch.device("cuda", device), True
+        self.dim, self.stride, self.numel = self.t.dim, self.t.stride, self.t.numel
+        self.element_size, self.is_contiguous = self.t.element_size, self.t.is_contiguous
+
+    def data_ptr(self):
+        return 1 << 20
+
+
+class Library:
+    """Records the calls that would be launched."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *a: self.calls.append((name, a)) or md.MD_OK
+
+
+@pytest.fixture
+def library(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(md, "lib", lambda: lib)
+    monkeypatch.setattr(md, "_torch_calls", md._NoCalls)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: types.SimpleNamespace(cuda_stream=0))
+    return lib
+
+
+def _rows(**kw):
+    i32, f32 = torch.int32, torch.float32
+    a = dict(q=Stub(4, 3, D), k=Stub(4, 2, D), v=Stub(4, 2, D), q_out=Stub(4, 3, D), k_out=Stub(4, 2, D), v_out=Stub(4, 2, D),
+             positions=Stub(4, dtype=i32), table=Stub(9, 64, 2, dtype=f32), q_weight=Stub(D, dtype=f32),
+             k_weight=Stub(D, dtype=f32))
+    a.update(kw)
+    rows = [a.pop(n) for n in ("q", "k", "v", "q_out", "k_out", "v_out")]
+    md.md_norm_rope(*rows, **a)
+
+
+@pytest.mark.parametrize("value", [False, 0, None, np.False_, True, 1, np.True_])
+def test_interleaved_is_taken_for_its_truth(library, value):
+    _rows(interleaved=value)
+    assert library.calls[0][1][0]._obj.interleaved == (1 if value else 0)

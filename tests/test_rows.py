@@ -198,6 +198,22 @@ def test_calls_without_the_c_module_are_the_same(monkeypatch):
 
 
 @gpu
+@pytest.mark.parametrize("value", [False, 0, None, np.False_, True, 1, np.True_])
+def test_interleaved_is_taken_for_its_truth(value, monkeypatch):
+    _need_gpu()
+    x = torch.randn((5, 4, D), device="cuda").bfloat16()
+    table, pos = md.md_rope_table(_freq(64), 50), torch.arange(5, dtype=torch.int32, device="cuda")
+    want = torch.empty_like(x)
+    md.md_norm_rope(x, None, None, want, None, None, positions=pos, table=table, interleaved=True if value else False)
+    for b in (md._binding(), md._NoCalls):
+        monkeypatch.setattr(md, "_torch_calls", None)
+        monkeypatch.setattr(md, "_fast", b)
+        got = torch.zeros_like(x)
+        md.md_norm_rope(x, None, None, got, None, None, positions=pos, table=table, interleaved=value)
+        assert torch.equal(got, want)
+
+
+@gpu
 def test_rows_on_another_stream():
     """The call goes to the stream it is given, behind the work that stream holds."""
     _need_gpu()
