@@ -324,8 +324,9 @@ def md_norm_rope(q, k, v, q_out, k_out, v_out, *, positions, table, q_weight=Non
             continue
         if x.dim() != 3 or x.shape[0] != T or x.shape[2] != MD_HEAD_DIM or x.dtype != first.dtype or not x.is_cuda:
             _bad(f"{name}: {T} tokens of heads of 128 elements, of {first.dtype}, expected")
-        if y is None or y.shape != x.shape or y.element_size() != 2 or not y.is_cuda:
-            _bad(f"{name}_out: bf16 of the shape of {name} expected")
+        if (y is None or y.shape != x.shape or str(y.dtype).split(".")[-1] not in ("bfloat16", "int16", "uint16")
+                or not y.is_cuda):
+            _bad(f"{name}_out: bf16 (or its raw bits) of the shape of {name} expected")
         if x.numel() and (x.stride(2) != 1 or y.stride(2) != 1):
             _bad(f"{name}: the elements of a row must be adjacent")
         setattr(a, name, x.data_ptr())

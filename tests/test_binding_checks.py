@@ -58,3 +58,20 @@ def _rows(**kw):
 def test_interleaved_is_taken_for_its_truth(library, value):
     _rows(interleaved=value)
     assert library.calls[0][1][0]._obj.interleaved == (1 if value else 0)
+
+
+@pytest.mark.parametrize("name", ["q_out", "k_out", "v_out"])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32, torch.int32, torch.uint8])
+def test_rows_are_written_as_bf16_only(library, name, dtype):
+    """An f16 tensor would receive bf16 bits."""
+    with pytest.raises(md.MemDecayError):
+        _rows(**{name: Stub(4, 3 if name == "q_out" else 2, D, dtype=dtype)})
+    assert not library.calls
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.int16, torch.uint16])
+def test_rows_are_written_as_bf16_or_its_bits(library, dtype):
+    f16 = torch.float16
+    _rows(q=Stub(4, 3, D, dtype=f16), k=Stub(4, 2, D, dtype=f16), v=Stub(4, 2, D, dtype=f16),
+          **{n: Stub(4, 3 if n == "q_out" else 2, D, dtype=dtype) for n in ("q_out", "k_out", "v_out")})
+    assert [c[0] for c in library.calls] == ["md_norm_rope"]
