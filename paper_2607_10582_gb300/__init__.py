@@ -247,13 +247,17 @@ def _bad(what: str):
     raise MemDecayError(MD_ERR_INVALID_ARG, what)
 
 
+def _here(name, t):
+    """Every tensor of a call lies on the current device."""
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        _bad(f"{name} on {t.device}: a tensor on the current device expected")
+
+
 def _on(t, stream):
     """The stream a call on tensor t goes to (default: the current one of its device)."""
     import torch
-    if not t.is_cuda:
-        _bad("device tensors expected")
-    if t.device.index != torch.cuda.current_device():
-        _bad(f"tensors on {t.device}, which is not the current device")
+    _here("rows or pages", t)
     return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
 
 
@@ -261,11 +265,10 @@ _KINDS = {"bf16": ("bfloat16", "int16"), "f32": ("float32",), "i32": ("int32",)}
 
 
 def _dense(name, t, shape, kind):
-    """Address of a contiguous device tensor of this shape and kind."""
-    if (tuple(t.shape) != tuple(shape) or str(t.dtype).split(".")[-1] not in _KINDS[kind] or not t.is_contiguous()
-            or not t.is_cuda):
-        _bad(f"{name}: a contiguous device tensor {tuple(shape)} of {kind} expected, "
-             f"not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    """Address of a contiguous tensor of this shape and kind on the current device."""
+    _here(name, t)
+    if tuple(t.shape) != tuple(shape) or str(t.dtype).split(".")[-1] not in _KINDS[kind] or not t.is_contiguous():
+        _bad(f"{name}: a contiguous tensor {tuple(shape)} of {kind} expected, not {tuple(t.shape)} of {t.dtype}")
     return t.data_ptr()
 
 
@@ -322,11 +325,12 @@ def md_norm_rope(q, k, v, q_out, k_out, v_out, *, positions, table, q_weight=Non
     for name, x, y in (("q", q, q_out), ("k", k, k_out), ("v", v, v_out)):
         if x is None:
             continue
-        if x.dim() != 3 or x.shape[0] != T or x.shape[2] != MD_HEAD_DIM or x.dtype != first.dtype or not x.is_cuda:
+        if x.dim() != 3 or x.shape[0] != T or x.shape[2] != MD_HEAD_DIM or x.dtype != first.dtype:
             _bad(f"{name}: {T} tokens of heads of 128 elements, of {first.dtype}, expected")
-        if (y is None or y.shape != x.shape or str(y.dtype).split(".")[-1] not in ("bfloat16", "int16", "uint16")
-                or not y.is_cuda):
+        if y is None or y.shape != x.shape or str(y.dtype).split(".")[-1] not in ("bfloat16", "int16", "uint16"):
             _bad(f"{name}_out: bf16 (or its raw bits) of the shape of {name} expected")
+        _here(name, x)
+        _here(name + "_out", y)
         if x.numel() and (x.stride(2) != 1 or y.stride(2) != 1):
             _bad(f"{name}: the elements of a row must be adjacent")
         setattr(a, name, x.data_ptr())

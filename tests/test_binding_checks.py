@@ -75,3 +75,49 @@ def test_rows_are_written_as_bf16_or_its_bits(library, dtype):
     _rows(q=Stub(4, 3, D, dtype=f16), k=Stub(4, 2, D, dtype=f16), v=Stub(4, 2, D, dtype=f16),
           **{n: Stub(4, 3 if n == "q_out" else 2, D, dtype=dtype) for n in ("q_out", "k_out", "v_out")})
     assert [c[0] for c in library.calls] == ["md_norm_rope"]
+
+
+def _pages(call, **kw):
+    """A call of one sequence, 2 layers, 4 pages of 16 tokens, 2 KV heads and 8 query heads."""
+    i32, f32 = torch.int32, torch.float32
+    a = dict(q=Stub(1, 2, 8, D), pool=Stub(2, 4, 2, 2, 16, D), bounds=Stub(2, 4, 2, 2, D), block_table=Stub(1, 4, dtype=i32),
+             scores=Stub(1, 2, 2, 4, dtype=f32), page_ids=Stub(1, 2, 2, 3, dtype=i32), out=Stub(1, 2, 8, D),
+             mass=Stub(1, 2, 2, 48, dtype=f32), n_tokens=[50])
+    a.update(kw)
+    names, keywords = CALLS[call]
+    getattr(md, call)(*(a[n] for n in names), **{n: a[n] if n in a else 16 for n in keywords})
+
+
+CALLS = {
+    "md_page_bounds": (("pool", "block_table", "n_tokens", "bounds"), ()),
+    "md_page_scores": (("q", "bounds", "block_table", "n_tokens", "scores"), ("page_size",)),
+    "md_page_top": (("scores", "n_tokens", "page_ids"), ("page_size",)),
+    "md_attend_pages": (("q", "pool", "block_table", "n_tokens", "page_ids", "out"), ("mass",)),
+}
+TENSORS = [(c, n) for c, (names, keywords) in CALLS.items() for n in names + keywords if n not in ("n_tokens", "page_size")]
+
+
+def _elsewhere(t):
+    return Stub(*t.shape, dtype=t.dtype, device=1)
+
+
+@pytest.mark.parametrize("call,name", TENSORS)
+def test_page_calls_take_tensors_of_one_device(library, call, name):
+    _pages(call)
+    assert [c[0] for c in library.calls] == [call]
+    like = dict(q=Stub(1, 2, 8, D), pool=Stub(2, 4, 2, 2, 16, D), bounds=Stub(2, 4, 2, 2, D),
+                block_table=Stub(1, 4, dtype=torch.int32), scores=Stub(1, 2, 2, 4, dtype=torch.float32),
+                page_ids=Stub(1, 2, 2, 3, dtype=torch.int32), out=Stub(1, 2, 8, D),
+                mass=Stub(1, 2, 2, 48, dtype=torch.float32))[name]
+    with pytest.raises(md.MemDecayError) as e:
+        _pages(call, **{name: _elsewhere(like)})
+    assert e.value.status == md.MD_ERR_INVALID_ARG and len(library.calls) == 1
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "q_out", "k_out", "v_out", "positions", "table", "q_weight", "k_weight"])
+def test_rows_take_tensors_of_one_device(library, name):
+    shape = dict(positions=(4,), table=(9, 64, 2), q_weight=(D,), k_weight=(D,), q=(4, 3, D), q_out=(4, 3, D))
+    dtype = dict(positions=torch.int32, table=torch.float32, q_weight=torch.float32, k_weight=torch.float32)
+    with pytest.raises(md.MemDecayError) as e:
+        _rows(**{name: Stub(*shape.get(name, (4, 2, D)), dtype=dtype.get(name, torch.bfloat16), device=1)})
+    assert e.value.status == md.MD_ERR_INVALID_ARG and not library.calls
