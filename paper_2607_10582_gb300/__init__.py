@@ -250,6 +250,8 @@ def _bad(what: str):
 def _here(name, t):
     """Every tensor of a call lies on the current device."""
     import torch
+    if t is None:
+        _bad(f"{name} is missing")
     if not t.is_cuda or t.device.index != torch.cuda.current_device():
         _bad(f"{name} on {t.device}: a tensor on the current device expected")
 
@@ -273,6 +275,8 @@ def _dense(name, t, shape, kind):
 
 
 def _dims(name, t, n):
+    if t is None:
+        _bad(f"{name} is missing")
     if t.dim() != n:
         _bad(f"{name}: {n} dimensions expected, not {t.dim()}")
     return t.shape
@@ -353,6 +357,7 @@ def md_norm_rope(q, k, v, q_out, k_out, v_out, *, positions, table, q_weight=Non
         _dims("table", table, 3)
         a.table = _dense("table", table, (table.shape[0], table.shape[1], 2), "f32")
         a.table_len, a.rotary_dim = table.shape[0], 2 * table.shape[1]
+        _here("positions", positions)
         a.num_axes = positions.shape[0] if positions.dim() == 2 else 1
         a.positions = _dense("positions", positions, (a.num_axes, T) if positions.dim() == 2 else (T,), "i32")
         if axes is not None:

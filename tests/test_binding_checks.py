@@ -121,3 +121,18 @@ def test_rows_take_tensors_of_one_device(library, name):
     with pytest.raises(md.MemDecayError) as e:
         _rows(**{name: Stub(*shape.get(name, (4, 2, D)), dtype=dtype.get(name, torch.bfloat16), device=1)})
     assert e.value.status == md.MD_ERR_INVALID_ARG and not library.calls
+
+
+@pytest.mark.parametrize("call,name", [x for x in TENSORS if x[1] != "mass"])
+def test_page_calls_say_which_tensor_is_missing(library, call, name):
+    with pytest.raises(md.MemDecayError) as e:
+        _pages(call, **{name: None})
+    assert e.value.status == md.MD_ERR_INVALID_ARG and name in str(e.value) and not library.calls
+
+
+def test_a_rotation_needs_positions(library):
+    with pytest.raises(md.MemDecayError) as e:
+        _rows(positions=None)
+    assert e.value.status == md.MD_ERR_INVALID_ARG and "positions" in str(e.value) and not library.calls
+    _rows(positions=None, table=None)
+    assert len(library.calls) == 1
