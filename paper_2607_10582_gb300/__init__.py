@@ -274,6 +274,19 @@ def _dense(name, t, shape, kind):
     return t.data_ptr()
 
 
+def _whole(name, arr, dtype):
+    """A host array of this type, each value as it was given."""
+    a = np.asarray(arr)
+    try:
+        with np.errstate(invalid="ignore"):
+            b = np.ascontiguousarray(a.astype(dtype))
+    except (OverflowError, TypeError, ValueError):
+        b = None
+    if b is None or not np.array_equal(a, b):
+        _bad(f"{name}: whole numbers of {np.dtype(dtype).name} expected")
+    return b, b.ctypes.data
+
+
 def _dims(name, t, n):
     if t is None:
         _bad(f"{name} is missing")
@@ -361,7 +374,7 @@ def md_norm_rope(q, k, v, q_out, k_out, v_out, *, positions, table, q_weight=Non
         a.num_axes = positions.shape[0] if positions.dim() == 2 else 1
         a.positions = _dense("positions", positions, (a.num_axes, T) if positions.dim() == 2 else (T,), "i32")
         if axes is not None:
-            host, a.axis_host = _host(axes, np.uint8)
+            host, a.axis_host = _whole("axes", axes, np.uint8)
             if host.size < table.shape[1]:
                 _bad(f"{host.size} axes for {table.shape[1]} pairs")
     a.stream = _on(first, stream)
@@ -369,7 +382,7 @@ def md_norm_rope(q, k, v, q_out, k_out, v_out, *, positions, table, q_weight=Non
 
 
 def _counts(n_tokens, batch: int):
-    n, p = _host(n_tokens, np.int32)
+    n, p = _whole("token counts or first pages", n_tokens, np.int32)
     if n.size < batch:
         _bad(f"{n.size} token counts for a batch of {batch}")
     return n, p

@@ -1,5 +1,6 @@
 """What the Python side of the row and page calls lets through, with stand-ins for device
 tensors and for the library: no GPU."""
+import math
 import types
 
 import numpy as np
@@ -135,4 +136,29 @@ def test_a_rotation_needs_positions(library):
         _rows(positions=None)
     assert e.value.status == md.MD_ERR_INVALID_ARG and "positions" in str(e.value) and not library.calls
     _rows(positions=None, table=None)
+    assert len(library.calls) == 1
+
+
+@pytest.mark.parametrize("counts", [np.array([(1 << 32) + 50]), np.array([50.5]), [50.5], np.array([math.nan]), [1 << 70]])
+@pytest.mark.parametrize("call", list(CALLS))
+def test_token_counts_are_taken_as_they_are(library, call, counts):
+    """A count that int32 does not hold is refused, not wrapped or cut."""
+    with pytest.raises(md.MemDecayError):
+        _pages(call, n_tokens=counts)
+    assert not library.calls
+
+
+@pytest.mark.parametrize("counts", [[50], (50,), np.array([50]), np.array([50, 9], np.int16), np.array([50.0]),
+                                    torch.tensor([50])])
+def test_token_counts_of_other_types_are_converted(library, counts):
+    _pages("md_page_top", n_tokens=counts)
+    assert len(library.calls) == 1
+
+
+@pytest.mark.parametrize("axes", [np.full(64, 256), np.full(64, -256), [0.5] * 64])
+def test_axes_are_taken_as_they_are(library, axes):
+    with pytest.raises(md.MemDecayError):
+        _rows(positions=Stub(2, 4, dtype=torch.int32), axes=axes)
+    assert not library.calls
+    _rows(positions=Stub(2, 4, dtype=torch.int32), axes=[0, 1] * 32)
     assert len(library.calls) == 1
