@@ -665,8 +665,9 @@ class Cache:
         if top_pages:
             n = int(lib().md_sparse_bytes(ctypes.byref(self.cfg), top_pages))
             if n:
-                buf = self.torch.empty(n + 256, dtype=self.torch.uint8, device=self.device)
-                buf.record_stream(self.stream)     # steps in flight may use it when it is given up
+                # on the handle's stream, the only one that uses it: taken and given up in its order
+                with self.torch.cuda.stream(self.stream):
+                    buf = self.torch.empty(n + 256, dtype=self.torch.uint8, device=self.device)
                 p = (buf.data_ptr() + 255) // 256 * 256
         self._check(lib().md_sparse_enable(self.h, top_pages, first_pages, last_pages, p, n))
         self.sparse_buffer = buf

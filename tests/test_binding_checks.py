@@ -1,5 +1,6 @@
 """What the Python side of the row and page calls lets through, with stand-ins for device
 tensors and for the library: no GPU."""
+import contextlib
 import math
 import types
 
@@ -162,3 +163,51 @@ def test_axes_are_taken_as_they_are(library, axes):
     assert not library.calls
     _rows(positions=Stub(2, 4, dtype=torch.int32), axes=[0, 1] * 32)
     assert len(library.calls) == 1
+
+
+class Streams:
+    """Stands in for torch: which stream is current when memory is taken, and what is ordered
+    behind what."""
+
+    uint8, float32 = torch.uint8, torch.float32
+
+    def __init__(self):
+        self.log, self.now, self.cuda = [], "current", self
+
+    @contextlib.contextmanager
+    def stream(self, s):
+        was, self.now = self.now, s
+        yield
+        self.now = was
+
+    def current_stream(self, *a):
+        return self.now
+
+    def current_device(self):
+        return 0
+
+    def empty(self, *a, **kw):
+        self.log.append(("taken", self.now))
+        return types.SimpleNamespace(data_ptr=lambda: 1 << 20, is_cuda=True, device=torch.device("cuda", 0),
+                                     record_stream=lambda s: self.log.append(("used", s)))
+
+
+class Stream:
+    cuda_stream = 77
+
+    def __init__(self, torch_):
+        self.torch = torch_
+
+    def wait_stream(self, s):
+        self.torch.log.append(("waits", s))
+
+
+def test_sparse_buffer_is_ordered_before_its_first_use(library):
+    """The allocator may give out a block that another stream's kernels still write: the handle's
+    stream, which uses the buffer, is the one it is taken on."""
+    c, t = object.__new__(md.Cache), Streams()
+    c.torch, c.stream, c.device, c.h, c.cfg = t, Stream(t), "cuda:0", None, md.md_config()
+    library.md_sparse_bytes = lambda *a: 1000
+    c.sparse_enable(4)
+    assert t.log[0] == ("taken", c.stream) or ("waits", "current") in t.log
+    assert library.calls[0][0] == "md_sparse_enable"

@@ -303,6 +303,31 @@ def test_queries_and_outputs_at_any_address(how):
 
 
 @gpu
+def test_enabled_from_another_stream_with_work_pending():
+    """A block that the current stream has given up, with writes to it pending, is no buffer of a
+    handle on another stream before those writes are done."""
+    if not torch.cuda.is_available():  # pragma: no cover
+        pytest.skip("needs a CUDA GPU")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        s = Loop(2, 16, 2, 16, [900, 400], seed=17, stream=side)
+    n = int(md.lib().md_sparse_bytes(ctypes.byref(s.c.cfg), 9)) + 256
+    old = torch.empty(n, dtype=torch.uint8, device="cuda")
+    big = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(100):
+        big.fill_(1)                               # some ms
+    old.fill_(0)
+    del old
+    s.c.sparse_enable(9)
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            s.check("step", 9)
+        torch.cuda.current_stream().wait_stream(torch.cuda.default_stream())
+        s.check("step", 9)
+
+
+@gpu
 def test_refusals_leave_the_handle_as_it_was():
     s = Loop(2, 16, 2, 16, [400], seed=9)
     for top, first, last in ((-1, 1, 1), (5000, 1, 1), (4, 1, 0), (4, -1, 1), (4, 3, 2), (4, 5, 1)):
