@@ -303,12 +303,16 @@ def _status(st: int, what: str):
 def md_rope_table(inv_freq, table_len: int, *, scale: float = 1.0, stream=None):
     """Table of a rotation, fp32 [table_len][rotary_dim / 2][2] on the current device:
     scale * (cos, sin) of pos * inv_freq[i], from 64-bit angles.  inv_freq: float64
-    [rotary_dim / 2] on the host."""
+    [rotary_dim / 2] on the host.  Written on `stream`, which waits for the current stream
+    (whose memory the table is); the current stream does not wait for it."""
     import torch
     f, p = _host(inv_freq, np.float64)
     if f.ndim != 1 or table_len < 1:
         _bad("inv_freq must have one dimension, table_len must be positive")
     out = torch.empty((table_len, f.size, 2), dtype=torch.float32, device="cuda")
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+        out.record_stream(stream)
     _status(lib().md_rope_table(p, 2 * f.size, table_len, scale, out.data_ptr(), _on(out, stream)), "md_rope_table")
     return out
 

@@ -2,6 +2,7 @@
 tensors and for the library: no GPU."""
 import contextlib
 import math
+import sys
 import types
 
 import numpy as np
@@ -211,3 +212,14 @@ def test_sparse_buffer_is_ordered_before_its_first_use(library):
     c.sparse_enable(4)
     assert t.log[0] == ("taken", c.stream) or ("waits", "current") in t.log
     assert library.calls[0][0] == "md_sparse_enable"
+
+
+def test_table_is_ordered_before_its_first_use(library, monkeypatch):
+    """A table written on a given stream: that stream waits for whoever had the memory, and the
+    memory is not given out again before that stream is done with it."""
+    t = Streams()
+    monkeypatch.setitem(sys.modules, "torch", t)
+    s = Stream(t)
+    md.md_rope_table(np.ones(64), 10, stream=s)
+    assert library.calls[0][0] == "md_rope_table" and library.calls[0][1][-1] == 77
+    assert ("taken", s) in t.log or (("waits", "current") in t.log and ("used", s) in t.log)

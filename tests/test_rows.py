@@ -232,6 +232,24 @@ def test_rows_on_another_stream():
     assert torch.equal(got, want)
 
 
+@gpu
+def test_table_on_another_stream_with_work_pending():
+    """Writes that the current stream still has to a block it gave up come before the table's."""
+    _need_gpu()
+    freq, s = _freq(64), torch.cuda.Stream()
+    want = md.md_rope_table(freq, 5000)
+    old = torch.empty_like(want)
+    big = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(100):
+        big.fill_(1)                               # some ms
+    old.fill_(7.0)
+    del old
+    got = md.md_rope_table(freq, 5000, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
 def _args(**kw):
     a = md.md_norm_rope_args()
     base = dict(n_tokens=4, num_q_heads=2, num_kv_heads=1, type=0, rotary_dim=128, num_axes=1, table_len=8, eps=1e-6,
