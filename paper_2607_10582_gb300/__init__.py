@@ -491,7 +491,9 @@ class Cache:
         need = md_workspace_size(c)
         if need == 0:
             raise MemDecayError(MD_ERR_INVALID_ARG, "invalid configuration")
-        self.workspace = torch.empty(need + 1024, dtype=torch.uint8, device=self.device)
+        # on the handle's stream, the only one that uses it: taken and given up in its order
+        with torch.cuda.stream(self.stream):
+            self.workspace = torch.empty(need + 1024, dtype=torch.uint8, device=self.device)
         base = self.workspace.data_ptr()
         aligned = (base + 1023) // 1024 * 1024
         c.workspace = aligned

@@ -223,3 +223,19 @@ def test_table_is_ordered_before_its_first_use(library, monkeypatch):
     md.md_rope_table(np.ones(64), 10, stream=s)
     assert library.calls[0][0] == "md_rope_table" and library.calls[0][1][-1] == 77
     assert ("taken", s) in t.log or (("waits", "current") in t.log and ("used", s) in t.log)
+
+
+def test_workspace_is_ordered_before_its_first_use(library, monkeypatch):
+    """The same for a handle's workspace."""
+    t = Streams()
+    for name in ("int32", "int64", "int16"):
+        setattr(t, name, getattr(torch, name))
+    t.device = lambda x: x
+    monkeypatch.setitem(sys.modules, "torch", t)
+    monkeypatch.setattr(md, "_fast", md._NoCalls)
+    library.md_workspace_size = lambda *a: 1000
+    s = Stream(t)
+    c = md.Cache(1, 1, 1, 16, 1, 4, 4, stream=s, device="cuda:0")
+    assert t.log[0] == ("taken", s) or ("waits", "current") in t.log
+    assert library.calls[0][0] == "md_create"
+    c.h = None
