@@ -551,8 +551,8 @@ md_status md_page_top(const float *scores_dev, const int32_t *n_tokens_host, int
 
 /* Attention over the cached tokens of the listed pages, for every layer and
  * query head, with md_decode_step's arithmetic but for the softmax weights, which
- * enter the product with V as two bf16 terms each (an infinite value may turn
- * NaN); entries outside a sequence's pages (-1) are skipped, and a row that lists
+ * enter the product with V as two bf16 terms each.  Infinite values of one sign make
+ * their channel infinite, whatever their tokens' weights; entries outside a sequence's pages (-1) are skipped, and a row that lists
  * no token yields zeros.  How a row is split over CTAs goes by the launch's shape:
  * calls of the same shape give the same bits, others may round differently.  The
  * kernel's waits for its own copies are bounded (2 s); a row that gives up is NaN.

@@ -938,6 +938,7 @@ md_status run_sparse(md_ctx *c, int batch, int l0, int L, const void *q_dev, voi
     AttendPagesParams ap;
     (PageSet &)ap = set;
     ap.q = (const uint16_t *)q_dev;
+    ap.pool = ptr<uint16_t>(c, c->lay.pool);
     ap.l0 = l0;
     ap.status = ptr<int>(c, c->lay.status);
     ap.limit_ns = c->spin_limit_ns;

@@ -303,6 +303,7 @@ struct PageTopParams {
 cudaError_t launch_page_top(const PageTopParams &p, cudaStream_t s);
 struct AttendPagesParams : PageSet {
   const uint16_t *q;
+  const uint16_t *pool;                  // of all layers, as the tensor map
   uint16_t *out;
   int l0;                                // first layer, in the tensor map
   int *status;                           // sticky device status words, or null

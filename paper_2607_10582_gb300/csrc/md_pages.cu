@@ -306,6 +306,9 @@ __global__ void __launch_bounds__(threads) page_top_kernel(const __grid_constant
  * score exceeds it by SLACK: most tiles then need no exchange between lanes and
  * no rescaling.
  *
+ * With an infinite value the terms' products cancel or are 0 times it, and the sum is NaN
+ * (infinite_sums).
+ *
  * The masses need the scores again with the final maxima and sums.  A row of one CTA
  * keeps them in tensor memory, four columns per tile in its warp's lanes: the shared
  * memory is left to the tiles, and up to four CTAs share an SM where their scores would
@@ -354,6 +357,35 @@ __device__ __noinline__ bool wait_copy(uint32_t bar, uint32_t parity, long long 
 
 /* The maxima against which weights are taken: 0 where nothing but -inf was seen. */
 __device__ __forceinline__ float max_base(float m) { return m == -INFINITY ? 0.f : m; }
+
+/* Sums over channels d .. d + 3 of V rows with finite weights, of which some came out
+ * NaN: infinite where the row's tokens have infinite values of one sign and no NaN, as
+ * every weight is above 0.  A pass over those channels, for such sums only. */
+__device__ __noinline__ float4 infinite_sums(const AttendParams &p, int row, int b, int l, int h, int d, float4 sums) {
+  uint32_t seen = 0;                                 // 4 bits per channel: inf, -inf, NaN
+  for (int e = 0; e < p.top; ++e) {
+    const int pg = p.ids[(size_t)row * p.top + e], phys = page_id(p, b, pg);
+    if (phys < 0) continue;
+    const int n = page_tokens(p, b, pg);
+    const uint16_t *v = p.pool + ((((size_t)(p.l0 + l) * p.P_phys + phys) * p.Hkv + h) * 2 + 1) * p.ps * D + d;
+    for (int i = 0; i < n; ++i) {
+      const uint2 w = *(const uint2 *)(v + i * D);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x = (k < 2 ? w.x : w.y) >> 16 * (k & 1);
+        if ((x & 0x7f80u) == 0x7f80u) seen |= (x & 0x7fu ? 4u : x & 0x8000u ? 2u : 1u) << 4 * k;
+      }
+    }
+  }
+  float *s = &sums.x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t x = seen >> 4 * k & 7u;
+    if (s[k] != s[k] && (x == 1u || x == 2u)) s[k] = x == 1u ? INFINITY : -INFINITY;
+  }
+  return sums;
+}
+__device__ __forceinline__ bool any_nan(float4 x) { return isnan(x.x + x.y) || isnan(x.z + x.w); }
 
 /* ---- tensor memory ---- */
 __device__ __forceinline__ void tm_alloc(uint32_t smem, int columns) {      // a whole warp
@@ -632,6 +664,7 @@ __global__ void __launch_bounds__(32 * NW)
     for (int i = 0; i < GP / NW; ++i) {
       const int head = warp + i * NW;
       const float r = inverse(sum[i]);
+      if (any_nan(acc[i]) && r > 0.f) acc[i] = infinite_sums(p, row, b, l, h, 4 * lane, acc[i]);
       if (head < p.G)
         *(uint2 *)(p.out + (q_row + head) * D + 4 * lane) =
             make_uint2(pack_bf16(acc[i].x * r, acc[i].y * r), pack_bf16(acc[i].z * r, acc[i].w * r));
@@ -674,6 +707,7 @@ __global__ void __launch_bounds__(32 * NW)
         y.z += f * x.z;
         y.w += f * x.w;
       }
+      if (any_nan(y) && r > 0.f) y = infinite_sums(p, row, b, l, h, at_e - head * D, y);
       if (head < p.G)
         *(uint2 *)(p.out + q_row * D + at_e) =
             make_uint2(pack_bf16(y.x * r, y.y * r), pack_bf16(y.z * r, y.w * r));
@@ -1010,6 +1044,7 @@ MD_API md_status md_attend_pages(const void *q, const void *pool, const int32_t 
                 num_phys_pages))
     return MD_ERR_INVALID_ARG;
   p.q = (const uint16_t *)q;
+  p.pool = (const uint16_t *)pool;
   p.out = (uint16_t *)out;
   p.ids = page_ids;
   p.mass = mass;

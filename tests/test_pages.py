@@ -292,6 +292,51 @@ def test_infinite_and_nan_tokens_stay_in_their_heads():
 
 
 @gpu
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+@pytest.mark.parametrize("ps,lengths,top", [(16, [200], 13), (32, [3000] * 40, 60), (16, [700, 3001], 188), (16, [7], 1)])
+def test_infinite_values_stay_infinite(ps, lengths, top, value):
+    """An infinite value makes its channel infinite in the heads that attend it, as in the
+    formula: in a full tile, and in the last token of a partly filled one."""
+    _need_gpu()
+    c = Case(2, 16, 2, ps, lengths, seed=21)
+    b, n = len(lengths) - 1, lengths[-1]
+    for tok, ch in ((n - 1, 5), (min(n - 1, 3 * ps + 2), 77)):
+        c.pool[0, c.table[b, tok // ps], 1, 1, tok % ps, ch] = value
+    ids = torch.full((c.B, 2, 2, top), -1, dtype=torch.int32)
+    for i in range(c.B):
+        keep = sorted(({3, c.pages[i] - 1} | set(range(min(top - 2, c.pages[i])))) & set(range(c.pages[i])))
+        ids[i, :, :, :len(keep)] = torch.tensor(keep, dtype=torch.int32)
+    out, mass = c.attend(ids.cuda())
+    want = torch.zeros_like(out, dtype=torch.bool)
+    want[b, 0, 8:, 5] = want[b, 0, 8:, 77] = True
+    assert torch.equal(out == value, want) and not out.isnan().any() and not mass.isnan().any()
+
+
+@gpu
+@pytest.mark.parametrize("lengths,top", [([900], 57), ([900] * 40, 57)])
+def test_infinite_values_of_any_weight_and_sign(lengths, top):
+    """A weight far below what 32 bits hold is above 0 all the same; values of both signs, or
+    a NaN, make their channel NaN; tokens that are not listed are not looked at."""
+    _need_gpu()
+    c = Case(1, 16, 2, 16, lengths, seed=22, scale=300.0)
+    clean = c.pool.clone()
+    at = [c.table[0, i // 16] for i in range(900)]
+    for tok, ch, x in ((40, 3, math.inf), (300, 3, math.inf), (500, 60, -math.inf), (17, 90, math.inf), (899, 90, -math.inf),
+                       (700, 127, math.nan), (701, 126, math.inf), (320, 30, math.inf)):
+        c.pool[0, at[tok], 0, 1, tok % 16, ch] = x
+    ids = torch.arange(top, dtype=torch.int32, device="cuda").repeat(c.B, 1, 2, 1)
+    ids[..., 20] = -1                                   # the page of token 320
+    out, mass = c.attend(ids)
+    c.pool = clean
+    want, same = c.attend(ids)
+    want[0, 0, :8, 3], want[0, 0, :8, 60], want[0, 0, :8, 126] = math.inf, -math.inf, math.inf
+    for ch in (90, 127):
+        assert out[0, 0, :8, ch].isnan().all()
+        out[0, 0, :8, ch] = want[0, 0, :8, ch] = 0.0
+    assert torch.equal(out, want) and torch.equal(mass, same)
+
+
+@gpu
 def test_results_repeat_and_streams_are_kept():
     _need_gpu()
     c = Case(2, 16, 2, 32, [9000, 40, 2500], seed=11)

@@ -328,6 +328,24 @@ def test_enabled_from_another_stream_with_work_pending():
 
 
 @gpu
+def test_infinite_values_stay_infinite():
+    """As in the step over all pages."""
+    outs = []
+    for top in (0, 12):
+        s = Loop(2, 16, 2, 16, [190], seed=18)
+        s.c.sparse_enable(top, 1, 2)                         # the infinity's page is the last but one
+        q, k, v = s.rand(1, 2, 16, D), s.rand(1, 2, 2, D), s.rand(1, 2, 2, D)
+        v[0, 1, 0, 9] = math.inf
+        s.step(q=q, kv=(k, v))
+        s.step(q=q, kv=(k, torch.zeros_like(v)))
+        s.step(q=q, kv=(k, torch.zeros_like(v)))             # the 193rd token: a 13th page
+        outs.append(s.step(q=q, kv=(k, torch.zeros_like(v)))[1])
+    want = torch.zeros_like(outs[0], dtype=torch.bool)
+    want[0, 1, :8, 9] = True
+    assert s.pages() == [13] and all(torch.equal(o.isinf(), want) and not o.isnan().any() for o in outs)
+
+
+@gpu
 def test_refusals_leave_the_handle_as_it_was():
     s = Loop(2, 16, 2, 16, [400], seed=9)
     for top, first, last in ((-1, 1, 1), (5000, 1, 1), (4, 1, 0), (4, -1, 1), (4, 3, 2), (4, 5, 1)):
