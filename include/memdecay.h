@@ -530,7 +530,8 @@ md_status md_page_bounds(const void *kv_pool_dev, const int32_t *block_table_dev
 /* scores[b][l][kvh][p] = max over the KV head's query heads h of
  *   sum_d (max(q_hd, 0) hi_pd + min(q_hd, 0) lo_pd) / sqrt(128)
  * for the sequence's pages p: at least the logit of any of these heads on any
- * of the page's tokens.  Entries past a sequence's pages are not written.
+ * of the page's tokens, up to the rounding of a 32-bit sum; -inf for a page without
+ * tokens.  Entries past a sequence's pages are not written.
  *   q_dev       bf16 [batch][L][Hq][128]             (16-byte aligned)
  *   scores_dev  fp32 [batch][L][Hkv][max_pages_per_seq] (written) */
 md_status md_page_scores(const void *q_dev, const void *bounds_dev, const int32_t *block_table_dev,

@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(256, 4) page_scores_kernel(const __grid_consta
   const int i0 = page_id(p, b, p0), i1 = page_id(p, b, p1);
   const uint4 *s0 = (const uint4 *)(p.bounds + (((size_t)l * p.P_phys + (i0 < 0 ? 0 : i0)) * p.Hkv + h) * 2 * D) + t;
   const uint4 *s1 = (const uint4 *)(p.bounds + (((size_t)l * p.P_phys + (i1 < 0 ? 0 : i1)) * p.Hkv + h) * 2 * D) + t;
-  const uint4 none = make_uint4(0, 0, 0, 0);
+  const uint32_t nan2 = 0x7FFF7FFFu;             // a page without tokens: told from a NaN key at the end
+  const uint4 none = make_uint4(nan2, nan2, nan2, nan2);
   uint4 x[8], y[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {                // 0..3: lo, 4..7: hi
@@ -160,8 +161,8 @@ __global__ void __launch_bounds__(256, 4) page_scores_kernel(const __grid_consta
     m1 = top(m1, __shfl_xor_sync(0xffffffffu, m1, o));
   }
   float *dst = p.scores + (size_t)row * p.P_max;
-  if (t == 0 && p0 < P) dst[p0] = m0 * p.scale;
-  if (t == 0 && p1 < P) dst[p1] = m1 * p.scale;
+  if (t == 0 && p0 < P) dst[p0] = m0 == m0 || page_id(p, b, p0) >= 0 ? m0 * p.scale : -INFINITY;
+  if (t == 0 && p1 < P) dst[p1] = m1 == m1 || page_id(p, b, p1) >= 0 ? m1 * p.scale : -INFINITY;
 }
 
 /* ---------------------------------------------------------------- top --- */

@@ -244,6 +244,28 @@ def test_lists_with_holes_and_tables_with_strangers(ps, lengths, top):
 
 
 @gpu
+def test_pages_outside_the_pool_are_selected_last():
+    """A table entry outside the pool is a page without tokens: no page of scores below 0 gives
+    way to it, whatever the queries."""
+    _need_gpu()
+    c = Case(2, 16, 2, 16, [500, 333], seed=23)
+    c.pool[:, :, :, 0] = -(c.pool[:, :, :, 0].abs())
+    c.q = c.q.abs()
+    c.q[1, 0, 0, 0] = math.inf
+    bounds = c.bounds()
+    for b, pg, entry in ((0, 4, c.P), (0, 18, -1), (1, 1, 1 << 30), (1, 16, -(1 << 31))):
+        c.table[b, pg] = entry
+    c.bt = torch.from_numpy(c.table).cuda()
+    scores = torch.zeros((2, 2, 2, c.W), device="cuda")
+    md.md_page_scores(c.q, bounds, c.bt, c.n, scores, page_size=16)
+    assert (scores[0][..., [4, 18]] == -math.inf).all() and (scores[1][..., [1, 16]] == -math.inf).all()
+    assert (scores[0, :, :, [0, 1, 2, 3, 5, 31]] < 0).all() and (scores[0, :, :, 5] > -math.inf).all()
+    ids = torch.zeros((2, 2, 2, 19), dtype=torch.int32, device="cuda")
+    md.md_page_top(scores, c.n, ids, page_size=16, first=0, last=0)
+    assert not (ids[0] == 4).any() and not (ids[0] == 18).any() and not (ids[1] == 1).any() and not (ids[1] == 16).any()
+
+
+@gpu
 @pytest.mark.parametrize("scale", [0.0, 30.0, 300.0])
 def test_flat_and_steep_softmax(scale):
     """Equal logits, and logits of hundreds, where the weights round to one token."""
