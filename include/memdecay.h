@@ -329,7 +329,11 @@ md_status md_profile_read(md_ctx *ctx, double *ms_per_stage, int64_t *launches_p
  *                             of C CTAs (1, 2, 4, 8 or 16) of W warps (4 or 8)
  *                             per item, scores in shared memory (S = 0) or in
  *                             scratch (1).  A step that cannot take the form
- *                             fails with MD_ERR_CUDA. */
+ *                             fails with MD_ERR_CUDA.
+ *   MD_DEBUG_LOST_TILE        -1 (default), or a tile that each warp of the
+ *                             attention over selected pages takes for one whose
+ *                             copy did not land in time (counted per warp from
+ *                             0; the step then reports MD_ERR_DEVICE_TIMEOUT) */
 enum {
   MD_DEBUG_SPIN_LIMIT_NS = 0,
   MD_DEBUG_EXTRA_ARRIVALS = 1,
@@ -338,7 +342,8 @@ enum {
   MD_DEBUG_FORCE_CHUNKS = 4,
   MD_DEBUG_COMBINE_OVERHEAD = 5,
   MD_DEBUG_ZERO_COPY = 6,
-  MD_DEBUG_CLUSTER_FORM = 7
+  MD_DEBUG_CLUSTER_FORM = 7,
+  MD_DEBUG_LOST_TILE = 8
 };
 md_status md_debug_set(md_ctx *ctx, int key, int64_t value);
 

@@ -51,7 +51,8 @@ MD_MAX_TOP_TOKENS = 65536
 (MD_QUERY_TOKENS, MD_QUERY_PAGES, MD_QUERY_FREE_TOP, MD_QUERY_STEP, MD_QUERY_WINDOW,
  MD_QUERY_PINNED_PAGES) = range(6)
 (MD_DEBUG_SPIN_LIMIT_NS, MD_DEBUG_EXTRA_ARRIVALS, MD_DEBUG_GRID_LIMIT, MD_DEBUG_UNIT_OVERHEAD,
- MD_DEBUG_FORCE_CHUNKS, MD_DEBUG_COMBINE_OVERHEAD, MD_DEBUG_ZERO_COPY, MD_DEBUG_CLUSTER_FORM) = range(8)
+ MD_DEBUG_FORCE_CHUNKS, MD_DEBUG_COMBINE_OVERHEAD, MD_DEBUG_ZERO_COPY, MD_DEBUG_CLUSTER_FORM,
+ MD_DEBUG_LOST_TILE) = range(9)
 STAGES = ("append", "attention", "fold", "score", "select")
 
 

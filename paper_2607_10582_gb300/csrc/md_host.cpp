@@ -70,6 +70,7 @@ struct md_ctx {
   int combine_overhead_kib = 192;   // planner: cost of a split into several chunks per item
   int force_chunks = 0;      // planner: 0 = choose
   int cluster_form = 0;      // MD_DEBUG_CLUSTER_FORM: 0 = by cost
+  int lost_tile = -1;        // MD_DEBUG_LOST_TILE: -1 = none
   /* the planner's last choice of pages per chunk, reused while its inputs
    * (batch, layers, knobs, pages per sequence) repeat */
   std::vector<int> plan_pages;
@@ -942,6 +943,7 @@ md_status run_sparse(md_ctx *c, int batch, int l0, int L, const void *q_dev, voi
     ap.l0 = l0;
     ap.status = ptr<int>(c, c->lay.status);
     ap.limit_ns = c->spin_limit_ns;
+    ap.lost_tile = c->lost_tile;
     ap.out = (uint16_t *)out_dev;
     ap.ids = tp.ids;
     ap.mass = nullptr;
@@ -1656,6 +1658,11 @@ MD_API md_status md_debug_set(md_ctx *c, int key, int64_t value) {
     if (value != 0 && (C < 1 || C > MAX_CLUSTER || (C & (C - 1)) || (warps != 4 && warps != 8) || spill < 0 || spill > 1))
       return fail(c, MD_ERR_INVALID_ARG, "unknown cluster form");
     c->cluster_form = (int)value;
+    return MD_OK;
+  }
+  if (key == MD_DEBUG_LOST_TILE) {
+    if (value < -1 || value > MD_MAX_TOP_TOKENS) return fail(c, MD_ERR_INVALID_ARG, "lost tile out of range");
+    c->lost_tile = (int)value;
     return MD_OK;
   }
   if (key == MD_DEBUG_COMBINE_OVERHEAD) {

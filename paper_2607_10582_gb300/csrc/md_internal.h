@@ -308,6 +308,7 @@ struct AttendPagesParams : PageSet {
   int l0;                                // first layer, in the tensor map
   int *status;                           // sticky device status words, or null
   long long limit_ns;                    // of the wait for a copy
+  int lost_tile;                         // of a warp, taken for one that did not land; -1: none
   const int32_t *ids;                    // [n_seqs][L][Hkv][top]
   float *mass;                           // [n_seqs][L][Hkv][top][ps], or null
   unsigned long long *mass_acc;          // [slots] fixed-point mass of the step, or null

@@ -527,7 +527,7 @@ __global__ void __launch_bounds__(32 * NW)
       const int n = __ffs(todo) - 1, have = __shfl_sync(0xffffffffu, valid, n);
       const int stage = done & (stages - 1);       // stages: 1 or 2
       const uint32_t st = ring + stage * TILE_BYTES, bar = bars + stage * 8, parity = done >> (stages - 1) & 1;
-      landed = mbar_try_wait(bar, parity) || wait_copy(bar, parity, p.limit_ns);
+      landed = done != p.lost_tile && (mbar_try_wait(bar, parity) || wait_copy(bar, parity, p.limit_ns));
       if (!__all_sync(0xffffffffu, landed)) {
         landed = false;
         break;
@@ -1055,6 +1055,7 @@ MD_API md_status md_attend_pages(const void *q, const void *pool, const int32_t 
   p.l0 = 0;
   p.status = nullptr;
   p.limit_ns = 2000000000LL;
+  p.lost_tile = -1;
   void *encode = tile_encoder();
   CUtensorMap tmap;
   const size_t rows = (size_t)num_layers * num_phys_pages * num_kv_heads * 2 * page_size;

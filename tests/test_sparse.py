@@ -346,6 +346,49 @@ def test_infinite_values_stay_infinite():
 
 
 @gpu
+@pytest.mark.parametrize("lengths,top,tile", [
+    ([3000, 500], 40, 0),                          # clusters of CTAs over a row
+    ([6000] * 30 + [40, 17], 300, 0),              # one CTA per row, scores in tensor memory; lists of hundreds,
+    ([6000] * 30 + [40, 17], 300, 5),              # of the last two sequences' most entries are no pages
+    ([6000] * 30 + [40, 17], 300, 33),             # in the second list of 32
+])
+def test_a_row_that_gives_up(lengths, top, tile):
+    """A copy taken for one that did not land: the step reports it, the row's outputs are NaN and
+    the others' are not, no state but the mass of the listed tokens is written, and a new handle
+    works."""
+    s = Loop(2, 16, 2, 16, lengths, seed=19)
+    s.c.sparse_enable(top)
+    s.step()
+    assert s.c.evict(np.array(s.pages(), np.int32))[0] == md.MD_OK and s.c.sync() == md.MD_OK
+    # the new tokens' own slots start with the step
+    state = {w: s.c.get_state(w).clone() for w in (md.MD_STATE_TOKEN_PRIO, md.MD_STATE_WINDOW, md.MD_STATE_AHAT)}
+    n = s.tokens()
+    s.c.debug_set(md.MD_DEBUG_LOST_TILE, tile)
+    q, out = s.step()
+    assert s.c.sync() == md.MD_ERR_DEVICE_TIMEOUT
+    with pytest.raises(md.MemDecayError):
+        s.step()
+    want, acc = s.by_page_calls(q, top, 1, 1, False)
+    nan = out.isnan()
+    gone = nan.all(-1)
+    assert torch.equal(gone, nan.any(-1)) and torch.equal(torch.where(nan, 0, out), torch.where(nan, 0, want))
+    short = [b for b, x in enumerate(lengths) if x < 100]
+    assert gone.all() if tile == 0 else gone.any() and not gone[short].any()
+    mass = s.c.get_state(md.MD_STATE_MASS)
+    listed = acc > 0
+    assert not mass[~listed].any()
+    table = s.c.get_state(md.MD_STATE_BLOCK_TABLE)
+    new = torch.tensor([int(table[b, x // 16]) * 16 + x % 16 for b, x in enumerate(n)], device="cuda")
+    for w, before in state.items():
+        now = s.c.get_state(w)
+        now[new] = before[new]
+        assert torch.equal(now.view(torch.int32), before.view(torch.int32)), w
+    t = Loop(2, 16, 2, 16, lengths, seed=19)
+    t.c.sparse_enable(top)
+    t.check("step", top)
+
+
+@gpu
 def test_refusals_leave_the_handle_as_it_was():
     s = Loop(2, 16, 2, 16, [400], seed=9)
     for top, first, last in ((-1, 1, 1), (5000, 1, 1), (4, 1, 0), (4, -1, 1), (4, 3, 2), (4, 5, 1)):
