@@ -144,7 +144,7 @@ md_status md_set_region_params(md_ctx *ctx, int region, float base_priority,
  *   regions_host      [n] region label per token (host memory)
  *   insert_steps_host [n] insertion step per token (host), each <= the current
  *                     step; NULL means the current step for all
- *   k_dev, v_dev      bf16 [L][Hkv][n][D] (device)
+ *   k_dev, v_dev      bf16 [L][Hkv][n][D] (device, 16-byte aligned)
  * Each token starts with a_i = 0 and t_ref_i = its insertion step.  New pages
  * are taken from the free stack. */
 md_status md_append_tokens(md_ctx *ctx, int seq, int n_tokens, const uint8_t *regions_host,
@@ -161,6 +161,8 @@ md_status md_append_tokens(md_ctx *ctx, int seq, int n_tokens, const uint8_t *re
  *   k_new_dev, v_new_dev bf16 [batch][L][Hkv][D]  (device)
  *   new_region_host     [batch]                   (host)
  *   out_dev             bf16 [batch][L][Hq][D]    (device, written)
+ * The rows may lie at any 2-byte address; inputs that are not 16-byte aligned may
+ * take a copy through the workspace.
  * All steps of one observation window must use the same batch. */
 md_status md_decode_step(md_ctx *ctx, int batch, const void *q_dev, const void *k_new_dev,
                          const void *v_new_dev, const uint8_t *new_region_host, void *out_dev);
@@ -405,7 +407,7 @@ md_status md_calib_fit(const double *mass_sum, const int64_t *count, int n_bucke
  *   block_table_dev  int32 [batch][max_pages_per_seq] physical page ids
  *   n_tokens_host    [batch] cached tokens per sequence (host), each >= 1 and
  *                    at most max_pages_per_seq * page_size
- *   q_dev            bf16 [batch][L][Hq][128]
+ *   q_dev            bf16 [batch][L][Hq][128] (16-byte aligned)
  *   out_dev          bf16 [batch][L][Hq][128] (written)
  *   mass_dev         fp32 [L*Hkv][num_phys_pages*page_size] (written at the
  *                    slots of cached tokens: sum over the KV head's query heads
@@ -584,8 +586,7 @@ md_status md_attend_pages(const void *q_dev, const void *kv_pool_dev, const int3
  * its other pages, top_pages in all; steps of shorter sequences are unchanged.
  * top_pages = 0 turns it off.  last_pages >= 1: the page being written is always
  * attended.
- * Queries that are not 16-byte aligned, and outputs that are not 8-byte aligned,
- * go through the workspace, one more copy each.
+ * Outputs that are not 8-byte aligned go through the workspace, one more copy.
  * The step's mass is that of the tokens attended: the others receive none, and
  * md_evict observes that.  Evicted pages are gone; pages that are not selected
  * stay, and any later step may select them.

@@ -1185,6 +1185,7 @@ extern "C" __attribute__((visibility("default"))) md_status md_attend_mass_noall
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e;
   const ClusterPlan plan = cluster_plan(ap, 0);
+  if ((uintptr_t)q_dev & (plan.C > 0 ? 3 : 15)) return MD_ERR_INVALID_ARG;   // words, bulk copies
   if (plan.C > 0) {   // needs no scratch: nothing of the array is touched
     if (!encode_tile_map(encode, &tmap, (void *)kv_pool_dev, rows, ps)) return MD_ERR_INVALID_ARG;
     e = launch_cluster(ap, plan, false, nullptr, tmap, st);

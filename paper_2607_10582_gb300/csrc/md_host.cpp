@@ -669,6 +669,7 @@ MD_API md_status md_append_tokens(md_ctx *c, int seq, int n, const uint8_t *regi
   if (n < 0) return fail(c, MD_ERR_INVALID_ARG, "negative token count");
   if (n == 0) return MD_OK;
   if (!regions_host || !k_dev || !v_dev) return fail(c, MD_ERR_INVALID_ARG, "null pointer");
+  if (((uintptr_t)k_dev | (uintptr_t)v_dev) & 15) return fail(c, MD_ERR_INVALID_ARG, "K/V rows not 16-byte aligned");
   for (int i = 0; i < n; ++i)
     if (!valid_region(regions_host[i])) return fail(c, MD_ERR_INVALID_ARG, "bad region label");
   if (steps_host)
@@ -959,27 +960,38 @@ md_status run_sparse(md_ctx *c, int batch, int l0, int L, const void *q_dev, voi
   return MD_OK;
 }
 
+/* Device rows that a kernel reads `align` bytes at a time: where the caller's lie at
+ * another address, their copy at `off` in the workspace. */
+cudaError_t align_rows(md_ctx *c, const void **rows, size_t off, size_t bytes, uintptr_t align) {
+  if (((uintptr_t)*rows & (align - 1)) == 0) return cudaSuccess;
+  void *copy = c->ws + off;
+  const cudaError_t e = cudaMemcpyAsync(copy, *rows, bytes, cudaMemcpyDefault, c->stream);
+  *rows = copy;
+  return e;
+}
+
 /* Stage 1 over layers [l0, l0 + L); q/out hold q_layers layers.  With k_new
  * the step's new tokens are appended too (device rows [batch][L][Hkv][D]), by
  * the attention launch or by one ahead of it. */
 md_status run_attention(md_ctx *c, int batch, int l0, int L, int q_layers, const void *q_dev,
                         const void *k_new, const void *v_new, void *out_dev) {
   const md_config &cf = c->cfg;
+  const size_t bytes = (size_t)batch * L * cf.num_q_heads * D * 2, kv_bytes = (size_t)batch * L * cf.num_kv_heads * D * 2;
+  cudaError_t e;
+  if (k_new) {
+    e = align_rows(c, &k_new, c->lay.io_k, kv_bytes, 16);
+    if (e == cudaSuccess) e = align_rows(c, &v_new, c->lay.io_v, kv_bytes, 16);
+    if (e != cudaSuccess) return cuda_fail(c, e, "K/V copy");
+  }
   if (sparse_step(c, batch)) {
-    /* the page kernels read queries 16 bytes and write outputs 8 bytes at a time: rows
-     * at other addresses go through the workspace */
-    const size_t bytes = (size_t)batch * L * cf.num_q_heads * D * 2;
+    /* the page kernels read queries 16 bytes and write outputs 8 bytes at a time */
     void *out = (uintptr_t)out_dev & 7 ? c->ws + c->lay.io_out : out_dev;
-    cudaError_t e = cudaSuccess;
-    if ((uintptr_t)q_dev & 15) {
-      e = cudaMemcpyAsync(c->ws + c->lay.io_q, q_dev, bytes, cudaMemcpyDeviceToDevice, c->stream);
-      q_dev = c->ws + c->lay.io_q;
-    }
+    e = align_rows(c, &q_dev, c->lay.io_q, bytes, 16);
     if (e != cudaSuccess) return cuda_fail(c, e, "query copy");
     md_status st = k_new ? append_step(c, batch, l0, L, k_new, v_new, nullptr, nullptr, 0) : MD_OK;
     if (st == MD_OK) st = run_sparse(c, batch, l0, L, q_dev, out);
     if (st == MD_OK && out != out_dev) {
-      e = cudaMemcpyAsync(out_dev, out, bytes, cudaMemcpyDeviceToDevice, c->stream);
+      e = cudaMemcpyAsync(out_dev, out, bytes, cudaMemcpyDefault, c->stream);
       if (e != cudaSuccess) return cuda_fail(c, e, "output copy");
     }
     return st;
@@ -1044,8 +1056,10 @@ md_status run_attention(md_ctx *c, int batch, int l0, int L, int q_layers, const
                            : form ? cluster_form(base, scratch, form & 255, (form >> 8) & 255, form >> 16)
                                   : cluster_plan(base, scratch);
   if (form && plan.C == 0) return cuda_fail(c, cudaErrorInvalidConfiguration, "cluster form");
+  e = align_rows(c, &q_dev, c->lay.io_q, bytes, plan.C > 0 ? 4 : 16);   // words by the cluster kernel, bulk copies
+  if (e != cudaSuccess) return cuda_fail(c, e, "query copy");
+  base.q = (const uint16_t *)q_dev;
   cudaEvent_t e0;
-  cudaError_t e;
   if (plan.C > 0) {
     prof_begin(c, &e0);
     e = launch_cluster(base, plan, k_new && l0 > 0, ptr<float>(c, c->lay.scratch), c->tmap_tile, c->stream);

@@ -563,6 +563,52 @@ def test_output_at_any_address(n):
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
 
 
+@pytest.mark.parametrize("kernel", ["cluster", "persistent", "append apart"])
+@pytest.mark.parametrize("how", ["step", "layers"])
+def test_inputs_at_any_address(kernel, how):
+    """Queries and new rows that start at any 2-byte address: the same bits."""
+    L, Hq, Hkv, B = 2, 16, 2, 3
+    rng = np.random.default_rng(61)
+    want = None
+    x = [to_dev(t) for t in (synth.q_host(61, B, L, Hq, Hkv, 1), *synth.step_kv_host(61, [70, 301, 16], [6] * B, L, Hkv))]
+    lab = [np.sort(rng.integers(0, 7, n)).astype(np.uint8) for n in (70, 301, 16)]
+    for shifts in ((0, 0, 0), (1, 0, 0), (0, 1, 0), (0, 0, 1), (2, 4, 2), (4, 2, 4), (3, 5, 7)):
+        c = md.Cache(L, Hq, Hkv, 16, B, 40, 120, region_aligned_pages=int(kernel == "append apart"))
+        if kernel != "cluster":
+            c.debug_set(md.MD_DEBUG_GRID_LIMIT, 512)
+        for b in range(B):
+            k, v = synth.kv_host(61, b, L, Hkv, 0, len(lab[b]), lab[b])
+            c.append_tokens(b, lab[b], to_dev(k), to_dev(v))
+        out = torch.zeros((B, L, Hq, 128), dtype=torch.int16, device="cuda")
+        for l in range(L) if how == "layers" else [slice(None)]:
+            rows, o = [], torch.zeros_like(out[:, l]).contiguous()
+            for t, s in zip(x, shifts):
+                part = t[:, l].contiguous()
+                buf = torch.zeros(part.numel() + 8, dtype=part.dtype, device="cuda")
+                buf[s:s + part.numel()] = part.flatten()
+                rows.append(buf)
+            at = [r.data_ptr() + 2 * s for r, s in zip(rows, shifts)]
+            c.decode_layer(l, B, *at, [6] * B, o) if how == "layers" else c.decode_step(B, *at, [6] * B, o)
+            assert c.sync() == md.MD_OK
+            out[:, l] = o
+        used = c.get_state(md.MD_STATE_BLOCK_TABLE)[0, :c.query(md.MD_QUERY_PAGES, 0)].long()
+        got = [out, c.get_state(md.MD_STATE_MASS), c.get_state(md.MD_STATE_POOL)[:, used]]
+        want = want or got
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and out.any()
+        c.close()
+
+
+def test_appended_rows_are_16_byte_aligned():
+    c = md.Cache(1, 4, 1, 16, 1, 8, 8)
+    rows = torch.zeros((1, 1, 4, 128), dtype=torch.int16, device="cuda")
+    for k, v in ((2, 0), (0, 8), (4, 4)):
+        with pytest.raises(md.MemDecayError) as e:
+            c.append_tokens(0, [1, 1], rows.data_ptr() + k, rows.data_ptr() + v)
+        assert e.value.status == md.MD_ERR_INVALID_ARG and c.query(md.MD_QUERY_TOKENS, 0) == 0
+    c.append_tokens(0, [1, 1], rows, rows)
+    assert c.query(md.MD_QUERY_TOKENS, 0) == 2 and c.sync() == md.MD_OK
+
+
 @pytest.mark.parametrize("ps,aligned,reduce", [(16, 0, 0), (32, 0, 1), (16, 1, 1), (32, 1, 0)])
 def test_one_launch_observation_selects_what_the_two_kernels_select(ps, aligned, reduce):
     """A batch of short sequences, scored and selected in one launch, against

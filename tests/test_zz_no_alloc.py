@@ -170,3 +170,13 @@ def test_noalloc_rejects_work_beyond_its_fixed_scratch():
     st = md.lib().md_attend_mass_noalloc(p, p, n_tok.ctypes.data, p, p, p, 1, 2, 16, 2, 24, 4096, 64, None)
     assert st == md.MD_ERR_INVALID_ARG
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("batch,tokens", [(1, 40), (16, 3000)])
+def test_noalloc_rejects_queries_that_its_kernels_cannot_read(batch, tokens):
+    """Before anything is launched, whichever kernel the launch would take."""
+    dummy = torch.zeros(64, dtype=torch.int32, device="cuda")
+    n_tok, p = np.full(batch, tokens, np.int32), dummy.data_ptr()
+    st = md.lib().md_attend_mass_noalloc(p, p, n_tok.ctypes.data, p + 2, p, p, batch, 16, 16, 2, 16, 200, 4000, None)
+    assert st == md.MD_ERR_INVALID_ARG
+    torch.cuda.synchronize()
