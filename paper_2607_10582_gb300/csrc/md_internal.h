@@ -284,8 +284,8 @@ struct PageSet {
 struct BoundsParams : PageSet {
   const uint16_t *pool;
   uint16_t *bounds;                      // [L][P_phys][Hkv][2][D]
-  int first[MD_MAX_BATCH];               // pages first[b] .. end[b] - 1 are bounded
-  int start[MD_MAX_BATCH + 1];           // their running count
+  int first[MD_MAX_BATCH];               // start[b + 1] - start[b] pages of sequence b are
+  int start[MD_MAX_BATCH + 1];           // bounded, from first[b] on
 };
 cudaError_t launch_bounds(const BoundsParams &p, cudaStream_t s);
 struct PageScoresParams : PageSet {

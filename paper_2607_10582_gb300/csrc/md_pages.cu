@@ -115,9 +115,13 @@ __device__ __forceinline__ void load_q(const uint16_t *q, int G, int g, int t, u
  * the query heads its columns, and lo and hi side by side the summed dimension,
  * against the queries' negative and positive parts.
  *
+ * The sum is left in the instructions' 32-bit accumulators: against 64 bits it is off by
+ * 1.6e-7 (rms, relative), three times what separate operations would be.
+ *
  * HBM bounds it, given registers for all of a tile's loads at once (64 a thread):
  * 2.1 M pages (1.08 GB of bounds) 161 us, 99% of the copy rate; 171 with 80 registers
- * and fewer warps, 180 with 54, where the loads went out in two parts. */
+ * and fewer warps, 180 with 54, where the loads went out in two parts, 167 with the
+ * pages that are not there kept in a register, which spilled one. */
 __global__ void __launch_bounds__(256, 4) page_scores_kernel(const __grid_constant__ PageScoresParams p, int tiles) {
   pdl_wait();
   pdl_trigger();
@@ -179,7 +183,8 @@ __device__ __forceinline__ uint32_t score_key(float x) {
  * taken whole or holds equal keys: two rounds for most rows.  The pages that are
  * taken become bits, and one scan over the words of bits gives all places.
  *
- * Latency bounds it: barriers and round trips through shared memory.  2 rows of 2,048
+ * Latency bounds it: barriers and round trips through shared memory; with several blocks
+ * per SM also the atomics, one per key and round.  2 rows of 2,048
  * pages 4.0 us, 576 rows of 4,096 9.6 us.  With keys in shared memory and a second pass
  * over them for the places 5.6 and 15.7; with eight-bit digits 7.3 and 24.3. */
 constexpr int BINS = 2048;
