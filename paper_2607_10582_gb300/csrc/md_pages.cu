@@ -366,14 +366,21 @@ __device__ __forceinline__ float max_base(float m) { return m == -INFINITY ? 0.f
 
 /* Sums over channels d .. d + 3 of V rows with finite weights, of which some came out
  * NaN: infinite where the row's tokens have infinite values of one sign and no NaN, as
- * every weight is above 0.  A pass over those channels, for such sums only. */
+ * every weight is above 0.  A pass over those channels, for such sums only, up to the
+ * page that shows all of them to be NaN (the first one, if all values are).  With
+ * infinite values a call takes about 1 us more per page of a list, 4 x 65,536 tokens of
+ * nothing else in 36 layers 767 us instead of 97. */
 __device__ __noinline__ float4 infinite_sums(const AttendParams &p, int row, int b, int l, int h, int d, float4 sums) {
-  uint32_t seen = 0;                                 // 4 bits per channel: inf, -inf, NaN
-  for (int e = 0; e < p.top; ++e) {
+  float *s = &sums.x;
+  uint32_t seen = 0, open = 0;                       // 4 bits per channel: inf, -inf, NaN; those to be told
+#pragma unroll
+  for (int k = 0; k < 4; ++k) open |= (s[k] != s[k] ? 1u : 0u) << 4 * k;
+  for (int e = 0; e < p.top && open; ++e) {
     const int pg = p.ids[(size_t)row * p.top + e], phys = page_id(p, b, pg);
     if (phys < 0) continue;
     const int n = page_tokens(p, b, pg);
     const uint16_t *v = p.pool + ((((size_t)(p.l0 + l) * p.P_phys + phys) * p.Hkv + h) * 2 + 1) * p.ps * D + d;
+#pragma unroll 8
     for (int i = 0; i < n; ++i) {
       const uint2 w = *(const uint2 *)(v + i * D);
 #pragma unroll
@@ -382,13 +389,11 @@ __device__ __noinline__ float4 infinite_sums(const AttendParams &p, int row, int
         if ((x & 0x7f80u) == 0x7f80u) seen |= (x & 0x7fu ? 4u : x & 0x8000u ? 2u : 1u) << 4 * k;
       }
     }
+    open &= ~(seen >> 2 | (seen & seen >> 1));
   }
-  float *s = &sums.x;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t x = seen >> 4 * k & 7u;
-    if (s[k] != s[k] && (x == 1u || x == 2u)) s[k] = x == 1u ? INFINITY : -INFINITY;
-  }
+  for (int k = 0; k < 4; ++k)
+    if (open >> 4 * k & 1u && seen >> 4 * k & 3u) s[k] = seen >> 4 * k & 1u ? INFINITY : -INFINITY;
   return sums;
 }
 __device__ __forceinline__ bool any_nan(float4 x) { return isnan(x.x + x.y) || isnan(x.z + x.w); }
