@@ -451,7 +451,8 @@ md_status md_attend_mass_noalloc(const void *kv_pool_dev, const int32_t *block_t
 enum {
   MD_TYPE_BF16 = 0,
   MD_TYPE_F16 = 1,
-  MD_TYPE_F32 = 2
+  MD_TYPE_F32 = 2,
+  MD_TYPE_E4M3 = 3                /* of a cache: 4 exponent and 3 fraction bits, no infinity */
 };
 #define MD_MAX_AXES 4             /* position axes of a rotation */
 
@@ -485,7 +486,7 @@ md_status md_rope_table(const double *inv_freq_host, int rotary_dim, int table_l
 typedef struct {
   int n_tokens;                /* 0: nothing is done */
   int num_q_heads, num_kv_heads; /* either may be 0; its pointers are then not read */
-  int type;                    /* of q, k and v: MD_TYPE_* */
+  int type;                    /* of q, k and v: MD_TYPE_BF16, F16 or F32 */
   int rotary_dim;              /* a multiple of 8 in [0, 128]; 0: no rotation */
   int interleaved;
   int num_axes;                /* rows of positions: 1 .. MD_MAX_AXES */
@@ -604,6 +605,96 @@ md_status md_attend_pages(const void *q_dev, const void *kv_pool_dev, const int3
 size_t md_sparse_bytes(const md_config *cfg, int top_pages);
 md_status md_sparse_enable(md_ctx *ctx, int top_pages, int first_pages, int last_pages, void *buffer_dev,
                            size_t bytes);
+
+/* ---- a cache in eight bits -------------------------------------------- */
+
+/* Half the bytes of a bf16 cache: twice the tokens in the same memory, and decode
+ * attention, which reads every one of them, in about half the time.  The cache is the
+ * caller's:
+ *   pool_dev         e4m3 [L][num_phys_pages][Hkv][2][page_size][128], 16-byte aligned:
+ *                    md_decode_step's layout with a byte per element
+ *   scales_dev       fp32 [L][num_phys_pages][Hkv][2][page_size / 16]: one for each block
+ *                    of 16 tokens of a layer, page, KV head, and K or V; 8-byte aligned.
+ *                    A code c stands for c * scale
+ *   block_table_dev  int32 [batch][max_pages_per_seq] physical page ids
+ * Limits as md_config's (batch <= MD_MAX_BATCH, pages of 16 or 32 tokens, at most
+ * MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS tokens per sequence).  The calls allocate nothing,
+ * keep nothing and enqueue their work on `stream`. */
+#define MD_SCALE_TOKENS 16        /* tokens of a scale */
+
+/* The tokens of md_write_cache8 and md_read_cache8: of each sequence b, count_host[b]
+ * tokens from position first_host[b] on, their rows one after the other in k and v,
+ * sequence by sequence.  Element (row, layer, KV head, d) of k is
+ * k[row * k_row + layer * k_layer + head * k_head + d] (strides in elements): a decode step's
+ * [batch][L][Hkv][128], a prompt's [L][Hkv][n][128], or one layer's part of a projection.
+ * Bases 8-byte aligned (fp32: 16), strides multiples of 4. */
+typedef struct {
+  int batch, num_layers, num_kv_heads, page_size, max_pages_per_seq, num_phys_pages;
+  int type;                      /* of k and v: MD_TYPE_BF16, F16 or F32 */
+  const int32_t *first_host;     /* [batch] position of the first token (host, read before return) */
+  const int32_t *count_host;     /* [batch] tokens, 0 or more (host, read before return) */
+  void *k, *v;                   /* (device; read by the write, written by the read) */
+  int64_t k_row, k_layer, k_head, v_row, v_layer, v_head;
+  void *pool_dev;
+  float *scales_dev;
+  const int32_t *block_table_dev;
+  void *stream;                  /* cudaStream_t */
+} md_cache8_args;
+
+/* Writes rows into the cache.  A block whose first token is among them gets the scale
+ *   s = the least power of two, 2^-126 at least, with |x| <= 448 s for its new values
+ * (values that are not finite are left out), and the codes of x / s, rounded to nearest
+ * even; what is not finite becomes NaN (0x7f).  In a block that held tokens before, as a decode
+ * step's mostly does, s is at least its scale until then; where that grows, the codes of the
+ * tokens before are moved to it: exactly, but for those that fall below 2^-6 s, which are
+ * rounded once more.  Slots behind the new tokens are left as they are.
+ * The slots of a block before first_host[b] must have been written.  A page belongs to one
+ * sequence of the call.  Rows whose block-table entry lies outside the pool are not written. */
+md_status md_write_cache8(const md_cache8_args *args);
+
+/* Reads tokens back into rows: code times scale, rounded once to the rows' type (bf16 and
+ * fp32 hold it exactly, but for results below their smallest normal number, or above the
+ * largest).  Rows whose block-table entry lies outside the pool are NaN.
+ * The scales and the pool are not written. */
+md_status md_read_cache8(const md_cache8_args *args);
+
+/* Decode attention over a cache that the caller owns, in eight bits or in bf16: one new
+ * token per sequence attends the cached tokens i that are visible to it,
+ *   i < n_tokens  and  (i < sinks  or  i >= n_tokens - window),
+ * with md_decode_step's arithmetic (softmax of q k / sqrt(128), in 32 bits; what is rounded
+ * stands below).  window = -1: all tokens are visible.  Only pages with visible tokens are
+ * read, and what lies in other slots, NaN included, has no part in the result.  A
+ * sequence without visible tokens yields zeros, and -inf as its logarithm.  Pages whose
+ * block-table entry lies outside the pool are taken for pages without tokens.
+ *   E4M3  the softmax weights enter the product with V rounded to 11 bits (f16), the queries
+ *         as f16 relative to the head's largest: exactly, but for elements below 2^-29 of it
+ *   BF16  the weights enter as two bf16 terms each.  Infinite values of one sign make their
+ *         channel infinite, whatever their tokens' weights
+ * How a row is split over CTAs goes by the launch's shape and whether there is a workspace:
+ * calls of the same shape give the same bits, others may round differently.  The kernel's
+ * waits for its own copies are bounded (2 s); a row that gives up is NaN.
+ *   workspace_dev: NULL, or MD_ATTEND_WORKSPACE bytes of device memory, 16-byte aligned, the
+ *   caller's; calls that may run at the same time need one each.  With it, long sequences
+ *   are split over more CTAs (few rows, or sequences of unequal length). */
+#define MD_ATTEND_WORKSPACE (16u << 20)
+typedef struct {
+  int batch, num_layers, num_q_heads, num_kv_heads, page_size, max_pages_per_seq, num_phys_pages;
+  int type;                      /* of the pool: MD_TYPE_E4M3 or MD_TYPE_BF16 */
+  int window;                    /* last tokens that are visible; -1: all */
+  int sinks;                     /* first tokens that are visible besides */
+  const void *q_dev;             /* bf16 [batch][L][Hq][128], 16-byte aligned */
+  const void *pool_dev;          /* [L][num_phys_pages][Hkv][2][page_size][128] */
+  const float *scales_dev;       /* E4M3 only, as above */
+  const int32_t *block_table_dev;
+  const int32_t *n_tokens_host;  /* [batch] cached tokens (host, read before return), 0 or more */
+  void *out_dev;                 /* bf16 [batch][L][Hq][128], 8-byte aligned (written) */
+  float *lse_dev;                /* fp32 [batch][L][Hq] (written), or NULL: the natural
+                                    logarithm of each head's sum of exponentials */
+  void *workspace_dev;
+  size_t workspace_bytes;        /* MD_ERR_WORKSPACE where there is one and it is smaller */
+  void *stream;                  /* cudaStream_t */
+} md_attend_cache_args;
+md_status md_attend_cache(const md_attend_cache_args *args);
 
 #ifdef __cplusplus
 }

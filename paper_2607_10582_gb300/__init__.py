@@ -45,9 +45,11 @@ MD_MAX_CHUNK_TOKENS = 4096
  MD_STATE_T_INS, MD_STATE_PAGE_FILL, MD_STATE_SEQ_TOKENS, MD_STATE_CALIB) = range(15)
 MD_CALIB_BUCKETS = 256
 MD_CALIB_BUCKET_WIDTH = 4
-MD_TYPE_BF16, MD_TYPE_F16, MD_TYPE_F32 = range(3)
+MD_TYPE_BF16, MD_TYPE_F16, MD_TYPE_F32, MD_TYPE_E4M3 = range(4)
 MD_MAX_AXES = 4
 MD_MAX_TOP_TOKENS = 65536
+MD_SCALE_TOKENS = 16
+MD_ATTEND_WORKSPACE = 16 << 20
 (MD_QUERY_TOKENS, MD_QUERY_PAGES, MD_QUERY_FREE_TOP, MD_QUERY_STEP, MD_QUERY_WINDOW,
  MD_QUERY_PINNED_PAGES) = range(6)
 (MD_DEBUG_SPIN_LIMIT_NS, MD_DEBUG_EXTRA_ARRIVALS, MD_DEBUG_GRID_LIMIT, MD_DEBUG_UNIT_OVERHEAD,
@@ -80,6 +82,22 @@ class md_norm_rope_args(ctypes.Structure):
                                                "q_out_token", "q_out_head", "k_out_token", "k_out_head",
                                                "v_out_token", "v_out_head")] +
                 [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "table", "positions", "axis_host", "stream")])
+
+
+class md_cache8_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("batch", "num_layers", "num_kv_heads", "page_size", "max_pages_per_seq",
+                                             "num_phys_pages", "type")] +
+                [(n, ctypes.c_void_p) for n in ("first_host", "count_host", "k", "v")] +
+                [(n, ctypes.c_int64) for n in ("k_row", "k_layer", "k_head", "v_row", "v_layer", "v_head")] +
+                [(n, ctypes.c_void_p) for n in ("pool_dev", "scales_dev", "block_table_dev", "stream")])
+
+
+class md_attend_cache_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("batch", "num_layers", "num_q_heads", "num_kv_heads", "page_size",
+                                             "max_pages_per_seq", "num_phys_pages", "type", "window", "sinks")] +
+                [(n, ctypes.c_void_p) for n in ("q_dev", "pool_dev", "scales_dev", "block_table_dev", "n_tokens_host",
+                                                "out_dev", "lse_dev", "workspace_dev")] +
+                [("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)])
 
 
 # name -> (restype, argtypes); the names and order of include/memdecay.h
@@ -117,6 +135,9 @@ SIGNATURES = {
     "md_page_scores": (_c.c_int, [_P] * 5 + [_c.c_int] * 7 + [_P]),
     "md_page_top": (_c.c_int, [_P] * 3 + [_c.c_int] * 8 + [_P]),
     "md_attend_pages": (_c.c_int, [_P] * 7 + [_c.c_int] * 8 + [_P]),
+    "md_write_cache8": (_c.c_int, [_c.POINTER(md_cache8_args)]),
+    "md_read_cache8": (_c.c_int, [_c.POINTER(md_cache8_args)]),
+    "md_attend_cache": (_c.c_int, [_c.POINTER(md_attend_cache_args)]),
     "md_sparse_bytes": (_c.c_size_t, [_c.POINTER(md_config), _c.c_int]),
     "md_sparse_enable": (_c.c_int, [_P, _c.c_int, _c.c_int, _c.c_int, _P, _c.c_size_t]),
 }
@@ -154,6 +175,7 @@ class _NoCalls:
 
     decode_step = decode_step_host = decode_layer = evict = get_state = _leave
     load_torch = norm_rope = page_bounds = page_scores = page_top = attend_pages = _leave
+    write_cache8 = read_cache8 = attend_cache = _leave
 
 
 def _binding():
@@ -264,7 +286,8 @@ def _on(t, stream):
     return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
 
 
-_KINDS = {"bf16": ("bfloat16", "int16"), "f32": ("float32",), "i32": ("int32",)}    # int16: raw bf16 bits
+_KINDS = {"bf16": ("bfloat16", "int16"), "f32": ("float32",), "i32": ("int32",),    # int16: raw bf16 bits
+          "e4m3": ("float8_e4m3fn", "uint8"), "bytes": ("uint8",)}                 # uint8: raw e4m3 bits
 
 
 def _dense(name, t, shape, kind):
@@ -468,6 +491,111 @@ def md_attend_pages(q, pool, block_table, n_tokens, page_ids, out, *, mass=None,
         _dense("out", out, (B, L, Hq, MD_HEAD_DIM), "bf16"),
         None if mass is None else _dense("mass", mass, (B, L, Hkv, top * ps), "f32"), B, L, Hq, Hkv, ps, P_max, P, top,
         _on(q, stream)), "md_attend_pages")
+
+
+def _cache8(call, written: bool, k, v, pool, scales, block_table, first, count, stream):
+    a = md_cache8_args()
+    B, P_max = _dims("block_table", block_table, 2)
+    L, P, Hkv, _, ps, _ = _dims("pool", pool, 6)
+    types, rows = _row_types(), _dims("k", k, 4)[0]
+    f, a.first_host = _counts(first, B)
+    n, a.count_host = _counts(count, B)
+    if (n[:B] < 0).any() or int(n[:B].sum(dtype=np.int64)) > rows:
+        _bad(f"counts of {int(n[:B].sum(dtype=np.int64))} tokens for {rows} rows")
+    if k.dtype not in types:
+        _bad(f"rows of {k.dtype}")
+    for name, x in (("k", k), ("v", v)):
+        _dims(name, x, 4)
+        _here(name, x)
+        if tuple(x.shape) != (rows, L, Hkv, MD_HEAD_DIM) or x.dtype != k.dtype:
+            _bad(f"{name}: {(rows, L, Hkv, MD_HEAD_DIM)} of {k.dtype} expected, not {tuple(x.shape)} of {x.dtype}")
+        if x.numel() and x.stride(3) != 1:
+            _bad(f"{name}: the elements of a row must be adjacent")
+        if written and any(x.shape[d] > 1 and x.stride(d) == 0 for d in range(3)):
+            _bad(f"{name}: rows that lie on one another cannot be written")
+        setattr(a, name, x.data_ptr())
+        for d, part in enumerate(("_row", "_layer", "_head")):
+            setattr(a, name + part, x.stride(d) if x.shape[d] > 1 else 0)
+    a.batch, a.num_layers, a.num_kv_heads, a.page_size, a.max_pages_per_seq, a.num_phys_pages = B, L, Hkv, ps, P_max, P
+    a.type = types[k.dtype]
+    a.pool_dev = _dense("pool", pool, (L, P, Hkv, 2, ps, MD_HEAD_DIM), "e4m3")
+    a.scales_dev = _dense("scales", scales, (L, P, Hkv, 2, ps // MD_SCALE_TOKENS), "f32")
+    a.block_table_dev = _dense("block_table", block_table, (B, P_max), "i32")
+    a.stream = _on(pool, stream)
+    _status(getattr(lib(), call)(ctypes.byref(a)), f"{call}: positions, counts, alignment or strides")
+
+
+def md_write_cache8(k, v, pool, scales, block_table, first, count, *, stream=None):
+    """Writes rows into a cache in eight bits: of each sequence, count[b] tokens from position
+    first[b] on.  A block of 16 tokens of a layer, KV head, and K or V has one scale, a power of two;
+    a block that holds tokens already keeps it or moves to a larger one; see md_write_cache8 in the header.
+      k, v         [rows][L][Hkv][128] bf16, f16 or f32, any strides over rows, layers and heads: the
+                   sequences' tokens one after the other (rows behind them are not read)
+      pool         e4m3 (or its raw bits, uint8) [L][pages][Hkv][2][page_size][128]; written
+      scales       fp32 [L][pages][Hkv][2][page_size / 16]; written
+      block_table  int32 [batch][max_pages_per_seq]
+      first, count int32 [batch] on the host"""
+    st = (_torch_calls or _ops()).write_cache8(k, v, pool, scales, block_table, first, count,
+                                               None if stream is None else stream.cuda_stream)
+    if st is not None:
+        return _status(st, "md_write_cache8: positions, counts, alignment or strides")
+    _cache8("md_write_cache8", False, k, v, pool, scales, block_table, first, count, stream)
+
+
+def md_read_cache8(k, v, pool, scales, block_table, first, count, *, stream=None):
+    """Reads tokens of a cache in eight bits back into rows, the other way round than
+    md_write_cache8: k and v are written (rows behind the tokens are left as they are)."""
+    st = (_torch_calls or _ops()).read_cache8(k, v, pool, scales, block_table, first, count,
+                                              None if stream is None else stream.cuda_stream)
+    if st is not None:
+        return _status(st, "md_read_cache8: positions, counts, alignment or strides")
+    _cache8("md_read_cache8", True, k, v, pool, scales, block_table, first, count, stream)
+
+
+def md_attend_cache(q, pool, block_table, n_tokens, out, *, scales=None, window=None, sinks: int = 0, lse=None,
+                    workspace=None, stream=None):
+    """Attention of one new token per sequence over the cached tokens that are visible to it: the
+    last `window` ones (None: all) and the first `sinks` ones.
+      q, out       bf16 [batch][L][Hq][128]
+      pool         [L][pages][Hkv][2][page_size][128]: e4m3 (or its raw bits) with its scales, else bf16
+      scales       fp32 [L][pages][Hkv][2][page_size / 16], or None: the pool is in bf16
+      block_table  int32 [batch][max_pages_per_seq]
+      n_tokens     int32 [batch] on the host
+      lse          fp32 [batch][L][Hq] or None; written: the logarithm of each head's sum of exponentials
+      workspace    uint8 [MD_ATTEND_WORKSPACE] or None: lets long sequences be split further; calls that may
+                   run at the same time need one each"""
+    st = (_torch_calls or _ops()).attend_cache(q, pool, block_table, n_tokens, out, scales, window, sinks, lse, workspace,
+                                               None if stream is None else stream.cuda_stream)
+    if st is not None:
+        return _status(st, "md_attend_cache")
+    a = md_attend_cache_args()
+    B, P_max = _dims("block_table", block_table, 2)
+    L, P, Hkv, _, ps, _ = _dims("pool", pool, 6)
+    Hq = _dims("q", q, 4)[2]
+    n, a.n_tokens_host = _counts(n_tokens, B)
+    a.batch, a.num_layers, a.num_q_heads, a.num_kv_heads = B, L, Hq, Hkv
+    a.page_size, a.max_pages_per_seq, a.num_phys_pages = ps, P_max, P
+    a.type = MD_TYPE_BF16 if scales is None else MD_TYPE_E4M3
+    for name, x in (("window", window), ("sinks", sinks)):
+        if x is None and name == "window":
+            a.window = -1
+            continue
+        x = int(_whole(name, [x], np.int64)[0].reshape(-1)[0])
+        if x < 0:
+            _bad(f"{name}: a whole number from 0 on expected")
+        setattr(a, name, min(x, (1 << 31) - 1))
+    a.q_dev = _dense("q", q, (B, L, Hq, MD_HEAD_DIM), "bf16")
+    a.pool_dev = _dense("pool", pool, (L, P, Hkv, 2, ps, MD_HEAD_DIM), "bf16" if scales is None else "e4m3")
+    if scales is not None:
+        a.scales_dev = _dense("scales", scales, (L, P, Hkv, 2, ps // MD_SCALE_TOKENS), "f32")
+    a.block_table_dev = _dense("block_table", block_table, (B, P_max), "i32")
+    a.out_dev = _dense("out", out, (B, L, Hq, MD_HEAD_DIM), "bf16")
+    if lse is not None:
+        a.lse_dev = _dense("lse", lse, (B, L, Hq), "f32")
+    if workspace is not None:
+        a.workspace_dev, a.workspace_bytes = _dense("workspace", workspace, (workspace.numel(),), "bytes"), workspace.numel()
+    a.stream = _on(q, stream)
+    _status(lib().md_attend_cache(ctypes.byref(a)), "md_attend_cache")
 
 
 class Cache:

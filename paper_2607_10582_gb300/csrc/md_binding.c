@@ -34,6 +34,9 @@ static md_status (*f_page_scores)(const void *, const void *, const int32_t *, c
 static md_status (*f_page_top)(const float *, const int32_t *, int32_t *, int, int, int, int, int, int, int, int, void *);
 static md_status (*f_attend_pages)(const void *, const void *, const int32_t *, const int32_t *, const int32_t *, void *,
                                    float *, int, int, int, int, int, int, int, int, void *);
+static md_status (*f_write_cache8)(const md_cache8_args *);
+static md_status (*f_read_cache8)(const md_cache8_args *);
+static md_status (*f_attend_cache)(const md_attend_cache_args *);
 
 static PyObject *load(PyObject *self, PyObject *path) {
   const char *s = PyUnicode_AsUTF8(path);
@@ -53,8 +56,12 @@ static PyObject *load(PyObject *self, PyObject *path) {
   *(void **)&f_page_scores = dlsym(h, "md_page_scores");
   *(void **)&f_page_top = dlsym(h, "md_page_top");
   *(void **)&f_attend_pages = dlsym(h, "md_attend_pages");
+  *(void **)&f_write_cache8 = dlsym(h, "md_write_cache8");
+  *(void **)&f_read_cache8 = dlsym(h, "md_read_cache8");
+  *(void **)&f_attend_cache = dlsym(h, "md_attend_cache");
   if (!f_decode_step || !f_decode_step_host || !f_decode_layer || !f_evict || !f_get_state || !f_norm_rope ||
-      !f_page_bounds || !f_page_scores || !f_page_top || !f_attend_pages) {
+      !f_page_bounds || !f_page_scores || !f_page_top || !f_attend_pages || !f_write_cache8 || !f_read_cache8 ||
+      !f_attend_cache) {
     PyErr_SetString(PyExc_OSError, "libmemdecay.so lacks an entry point");
     return NULL;
   }
@@ -234,7 +241,7 @@ static PyObject *get_state(PyObject *self, PyObject *const *a, Py_ssize_t n) {
  * Against reading the object's attributes, on a Grace core, a call: norm_rope of one
  * token (ten tensors) 6.4 -> 4.0 us, bounds of 32 pages 4.4 -> 3.5, scores of one row
  * 4.7 -> 3.5, attention of one row over one layer 5.9 -> 4.9. */
-enum { T_BF16, T_F16, T_F32, T_I16, T_I32, T_OTHER };
+enum { T_BF16, T_F16, T_F32, T_I16, T_I32, T_E4M3, T_U8, T_OTHER };
 #define MAX_DIMS 6
 
 static struct {
@@ -261,7 +268,8 @@ static PyObject *load_torch(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   if (!l || !g) Py_RETURN_FALSE;
   static const char *const kinds[T_OTHER] = {"aoti_torch_dtype_bfloat16", "aoti_torch_dtype_float16",
                                              "aoti_torch_dtype_float32", "aoti_torch_dtype_int16",
-                                             "aoti_torch_dtype_int32"};
+                                             "aoti_torch_dtype_int32", "aoti_torch_dtype_float8_e4m3fn",
+                                             "aoti_torch_dtype_uint8"};
   int32_t (*kind)(void);
   for (int i = 0; i < T_OTHER; ++i) {
     *(void **)&kind = dlsym(l, kinds[i]);
@@ -549,6 +557,139 @@ static PyObject *attend_pages(PyObject *self, PyObject *const *a, Py_ssize_t n) 
   return PyLong_FromLong(st);
 }
 
+static int one_byte(const tensor *t) { return t->type == T_E4M3 || t->type == T_U8; }
+
+/* A pool in eight bits, [L][pages][Hkv][2][page_size][128], and its scales. */
+static int pool8_tensor(PyObject *o, tensor *t) {
+  return dense_tensor(o, t) && t->dims == 6 && one_byte(t) && t->n[3] == 2 && t->n[5] == MD_HEAD_DIM &&
+         t->n[0] < 256 && t->n[1] < INT32_MAX && t->n[2] < INT32_MAX && t->n[4] < INT32_MAX;
+}
+static int scale_tensor(PyObject *o, tensor *t, const tensor *pool) {
+  return dense_tensor(o, t) && t->type == T_F32 &&
+         has_shape(t, 5, pool->n[0], pool->n[1], pool->n[2], 2, pool->n[4] / MD_SCALE_TOKENS) && t->device == pool->device;
+}
+
+/* (k, v, pool, scales, block_table, first, count, stream) of md_write_cache8 and md_read_cache8 */
+static PyObject *cache8(PyObject *const *a, Py_ssize_t n, md_status (*f)(const md_cache8_args *)) {
+  if (arity(n, 8)) return NULL;
+  md_cache8_args r = {0};
+  tensor x[2], pool, scales, table;
+  int64_t *stride[2][3] = {{&r.k_row, &r.k_layer, &r.k_head}, {&r.v_row, &r.v_layer, &r.v_head}};
+  if (!pool8_tensor(a[2], &pool) || !scale_tensor(a[3], &scales, &pool) || !block_table_tensor(a[4], &table) ||
+      table.device != pool.device)
+    return leave();
+  for (int i = 0; i < 2; ++i) {
+    if (!device_tensor(a[i], &x[i]) || x[i].dims != 4 || x[i].type > T_F32 || x[i].type != x[0].type ||
+        x[i].device != pool.device || x[i].n[0] != x[0].n[0] || x[i].n[1] != pool.n[0] || x[i].n[2] != pool.n[2] ||
+        x[i].n[3] != MD_HEAD_DIM || x[i].stride[3] != 1)
+      return leave();
+    for (int d = 0; d < 3; ++d) {
+      if (f == f_read_cache8 && x[i].n[d] > 1 && x[i].stride[d] == 0) return leave();   // rows on one another
+      *stride[i][d] = x[i].n[d] > 1 ? x[i].stride[d] : 0;
+    }
+  }
+  Py_buffer first, count;
+  if (!call_stream(pool.device, a[7], &r.stream) || !count_view(a[5], table.n[0], &first)) return leave();
+  if (!count_view(a[6], table.n[0], &count)) {
+    PyBuffer_Release(&first);
+    return leave();
+  }
+  long long rows = 0;
+  int whole = 1, st = 0;
+  for (int64_t b = 0; b < table.n[0]; ++b) {
+    const int32_t c = ((const int32_t *)count.buf)[b];
+    whole &= c >= 0;
+    rows += c;
+  }
+  if (whole && rows <= x[0].n[0]) {
+    r.batch = (int)table.n[0];
+    r.num_layers = (int)pool.n[0];
+    r.num_kv_heads = (int)pool.n[2];
+    r.page_size = (int)pool.n[4];
+    r.max_pages_per_seq = (int)table.n[1];
+    r.num_phys_pages = (int)pool.n[1];
+    r.type = x[0].type == T_BF16 ? MD_TYPE_BF16 : x[0].type == T_F16 ? MD_TYPE_F16 : MD_TYPE_F32;
+    r.first_host = first.buf;
+    r.count_host = count.buf;
+    r.k = x[0].p;
+    r.v = x[1].p;
+    r.pool_dev = pool.p;
+    r.scales_dev = scales.p;
+    r.block_table_dev = table.p;
+    Py_BEGIN_ALLOW_THREADS
+    st = f(&r);
+    Py_END_ALLOW_THREADS
+  }
+  PyBuffer_Release(&first);
+  PyBuffer_Release(&count);
+  if (!whole || rows > x[0].n[0]) return leave();
+  return PyLong_FromLong(st);
+}
+static PyObject *write_cache8(PyObject *self, PyObject *const *a, Py_ssize_t n) { return cache8(a, n, f_write_cache8); }
+static PyObject *read_cache8(PyObject *self, PyObject *const *a, Py_ssize_t n) { return cache8(a, n, f_read_cache8); }
+
+/* A whole number from `least` to INT32_MAX. */
+static int count_arg(PyObject *o, int least, int *out) {
+  if (!PyLong_Check(o)) return 0;
+  const long long v = PyLong_AsLongLong(o);
+  if (PyErr_Occurred() || v < least || v > INT32_MAX) return 0;
+  *out = (int)v;
+  return 1;
+}
+
+/* attend_cache(q, pool, block_table, n_tokens, out, scales, window, sinks, lse, workspace, stream) */
+static PyObject *attend_cache(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  if (arity(n, 11)) return NULL;
+  md_attend_cache_args r = {0};
+  tensor q, pool, table, out, t;
+  const int wide = a[5] == Py_None;
+  if (!(wide ? pool_tensor(a[1], &pool) : pool8_tensor(a[1], &pool)) || !block_table_tensor(a[2], &table) ||
+      !dense_tensor(a[0], &q) || !two_bytes(&q) || q.dims != 4 || q.n[2] > INT32_MAX || pool.n[4] > INT32_MAX ||
+      !has_shape(&q, 4, table.n[0], pool.n[0], q.n[2], MD_HEAD_DIM, 0) || !dense_tensor(a[4], &out) ||
+      !two_bytes(&out) || !has_shape(&out, 4, q.n[0], q.n[1], q.n[2], MD_HEAD_DIM, 0) || q.device != pool.device ||
+      table.device != pool.device || out.device != pool.device)
+    return leave();
+  r.type = MD_TYPE_BF16;
+  if (!wide) {
+    if (!scale_tensor(a[5], &t, &pool)) return leave();
+    r.scales_dev = t.p;
+    r.type = MD_TYPE_E4M3;
+  }
+  r.window = -1;
+  if ((a[6] != Py_None && !count_arg(a[6], 0, &r.window)) || !count_arg(a[7], 0, &r.sinks)) return leave();
+  if (a[8] != Py_None) {
+    if (!dense_tensor(a[8], &t) || t.type != T_F32 || !has_shape(&t, 3, q.n[0], q.n[1], q.n[2], 0, 0) ||
+        t.device != pool.device)
+      return leave();
+    r.lse_dev = t.p;
+  }
+  if (a[9] != Py_None) {
+    if (!dense_tensor(a[9], &t) || t.type != T_U8 || t.dims != 1 || t.device != pool.device) return leave();
+    r.workspace_dev = t.p;
+    r.workspace_bytes = (size_t)t.n[0];
+  }
+  Py_buffer count;
+  if (!call_stream(pool.device, a[10], &r.stream) || !count_view(a[3], table.n[0], &count)) return leave();
+  r.batch = (int)table.n[0];
+  r.num_layers = (int)pool.n[0];
+  r.num_q_heads = (int)q.n[2];
+  r.num_kv_heads = (int)pool.n[2];
+  r.page_size = (int)pool.n[4];
+  r.max_pages_per_seq = (int)table.n[1];
+  r.num_phys_pages = (int)pool.n[1];
+  r.q_dev = q.p;
+  r.pool_dev = pool.p;
+  r.block_table_dev = table.p;
+  r.n_tokens_host = count.buf;
+  r.out_dev = out.p;
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_attend_cache(&r);
+  Py_END_ALLOW_THREADS
+  PyBuffer_Release(&count);
+  return PyLong_FromLong(st);
+}
+
 static PyMethodDef methods[] = {
     {"load", load, METH_O, "load(path): binds the calls to libmemdecay.so"},
     {"decode_step", (PyCFunction)(void (*)(void))decode_step, METH_FASTCALL, "md_decode_step"},
@@ -562,6 +703,9 @@ static PyMethodDef methods[] = {
     {"page_scores", (PyCFunction)(void (*)(void))page_scores, METH_FASTCALL, "md_page_scores"},
     {"page_top", (PyCFunction)(void (*)(void))page_top, METH_FASTCALL, "md_page_top"},
     {"attend_pages", (PyCFunction)(void (*)(void))attend_pages, METH_FASTCALL, "md_attend_pages"},
+    {"write_cache8", (PyCFunction)(void (*)(void))write_cache8, METH_FASTCALL, "md_write_cache8"},
+    {"read_cache8", (PyCFunction)(void (*)(void))read_cache8, METH_FASTCALL, "md_read_cache8"},
+    {"attend_cache", (PyCFunction)(void (*)(void))attend_cache, METH_FASTCALL, "md_attend_cache"},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

@@ -281,6 +281,12 @@ struct PageSet {
   int n_tokens[MD_MAX_BATCH];
   int n_pages[MD_MAX_BATCH];
 };
+/* The checks that the page calls share, and what their launches share (Hq: 0 where
+ * a call has no queries); false: refused. */
+bool page_set(PageSet &p, const int32_t *block_table, const int32_t *n_tokens, int batch, int L, int Hq, int Hkv, int ps,
+              int P_max, int P_phys);
+/* The driver's tensor-map encoder, looked up once per process. */
+void *tile_encoder();
 struct BoundsParams : PageSet {
   const uint16_t *pool;
   uint16_t *bounds;                      // [L][P_phys][Hkv][2][D]

@@ -934,10 +934,6 @@ cudaError_t launch_attend_pages(const AttendPagesParams &base, const CUtensorMap
                          : launch(launch_attend<8, true, false>, launch_attend<4, true, false>);
 }
 
-namespace {
-
-/* The checks that the calls share, and what their launches share (Hq: 0 where
- * a call has no queries). */
 bool page_set(PageSet &p, const int32_t *block_table, const int32_t *n_tokens, int batch, int L, int Hq, int Hkv, int ps,
               int P_max, int P_phys) {
   if (!n_tokens || batch < 1 || batch > MD_MAX_BATCH || L < 1 || L > 255 || Hkv < 1 || (ps != 16 && ps != 32) ||
@@ -963,7 +959,6 @@ bool page_set(PageSet &p, const int32_t *block_table, const int32_t *n_tokens, i
   return true;
 }
 
-/* The driver's tensor-map encoder, looked up once per process. */
 void *tile_encoder() {
   static std::atomic<void *> known{nullptr};
   void *fn = known.load();
@@ -976,6 +971,8 @@ void *tile_encoder() {
   }
   return fn;
 }
+
+namespace {
 
 bool misaligned(const void *p) { return !p || ((uintptr_t)p & 15); }
 
