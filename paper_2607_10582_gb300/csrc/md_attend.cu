@@ -5,112 +5,645 @@
 
 #include <math.h>
 
-#include "md_internal.h"
-#include "md_ptx.cuh"
+#include <algorithm>
+
+#include "md_attn.cuh"
 
 namespace md {
 
 namespace {
 
 constexpr int BLOCK = MD_SCALE_TOKENS;
+static_assert(BLOCK == TILE, "a block is a matrix instruction's rows");
+constexpr int STEP_BYTES = 8192;             // K and V of a step: 32 tokens of an e4m3 cache, 16 of a bf16 one
+constexpr int PARTIAL = GP * D + 2 * GP;     // floats of a part of a row: O [8][128], exponents [8], sums [8]
+constexpr int MAX_PARTIALS = MD_ATTEND_WORKSPACE / (PARTIAL * 4);
+constexpr float SLACK = 10.f;                // log2 of the most that a weight may be above its base
+constexpr float LIFT = 5.f;                  // log2 of the weight at the base (E4M3)
+constexpr int OS = D + 4;                    // padded row of a warp's O
+static_assert(GP * OS * 4 <= STEP_BYTES, "a warp's O fits a stage");
 
 struct AttendCacheParams : PageSet {
   const uint16_t *q;
   const void *pool;
   const float *scales;
   uint16_t *out;
-  float *lse;
-  float scale_log2;            // log2(e) / sqrt(D)
-  int window, sinks;           // window: INT_MAX for all
+  float *lse;                                // or null
+  float *partials;                           // of rows that are split over units
+  float scale_log2;                          // log2(e) / sqrt(D)
+  long long limit_ns;
+  int window, sinks;                         // window: INT_MAX for all
+  int C;                                     // CTAs per unit
+  int unit_start[MD_MAX_BATCH + 1];          // units of the sequences before
+  int part_start[MD_MAX_BATCH];              // first partial of a sequence whose rows are split
 };
 
-__device__ __forceinline__ float4 decode4(uint32_t c) {
-  uint32_t lo, hi;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((uint16_t)c));
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((uint16_t)(c >> 16)));
-  const float2 a = __half22float2(*(const __half2 *)&lo), b = __half22float2(*(const __half2 *)&hi);
-  return make_float4(a.x, a.y, b.x, b.y);
+/* The visible tokens of a sequence by blocks of 16: the first `head` blocks, and those from block
+ * `tail` on; `blocks` in all. */
+struct Visible {
+  int w0, sinks;                             // tokens from w0 on, and the first `sinks`
+  int head, tail, blocks;
+};
+__host__ __device__ __forceinline__ Visible visible(int n, int window, int sinks) {
+  Visible v;
+  v.w0 = n - window > 0 ? n - window : 0;
+  v.sinks = sinks < v.w0 ? sinks : v.w0;
+  v.head = (v.sinks + BLOCK - 1) / BLOCK;
+  v.tail = v.w0 / BLOCK;
+  if (v.tail <= v.head) v.head = v.tail = 0; // no block between them
+  v.blocks = v.head + (n + BLOCK - 1) / BLOCK - v.tail;
+  if (v.w0 == n) v.blocks = v.sinks ? (v.sinks + BLOCK - 1) / BLOCK : 0;
+  return v;
 }
-__device__ __forceinline__ float4 bf16x4(uint2 u) {
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xffff0000u));
-}
-/* Channels 4 lane .. of a row of the pool. */
-template <bool E4M3>
-__device__ __forceinline__ float4 row4(const void *pool, size_t row, int lane, const float *scales) {
-  if (!E4M3) return bf16x4(*((const uint2 *)((const uint16_t *)pool + row * D) + lane));
-  const float4 x = decode4(*((const uint32_t *)((const uint8_t *)pool + row * D) + lane));
-  const float s = scales[row / BLOCK];
-  return make_float4(x.x * s, x.y * s, x.z * s, x.w * s);
+/* Which of a block's tokens are visible. */
+__device__ __forceinline__ uint32_t visible_mask(const Visible &v, int n, int tok) {
+  auto below = [](int x) { return x <= 0 ? 0u : x >= BLOCK ? 0xffffu : (1u << x) - 1; };
+  return below(n - tok) & (below(v.sinks - tok) | ~below(v.w0 - tok));
 }
 
-constexpr int WARPS = 8;
+/* The maxima against which weights are taken: 0 where nothing but -inf was seen. */
+__device__ __forceinline__ float max_base(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ float inverse(float s) { return s > 0.f ? 1.f / s : s == 0.f ? 0.f : s; }   // NaN stays
+__device__ __forceinline__ float logarithm(float base, float sum) {
+  return sum == 0.f ? -INFINITY : 0.69314718f * (base + log2f(sum));
+}
 
-/* A block per (sequence, layer, KV head), a warp per token in turn, a lane per four channels:
- * one pass with the running maximum and sum of each head. */
-template <bool E4M3>
-__global__ void __launch_bounds__(32 * WARPS) attend_cache_kernel(const __grid_constant__ AttendCacheParams p) {
-  __shared__ float so[WARPS][GP][D], sm[WARPS][GP], sl[WARPS][GP];
-  pdl_wait();
-  pdl_trigger();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int lh = p.L * p.Hkv, row = blockIdx.x;
-  const int b = row / lh, l = row % lh / p.Hkv, h = row % p.Hkv;
-  const int n = p.n_tokens[b], w0 = max(0, n - p.window), first = min(p.sinks, w0);
-  const size_t q_row = ((size_t)b * p.L + l) * p.Hq + h * p.G;
-  float4 q[GP], o[GP];
-  float m[GP], z[GP];
+/* Bounded wait on an mbarrier phase. */
+__device__ __noinline__ bool wait_copy(uint32_t bar, uint32_t parity, long long limit_ns) {
+  const long long t0 = globaltimer();
+  while (!mbar_try_wait(bar, parity))
+    if (globaltimer() - t0 > limit_ns) return false;
+  return true;
+}
+
+/* D(16x8, f32) = A(16x16, f16, row) * B(16x8, f16, col) + C */
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1, float c0, float c1, float c2, float c3) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%10,%11,%12,%13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+/* Two e4m3 codes (the lower and the upper 16 bits' two) as f16: exact. */
+__device__ __forceinline__ uint32_t f16_lo(uint32_t c) {
+  uint32_t r;
+  asm("{.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;}" : "=r"(r) : "r"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t f16_hi(uint32_t c) {
+  uint32_t r;
+  asm("{.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;}" : "=r"(r) : "r"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 r;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr));
+  return r;
+}
+__device__ __forceinline__ uint32_t word(const uint4 &x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
+
+/* Sums over channels d .. d + 3 of bf16 V rows with finite weights, of which some came out NaN:
+ * infinite where the row's visible tokens have infinite values of one sign and no NaN, as
+ * every weight is above 0 (the two terms of a weight may be 0 or cancel, and their products with
+ * an infinite value give NaN). */
+__device__ __noinline__ float4 infinite_sums(const AttendCacheParams &p, int b, int l, int h, int d, float4 sums) {
+  float *s = &sums.x;
+  uint32_t seen = 0, open = 0;                       // 4 bits per channel: inf, -inf, NaN; those to be told
 #pragma unroll
-  for (int i = 0; i < GP; ++i) {
-    q[i] = i < p.G ? bf16x4(*((const uint2 *)(p.q + (q_row + i) * D) + lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
-    o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    m[i] = -INFINITY;
-    z[i] = 0.f;
-  }
-  for (int j = warp; j < first + n - w0; j += WARPS) {
-    const int tok = j < first ? j : j - first + w0, pg = tok / p.ps;
+  for (int k = 0; k < 4; ++k) open |= (s[k] != s[k] ? 1u : 0u) << 4 * k;
+  const int n = p.n_tokens[b];
+  const Visible v = visible(n, p.window, p.sinks);
+  for (int i = 0; i < v.blocks && open; ++i) {
+    const int tok = (i < v.head ? i : i - v.head + v.tail) * BLOCK, pg = tok / p.ps;
     const int phys = p.block_table[(size_t)b * p.P_max + pg];
     if ((unsigned)phys >= (unsigned)p.P_phys) continue;
-    const size_t k_row = (((size_t)l * p.P_phys + phys) * p.Hkv + h) * 2 * p.ps + tok - pg * p.ps;
-    const float4 k = row4<E4M3>(p.pool, k_row, lane, p.scales), v = row4<E4M3>(p.pool, k_row + p.ps, lane, p.scales);
+    const uint32_t mask = visible_mask(v, n, tok);
+    const uint16_t *r = (const uint16_t *)p.pool +
+                        (((((size_t)l * p.P_phys + phys) * p.Hkv + h) * 2 + 1) * p.ps + tok - pg * p.ps) * D + d;
+#pragma unroll 8
+    for (int t = 0; t < BLOCK; ++t) {
+      if (!(mask >> t & 1)) continue;
+      const uint2 w = *(const uint2 *)(r + t * D);
 #pragma unroll
-    for (int i = 0; i < GP; ++i) {
-      float s = (q[i].x * k.x + q[i].y * k.y) + (q[i].z * k.z + q[i].w * k.w);
-#pragma unroll
-      for (int e = 16; e; e >>= 1) s += __shfl_xor_sync(0xffffffffu, s, e);
-      s *= p.scale_log2;
-      const float top = fmaxf(m[i], s), base = top == -INFINITY ? 0.f : top;
-      const float f = exp2f(m[i] - base), w = exp2f(s - base);
-      m[i] = top;
-      z[i] = z[i] * f + w;
-      o[i] = make_float4(o[i].x * f + w * v.x, o[i].y * f + w * v.y, o[i].z * f + w * v.z, o[i].w * f + w * v.w);
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x = (k < 2 ? w.x : w.y) >> 16 * (k & 1);
+        if ((x & 0x7f80u) == 0x7f80u) seen |= (x & 0x7fu ? 4u : x & 0x8000u ? 2u : 1u) << 4 * k;
+      }
     }
+    open &= ~(seen >> 2 | (seen & seen >> 1));
   }
 #pragma unroll
-  for (int i = 0; i < GP; ++i) {
-    *(float4 *)&so[warp][i][4 * lane] = o[i];
-    if (lane == 0) {
-      sm[warp][i] = m[i];
-      sl[warp][i] = z[i];
+  for (int k = 0; k < 4; ++k)
+    if (open >> 4 * k & 1u && seen >> 4 * k & 3u) s[k] = seen >> 4 * k & 1u ? INFINITY : -INFINITY;
+  return sums;
+}
+__device__ __forceinline__ bool any_nan(float4 x) { return isnan(x.x + x.y) || isnan(x.z + x.w); }
+
+/* Four channels of a head of a row: divided by the sum, rounded, written. */
+template <bool E4M3>
+__device__ __forceinline__ void put_out(const AttendCacheParams &p, int b, int l, int h, int head, int d, float4 acc, float r) {
+  if (!E4M3 && any_nan(acc) && r > 0.f) acc = infinite_sums(p, b, l, h, d, acc);
+  uint16_t *dst = p.out + (((size_t)b * p.L + l) * p.Hq + h * p.G + head) * D + d;
+  *(uint2 *)dst = make_uint2(pack_bf16(acc.x * r, acc.y * r), pack_bf16(acc.z * r, acc.w * r));
+}
+
+constexpr size_t attend_smem(int C, int warps, int stages) {
+  return 1024 + (size_t)warps * stages * STEP_BYTES + (2 * warps * GP + 2 * GP) * 4 +
+         (C > 1 ? (MAX_CLUSTER * GP * 2 + GP * D) * 4 : 0) + 128 + warps * stages * 8;
+}
+
+/* A unit is a (sequence, layer, KV head) row, or one of the equal parts of it; C CTAs of NW warps
+ * per unit, a cluster.  The unit's blocks go to the warps in turn, a step at a time; a
+ * warp copies its own steps by TMA (K and V rows, 128-byte swizzle), ST in flight, and computes
+ *   S = K Q^T   rows are tokens, columns the group's heads
+ *   O^T = V^T P^T  rows are channels, summed over the tokens.
+ *
+ * E4M3: codes become f16 on their way from shared memory into the fragments, exactly; the scales are
+ * applied to the 32-bit results, K's to the scores and V's as a block's product is added to O.  A
+ * lane reads 16 bytes of a row at a time, and the fragments' rows and summed dimension are permuted
+ * so that these are what it needs: row g of K's fragments is token g ^ (4 if g is odd), which with the
+ * swizzle keeps 16-byte reads of K (a row's chunks t and t + 4) and of V (chunk g of the rows of
+ * tokens 2t, 2t + 1) free of bank conflicts; V's bytes are paired by token with a byte permutation.
+ *
+ * The weights are taken against a base that follows the running maximum only when a score exceeds
+ * it by SLACK: most steps then need no exchange between lanes and no rescaling. */
+template <int NW, int ST, bool E4M3, bool ONE>
+__global__ void __launch_bounds__(32 * NW)
+    attend_cache_kernel(const __grid_constant__ AttendCacheParams p, const __grid_constant__ CUtensorMap tmap) {
+  constexpr int NB = E4M3 ? 2 : 1;                   // blocks of a step
+  constexpr int PER = 32 / NB;                       // steps whose blocks the lanes hold
+  constexpr int BYTES = STEP_BYTES / NB;             // of a block
+  constexpr int WARP_FLOATS = ST * STEP_BYTES / 4;
+  extern __shared__ uint8_t smem_raw[];
+  float *so = (float *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);   // [NW] the warps' stages, later their O [8][OS]
+  float *sm = so + NW * WARP_FLOATS;                 // [NW][8] exponents of the bases, then sums
+  float *sl = sm + NW * GP;
+  float *fin = sl + NW * GP;                         // [8] final bases, [8] 1 / sums
+  float *xo = fin + 2 * GP;                          // [C][1024 / C] every CTA's part of this one's slice
+  float *xml = xo + (ONE ? 0 : GP * D);              // [C][8][2]
+  float *zero = xml + (ONE ? 0 : MAX_CLUSTER * GP * 2);                     // 128 bytes of zeros
+  uint64_t *full = (uint64_t *)(zero + 32);          // [NW][ST]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int C = ONE ? 1 : p.C, unit = blockIdx.x / C, rank = blockIdx.x - unit * C;
+  const uint32_t ring = smem_u32(so) + warp * ST * STEP_BYTES, bars = smem_u32(full + warp * ST);
+  if (lane < ST) {
+    mbar_init(bars + lane * 8, NB);
+    fence_barrier_init();
+  }
+  if (lane == 0) tma_prefetch_desc(&tmap);
+  if (!E4M3 && warp == 0) zero[lane] = 0.f;
+  __syncthreads();
+  if (!ONE) cluster_arrive();                        // this CTA runs: the others may write its shared memory
+  int b = 0;                                         // the sequence: unit_start[b] <= unit < unit_start[b + 1]
+  for (int hi = p.n_seqs; hi - b > 1;) {
+    const int mid = (b + hi) >> 1;
+    if (p.unit_start[mid] <= unit) b = mid;
+    else hi = mid;
+  }
+  const int lh = p.L * p.Hkv, parts = (p.unit_start[b + 1] - p.unit_start[b]) / lh;
+  const int item = (unit - p.unit_start[b]) / parts, part = unit - p.unit_start[b] - item * parts;
+  const int l = item / p.Hkv, h = item - l * p.Hkv;
+  const int n_tok = p.n_tokens[b];
+  const Visible vis = visible(n_tok, p.window, p.sinks);
+  /* this unit's blocks, in whole steps but for the last */
+  const int steps = (vis.blocks + NB - 1) / NB;
+  const int s0 = (int)((long long)steps * part / parts), s1 = (int)((long long)steps * (part + 1) / parts);
+  const int W = C * NW, w = rank * NW + warp;        // warps of the unit; this one takes steps s0 + w, s0 + w + W, ...
+  const int nt = s1 - s0 > w ? (s1 - s0 - w + W - 1) / W : 0;
+  const size_t q_row = ((size_t)b * p.L + l) * p.Hq + h * p.G;
+  const uint64_t stream = policy_evict_first();
+  const int per_page = p.ps / BLOCK, page_shift = per_page - 1;   // 1 or 2 blocks
+  pdl_wait();
+  pdl_trigger();
+
+  /* The lanes hold the blocks of PER steps: lane i the block i % NB of the steps j = i / NB (mod PER).
+   * A step's page is looked up PER steps ahead, its copy and scales are asked for ST steps ahead. */
+  int phys = -1;
+  uint32_t mask = 0;
+  float ks = 0.f, vs = 0.f;
+  auto block_of = [&](int j) {                       // the lane's block of step j, or -1
+    const int i = (s0 + w + W * j) * NB + (lane & (NB - 1));
+    return j < nt && i < vis.blocks ? (i < vis.head ? i : i - vis.head + vis.tail) : -1;
+  };
+  auto look_up = [&](int j) {
+    const int at = block_of(j);
+    phys = at >= 0 ? p.block_table[(size_t)b * p.P_max + (at >> page_shift)] : -1;
+  };
+  auto issue = [&](int j) {
+    const int at = block_of(j), sub = (at & page_shift) * BLOCK;
+    const uint32_t bar = bars + (j & (ST - 1)) * 8, dst = ring + (j & (ST - 1)) * STEP_BYTES + (lane & (NB - 1)) * BYTES;
+    mask = 0;
+    ks = vs = 0.f;
+    if (at >= 0 && (unsigned)phys < (unsigned)p.P_phys) {
+      mask = visible_mask(vis, n_tok, at * BLOCK);
+      const int row = (l * p.P_phys + phys) * p.Hkv + h;
+      mbar_arrive_expect_tx(bar, BYTES);
+      tma_load_4d(dst, &tmap, 0, sub, 0, row, bar, stream);
+      if (E4M3) {
+        const float *s = p.scales + ((size_t)row * 2 << page_shift) + (at & page_shift);
+        ks = s[0];
+        vs = s[per_page];
+      } else {
+        tma_load_4d(dst + BYTES / 2, &tmap, 64, sub, 0, row, bar, stream);
+      }
+    } else {
+      mbar_arrive(bar);
+    }
+    look_up(j + PER);
+  };
+  look_up(lane / NB);
+  if (lane / NB < ST && lane / NB < nt) issue(lane / NB);
+
+  uint32_t q[8][2];                                  // fragments of head g
+  float qs[2] = {p.scale_log2, p.scale_log2};        // factors of the scores of heads 2t, 2t + 1
+  if (E4M3) {                                        // channels 16 t + 4 i .., 64 + 16 t + 4 i ..
+    uint32_t x[16];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 u = g < p.G ? *((const uint4 *)(p.q + (q_row + g) * D) + 8 * (i >> 1) + 2 * t + (i & 1)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x[4 * i + k] = word(u, k);
+        most = max(most, max(word(u, k) << 16 & 0x7fff0000u, word(u, k) & 0x7fff0000u));
+      }
+    }
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    /* f16 holds them relative to the largest: 2^-e x is below 2^15 */
+    int e = (int)(most >> 23) - 127 - 14;
+    e = most == 0 || most >= 0x7f800000u ? 0 : max(e, -126);
+    const float down = __uint_as_float((127 - e) << 23), up = __uint_as_float((127 + e) << 23);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      q[i >> 1][i & 1] = pack_f16(__uint_as_float(x[i] << 16) * down, __uint_as_float(x[i] & 0xffff0000u) * down);
+    qs[0] *= __shfl_sync(0xffffffffu, up, 8 * t);
+    qs[1] *= __shfl_sync(0xffffffffu, up, 8 * t + 4);
+  } else {                                           // channels 16 i + 2 t, + 1 and + 8, + 9
+    const uint16_t *r = p.q + (q_row + g) * D + 2 * t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      q[i][0] = g < p.G ? *(const uint32_t *)(r + 16 * i) : 0u;
+      q[i][1] = g < p.G ? *(const uint32_t *)(r + 16 * i + 8) : 0u;
+    }
+  }
+  const int mi = lane >> 3, rr = lane & 7;           // ldmatrix: matrix and row of this lane's address
+  const int tok0 = E4M3 ? g ^ (g & 1) << 2 : g;      // the token of row g of the fragments; row g + 8: 8 more
+  const int v0 = 2 * t, v1 = (2 * t + 1) ^ 4;        // E4M3: tokens summed by this lane, and 8 more
+  const uint32_t k_at = tok0 * 128 + ((t ^ (tok0 & 7)) << 4);
+  const uint32_t v_at0 = (BLOCK + v0) * 128 + ((g ^ v0) << 4), v_at1 = (BLOCK + v1) * 128 + ((g ^ v1) << 4);
+  const uint32_t zeros = smem_u32(zero);
+  float m[2] = {-INFINITY, -INFINITY}, z[2] = {0.f, 0.f}, o[8][4];
+  float base[2] = {0.f, 0.f}, lim[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  bool landed = true;
+  int k = 0;
+  for (; k < nt; ++k) {
+    const uint32_t st = ring + (k & (ST - 1)) * STEP_BYTES, bar = bars + (k & (ST - 1)) * 8, parity = k / ST & 1;
+    landed = mbar_try_wait(bar, parity) || wait_copy(bar, parity, p.limit_ns);
+    if (!__all_sync(0xffffffffu, landed)) {
+      landed = false;
+      break;
+    }
+    uint32_t seen[NB];
+    float c[NB][4], vscale[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int from = (k & (PER - 1)) * NB + j;
+      seen[j] = __shfl_sync(0xffffffffu, mask, from);
+      float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f}, kscale = 1.f;
+      if (E4M3) {
+        kscale = __shfl_sync(0xffffffffu, ks, from);
+        vscale[j] = __shfl_sync(0xffffffffu, vs, from);
+        const uint32_t kb = st + j * BYTES + k_at;
+        const uint4 a = lds128(kb), a8 = lds128(kb + 8 * 128), e = lds128(kb ^ 64), e8 = lds128((kb ^ 64) + 8 * 128);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          mma_f16(x, f16_lo(word(a, i)), f16_lo(word(a8, i)), f16_hi(word(a, i)), f16_hi(word(a8, i)), q[i][0], q[i][1], x[0],
+                  x[1], x[2], x[3]);
+          mma_f16(y, f16_lo(word(e, i)), f16_lo(word(e8, i)), f16_hi(word(e, i)), f16_hi(word(e8, i)), q[4 + i][0],
+                  q[4 + i][1], y[0], y[1], y[2], y[3]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint32_t a0, a1, a2, a3;
+          ldmatrix_x4(swz<TILE>(st, (mi & 1) * 8 + rr, i * 16 + (mi >> 1) * 8), a0, a1, a2, a3);
+          mma_bf16(i & 1 ? y : x, a0, a1, a2, a3, q[i][0], q[i][1]);
+        }
+      }
+      /* token tok0, heads 2t, 2t + 1; token tok0 + 8 */
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        c[j][i] = seen[j] >> (tok0 + 8 * (i >> 1)) & 1 && 2 * t + (i & 1) < p.G ? (x[i] + y[i]) * qs[i & 1] * kscale : -INFINITY;
+    }
+    float mx[2] = {fmaxf(c[0][0], c[0][2]), fmaxf(c[0][1], c[0][3])};
+#pragma unroll
+    for (int j = 1; j < NB; ++j) {
+      mx[0] = fmaxf(mx[0], fmaxf(c[j][0], c[j][2]));
+      mx[1] = fmaxf(mx[1], fmaxf(c[j][1], c[j][3]));
+    }
+    if (__any_sync(0xffffffffu, mx[0] > lim[0] || mx[1] > lim[1])) {
+#pragma unroll
+      for (int s = 4; s < 32; s <<= 1)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], s));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float last = m[i];                     // -inf: nothing to rescale
+        m[i] = fmaxf(m[i], mx[i]);
+        const float alpha = ex2(last - max_base(m[i]));
+        base[i] = max_base(m[i]) - (E4M3 ? LIFT : 0.f);
+        lim[i] = m[i] + SLACK;
+        z[i] *= alpha;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          o[j][i] *= alpha;
+          o[j][2 + i] *= alpha;
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      float x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = ex2(c[j][i] - base[i & 1]);
+      z[0] += x[0] + x[2];
+      z[1] += x[1] + x[3];
+      if (E4M3) {
+        const uint32_t b0 = movmatrix_trans(pack_f16(x[0], x[1])), b1 = movmatrix_trans(pack_f16(x[2], x[3]));
+        const uint32_t vb = st + j * BYTES;
+        uint4 r0 = lds128(vb + v_at0), r1 = lds128(vb + v_at1), r2 = lds128(vb + v_at0 + 8 * 128),
+              r3 = lds128(vb + v_at1 + 8 * 128);
+        if (seen[j] != 0xffffu) {                    // what invisible tokens hold may be NaN
+          const uint4 none = make_uint4(0, 0, 0, 0);
+          if (!(seen[j] >> v0 & 1)) r0 = none;
+          if (!(seen[j] >> v1 & 1)) r1 = none;
+          if (!(seen[j] >> v0 & 0x100)) r2 = none;
+          if (!(seen[j] >> v1 & 0x100)) r3 = none;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {                // channels 16 g + 2 i, + 1
+          const int sel = i & 1 ? 0x7362 : 0x5140;
+          const uint32_t lo = __byte_perm(word(r0, i >> 1), word(r1, i >> 1), sel);
+          const uint32_t hi = __byte_perm(word(r2, i >> 1), word(r3, i >> 1), sel);
+          float d[4];
+          mma_f16(d, f16_lo(lo), f16_hi(lo), f16_lo(hi), f16_hi(hi), b0, b1, 0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][e] = fmaf(d[e], vscale[j], o[i][e]);
+        }
+      } else {
+        uint32_t hi[2], lo[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t u = pack_bf16(x[2 * i], x[2 * i + 1]);
+          hi[i] = movmatrix_trans(u);
+          lo[i] = movmatrix_trans(
+              pack_bf16(x[2 * i] - __uint_as_float(u << 16), x[2 * i + 1] - __uint_as_float(u & 0xffff0000u)));
+        }
+        /* rows of invisible tokens, whatever they hold: zeros */
+        const int vr = (mi >> 1) * 8 + rr;
+        const bool in = seen[j] >> vr & 1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {                // channels 16 i + g, + 8
+          uint32_t a0, a1, a2, a3;
+          ldmatrix_x4_trans(in ? swz<TILE>(st, BLOCK + vr, i * 16 + (mi & 1) * 8) : zeros, a0, a1, a2, a3);
+          mma_bf16(o[i], a0, a1, a2, a3, hi[0], hi[1]);
+          mma_bf16(o[i], a0, a1, a2, a3, lo[0], lo[1]);
+        }
+      }
+    }
+    __syncwarp();
+    if (k + ST < nt && lane / NB == (k + ST) % PER) {   // refill the stage: its reads come before the copy
+      fence_proxy_async_smem();
+      issue(k + ST);
+    }
+  }
+  if (!landed) {                                     // what is in flight must land before the stages are reused
+    for (int j = k; j < min(k + ST, nt); ++j) wait_copy(bars + (j & (ST - 1)) * 8, j / ST & 1, DRAIN_LIMIT_NS);
+    z[0] = z[1] = NAN;
+  }
+#pragma unroll
+  for (int s = 4; s < 32; s <<= 1)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) z[i] += __shfl_xor_sync(0xffffffffu, z[i], s);
+  if (g == 0)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      sm[warp * GP + 2 * t + i] = m[i] - (E4M3 ? LIFT : 0.f);
+      sl[warp * GP + 2 * t + i] = z[i];
+    }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int d = E4M3 ? 16 * g + 2 * i + (e >> 1) : 16 * i + g + 8 * (e >> 1);
+      so[warp * WARP_FLOATS + (2 * t + (e & 1)) * OS + d] = o[i][e];
+    }
+  __syncthreads();
+  /* the CTA's sums: 4 channels of a head per thread, 8 / NW heads per warp */
+  const int slice = GP * D / C;
+  float4 acc[GP / NW];
+  float top[GP / NW], sum[GP / NW];
+#pragma unroll
+  for (int i = 0; i < GP / NW; ++i) {
+    const int head = warp + i * NW;
+    top[i] = -INFINITY;
+#pragma unroll
+    for (int y = 0; y < NW; ++y) top[i] = fmaxf(top[i], sm[y * GP + head]);
+    const float to = max_base(top[i]);
+    sum[i] = 0.f;
+    acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int y = 0; y < NW; ++y) {
+      const float f = ex2(sm[y * GP + head] - to);
+      const float4 e = *(const float4 *)&so[y * WARP_FLOATS + head * OS + 4 * lane];
+      sum[i] += f * sl[y * GP + head];
+      acc[i].x += f * e.x;
+      acc[i].y += f * e.y;
+      acc[i].z += f * e.z;
+      acc[i].w += f * e.w;
+    }
+  }
+  float *partial = p.partials + (size_t)(p.part_start[b] + unit - p.unit_start[b]) * PARTIAL;   // where parts > 1
+  if (ONE) {
+#pragma unroll
+    for (int i = 0; i < GP / NW; ++i) {
+      const int head = warp + i * NW;
+      if (parts > 1) {
+        *(float4 *)(partial + head * D + 4 * lane) = acc[i];
+        if (lane == 0) {
+          partial[GP * D + head] = top[i];
+          partial[GP * D + GP + head] = sum[i];
+        }
+      } else if (head < p.G) {
+        put_out<E4M3>(p, b, l, h, head, 4 * lane, acc[i], inverse(sum[i]));
+        if (p.lse && lane == 0) p.lse[q_row + head] = logarithm(max_base(top[i]), sum[i]);
+      }
+    }
+    return;
+  }
+  cluster_wait();                                    // every CTA runs
+#pragma unroll
+  for (int i = 0; i < GP / NW; ++i) {
+    const int head = warp + i * NW, e = head * D + 4 * lane, to = e / slice;
+    st_cluster_v4(cluster_map(smem_u32(xo + rank * slice + e - to * slice), to), acc[i].x, acc[i].y, acc[i].z, acc[i].w);
+    if (lane < C) st_cluster_v2(cluster_map(smem_u32(xml + (rank * GP + head) * 2), lane), top[i], sum[i]);
+  }
+  cluster_arrive();
+  cluster_wait();
+  if (threadIdx.x < GP) {
+    const int head = threadIdx.x;
+    float most = -INFINITY, s = 0.f;
+    for (int y = 0; y < C; ++y) most = fmaxf(most, xml[(y * GP + head) * 2]);
+    const float to = max_base(most);
+    for (int y = 0; y < C; ++y) s += ex2(xml[(y * GP + head) * 2] - to) * xml[(y * GP + head) * 2 + 1];
+    fin[head] = to;
+    fin[GP + head] = inverse(s);
+    if (rank == 0) {
+      if (parts > 1) {
+        partial[GP * D + head] = most;
+        partial[GP * D + GP + head] = s;
+      } else if (p.lse && head < p.G) {
+        p.lse[q_row + head] = logarithm(to, s);
+      }
     }
   }
   __syncthreads();
-  if (warp >= p.G) return;
-  float top = -INFINITY, sum = 0.f;
-  for (int y = 0; y < WARPS; ++y) top = fmaxf(top, sm[y][warp]);
-  const float base = top == -INFINITY ? 0.f : top;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int y = 0; y < WARPS; ++y) {
-    const float f = exp2f(sm[y][warp] - base);
-    const float4 e = *(const float4 *)&so[y][warp][4 * lane];
-    sum += f * sl[y][warp];
-    acc = make_float4(acc.x + f * e.x, acc.y + f * e.y, acc.z + f * e.z, acc.w + f * e.w);
+  for (int e = threadIdx.x * 4; e < slice; e += 32 * NW * 4) {
+    const int at_e = rank * slice + e, head = at_e / D;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < C; ++i) {
+      const float f = ex2(xml[(i * GP + head) * 2] - fin[head]);
+      const float4 x = *(const float4 *)&xo[i * slice + e];
+      y.x += f * x.x;
+      y.y += f * x.y;
+      y.z += f * x.z;
+      y.w += f * x.w;
+    }
+    if (parts > 1)
+      *(float4 *)(partial + at_e) = y;
+    else if (head < p.G)
+      put_out<E4M3>(p, b, l, h, head, at_e - head * D, y, fin[GP + head]);
   }
-  const float r = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;   // no token: zeros; NaN stays
-  *(uint2 *)(p.out + (q_row + warp) * D + 4 * lane) =
-      make_uint2(pack_bf16(acc.x * r, acc.y * r), pack_bf16(acc.z * r, acc.w * r));
-  if (p.lse && lane == 0)
-    p.lse[q_row + warp] = sum == 0.f ? -INFINITY : 0.69314718f * (base + log2f(sum));
+}
+
+/* The parts of split rows together: a block per row, a warp per head. */
+template <bool E4M3>
+__global__ void __launch_bounds__(32 * GP) attend_join_kernel(const __grid_constant__ AttendCacheParams p) {
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31, head = threadIdx.x >> 5, b = blockIdx.y;
+  const int lh = p.L * p.Hkv, parts = (p.unit_start[b + 1] - p.unit_start[b]) / lh;
+  if (parts <= 1 || head >= p.G) return;
+  const int item = blockIdx.x, l = item / p.Hkv, h = item - l * p.Hkv;
+  const float *from = p.partials + (size_t)(p.part_start[b] + item * parts) * PARTIAL;
+  float top = -INFINITY, sum = 0.f;
+  for (int y = lane; y < parts; y += 32) top = fmaxf(top, from[(size_t)y * PARTIAL + GP * D + head]);
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  const float base = max_base(top);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int y = 0; y < parts; ++y) {
+    const float *x = from + (size_t)y * PARTIAL;
+    const float f = ex2(x[GP * D + head] - base);
+    const float4 e = *(const float4 *)(x + head * D + 4 * lane);
+    sum += f * x[GP * D + GP + head];
+    acc.x += f * e.x;
+    acc.y += f * e.y;
+    acc.z += f * e.z;
+    acc.w += f * e.w;
+  }
+  put_out<E4M3>(p, b, l, h, head, 4 * lane, acc, inverse(sum));
+  if (p.lse && lane == 0) p.lse[((size_t)b * p.L + l) * p.Hq + h * p.G + head] = logarithm(base, sum);
+}
+
+struct Form {
+  int C = 1, warps = 4;
+};
+
+/* How many CTAs and warps per unit, and how many units per row. */
+Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
+  const int NB = e4m3 ? 2 : 1, lh = p.L * p.Hkv;
+  constexpr int SMS = 152, SLOTS = 3 * SMS;
+  int steps[MD_MAX_BATCH], most = 0;
+  long long total = 0;
+  for (int b = 0; b < p.n_seqs; ++b) {
+    steps[b] = (visible(p.n_tokens[b], p.window, p.sinks).blocks + NB - 1) / NB;
+    most = std::max(most, steps[b]);
+    total += (long long)steps[b] * lh;
+  }
+  Form f;
+  const long long rows = (long long)p.n_seqs * lh;
+  while (f.C < MAX_CLUSTER && rows * f.C * 2 <= SLOTS && f.C * f.warps < most) f.C *= 2;
+  const long long unit = std::max<long long>(64, total / (SLOTS / f.C * 4) + 1);   // steps of a unit
+  p.unit_start[0] = 0;
+  int partials = 0;
+  for (int b = 0; b < p.n_seqs; ++b) {
+    long long parts = workspace ? std::max<long long>(1, steps[b] / unit) : 1;
+    if (partials + parts * lh > MAX_PARTIALS) parts = 1;
+    p.part_start[b] = partials;
+    if (parts > 1) partials += (int)parts * lh;
+    p.unit_start[b + 1] = p.unit_start[b] + (int)parts * lh;
+  }
+  return f;
+}
+
+template <int NW, int ST, bool E4M3, bool ONE>
+cudaError_t launch_attend(const AttendCacheParams &p, const CUtensorMap &tmap, cudaStream_t s) {
+  constexpr int which = ATTR_ATTEND_CACHE + (E4M3 ? 1 : 0) + (ONE ? 2 : 0) + (NW == 8 ? 4 : 0);
+  const auto kernel = attend_cache_kernel<NW, ST, E4M3, ONE>;
+  const cudaError_t e = once_per_device<which>([&] {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)attend_smem(ONE ? 1 : MAX_CLUSTER, NW, ST));
+    return e != cudaSuccess || ONE ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  });
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.unit_start[p.n_seqs] * p.C));
+  cfg.blockDim = dim3(32 * NW);
+  cfg.dynamicSmemBytes = attend_smem(p.C, NW, ST);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.C;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = ONE ? 1 : 2;
+  return cudaLaunchKernelEx(&cfg, kernel, p, tmap);
+}
+
+/* Blocks of K and V rows of a pool in eight bits: 128 bytes x 16 rows x (K, V), swizzled. */
+bool encode_block_map(void *encode, CUtensorMap *m, const void *pool, size_t items, int ps) {
+  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)ps, 2, (cuuint64_t)items};
+  const cuuint64_t strides[3] = {(cuuint64_t)D, (cuuint64_t)D * ps, (cuuint64_t)D * ps * 2};
+  const cuuint32_t box[4] = {(cuuint32_t)D, BLOCK, 2, 1}, one[4] = {1, 1, 1, 1};
+  return ((decltype(&cuTensorMapEncodeTiled))encode)(
+             m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, (void *)pool, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool E4M3>
+cudaError_t run(AttendCacheParams &p, const CUtensorMap &tmap, bool workspace, cudaStream_t s) {
+  const Form f = attend_form(p, E4M3, workspace);
+  p.C = f.C;
+  cudaError_t e = f.C > 1 ? launch_attend<4, 2, E4M3, false>(p, tmap, s) : launch_attend<4, 2, E4M3, true>(p, tmap, s);
+  const int lh = p.L * p.Hkv;
+  if (e == cudaSuccess && p.unit_start[p.n_seqs] > p.n_seqs * lh)
+    e = launch_pdl(attend_join_kernel<E4M3>, dim3(lh, p.n_seqs), 32 * GP, 0, s, p);
+  return e;
 }
 
 }  // namespace
@@ -139,10 +672,18 @@ MD_API md_status md_attend_cache(const md_attend_cache_args *args) {
   p.scales = a.scales_dev;
   p.out = (uint16_t *)a.out_dev;
   p.lse = a.lse_dev;
+  p.partials = (float *)a.workspace_dev;
   p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
+  p.limit_ns = 2000000000LL;
   p.window = a.window < 0 ? INT32_MAX : a.window;
   p.sinks = a.sinks;
-  const dim3 grid((unsigned)(a.batch * a.num_layers * a.num_kv_heads));
-  const auto kernel = e4m3 ? attend_cache_kernel<true> : attend_cache_kernel<false>;
-  return launch_pdl(kernel, grid, 32 * WARPS, 0, (cudaStream_t)a.stream, p) == cudaSuccess ? MD_OK : MD_ERR_CUDA;
+  void *encode = tile_encoder();
+  CUtensorMap tmap;
+  const size_t items = (size_t)a.num_layers * a.num_phys_pages * a.num_kv_heads;
+  if (!encode || !(e4m3 ? encode_block_map(encode, &tmap, a.pool_dev, items, a.page_size)
+                        : encode_tile_map(encode, &tmap, (void *)a.pool_dev, items * 2 * a.page_size, a.page_size)))
+    return MD_ERR_CUDA;
+  const cudaStream_t s = (cudaStream_t)a.stream;
+  const bool workspace = a.workspace_dev != nullptr;
+  return (e4m3 ? run<true>(p, tmap, workspace, s) : run<false>(p, tmap, workspace, s)) == cudaSuccess ? MD_OK : MD_ERR_CUDA;
 }
