@@ -107,7 +107,12 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   return r;
 }
 __device__ __forceinline__ uint32_t word(const uint4 &x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
-
+/* Two 16x16 matrices of bytes, transposed: lane (g, t) gets columns g and g + 8 of each at rows 4t .. 4t + 3. */
+__device__ __forceinline__ void ldmatrix_b8_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
 /* Sums over channels d .. d + 3 of bf16 V rows with finite weights, of which some came out NaN:
  * infinite where the row's visible tokens have infinite values of one sign and no NaN, as
  * every weight is above 0 (the two terms of a weight may be 0 or cancel, and their products with
@@ -165,11 +170,11 @@ constexpr size_t attend_smem(int C, int warps, int stages) {
  *   O^T = V^T P^T  rows are channels, summed over the tokens.
  *
  * E4M3: codes become f16 on their way from shared memory into the fragments, exactly; the scales are
- * applied to the 32-bit results, K's to the scores and V's as a block's product is added to O.  A
- * lane reads 16 bytes of a row at a time, and the fragments' rows and summed dimension are permuted
- * so that these are what it needs: row g of K's fragments is token g ^ (4 if g is odd), which with the
- * swizzle keeps 16-byte reads of K (a row's chunks t and t + 4) and of V (chunk g of the rows of
- * tokens 2t, 2t + 1) free of bank conflicts; V's bytes are paired by token with a byte permutation.
+ * applied to the 32-bit results, K's to the scores and V's as a block's product is added to O.  K is
+ * read 16 bytes of a row at a time (the summed channels are permuted alike in the queries), V by
+ * transposed loads, four tokens of a channel per register.  Row g of the scores is token
+ * t(g) = g ^ (4 if g is odd), row g + 8 token 8 + (t(g) ^ 4): with the swizzle, neither meets a bank
+ * twice, and the weights lie where V's registers want them.
  *
  * The weights are taken against a base that follows the running maximum only when a score exceeds
  * it by SLACK: most steps then need no exchange between lanes and no rescaling. */
@@ -182,13 +187,13 @@ __global__ void __launch_bounds__(32 * NW)
   constexpr int WARP_FLOATS = ST * STEP_BYTES / 4;
   extern __shared__ uint8_t smem_raw[];
   float *so = (float *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);   // [NW] the warps' stages, later their O [8][OS]
-  float *sm = so + NW * WARP_FLOATS;                 // [NW][8] exponents of the bases, then sums
+  float *zero = so + NW * WARP_FLOATS;               // 128 bytes of zeros
+  float *sm = zero + 32;                             // [NW][8] exponents of the bases, then sums
   float *sl = sm + NW * GP;
   float *fin = sl + NW * GP;                         // [8] final bases, [8] 1 / sums
   float *xo = fin + 2 * GP;                          // [C][1024 / C] every CTA's part of this one's slice
   float *xml = xo + (ONE ? 0 : GP * D);              // [C][8][2]
-  float *zero = xml + (ONE ? 0 : MAX_CLUSTER * GP * 2);                     // 128 bytes of zeros
-  uint64_t *full = (uint64_t *)(zero + 32);          // [NW][ST]
+  uint64_t *full = (uint64_t *)(xml + (ONE ? 0 : MAX_CLUSTER * GP * 2));    // [NW][ST]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int C = ONE ? 1 : p.C, unit = blockIdx.x / C, rank = blockIdx.x - unit * C;
   const uint32_t ring = smem_u32(so) + warp * ST * STEP_BYTES, bars = smem_u32(full + warp * ST);
@@ -197,7 +202,7 @@ __global__ void __launch_bounds__(32 * NW)
     fence_barrier_init();
   }
   if (lane == 0) tma_prefetch_desc(&tmap);
-  if (!E4M3 && warp == 0) zero[lane] = 0.f;
+  if (warp == 0) zero[lane] = 0.f;
   __syncthreads();
   if (!ONE) cluster_arrive();                        // this CTA runs: the others may write its shared memory
   int b = 0;                                         // the sequence: unit_start[b] <= unit < unit_start[b + 1]
@@ -222,43 +227,49 @@ __global__ void __launch_bounds__(32 * NW)
   pdl_wait();
   pdl_trigger();
 
-  /* The lanes hold the blocks of PER steps: lane i the block i % NB of the steps j = i / NB (mod PER).
-   * A step's page is looked up PER steps ahead, its copy and scales are asked for ST steps ahead. */
-  int phys = -1;
-  uint32_t mask = 0;
-  float ks = 0.f, vs = 0.f;
-  auto block_of = [&](int j) {                       // the lane's block of step j, or -1
-    const int i = (s0 + w + W * j) * NB + (lane & (NB - 1));
+  /* The lanes hold the blocks of a list of PER steps: lane i the block i % NB of its step i / NB.  Of
+   * the list after it, the pages are looked up when a list begins, and the scales asked for in its middle. */
+  auto block_of = [&](int list) {                    // the lane's block, or -1
+    const int j = list + lane / NB, i = (s0 + w + W * j) * NB + (lane & (NB - 1));
     return j < nt && i < vis.blocks ? (i < vis.head ? i : i - vis.head + vis.tail) : -1;
   };
-  auto look_up = [&](int j) {
-    const int at = block_of(j);
-    phys = at >= 0 ? p.block_table[(size_t)b * p.P_max + (at >> page_shift)] : -1;
+  auto look_up = [&](int list) {
+    const int at = block_of(list);
+    return at >= 0 ? p.block_table[(size_t)b * p.P_max + (at >> page_shift)] : -1;
   };
-  auto issue = [&](int j) {
-    const int at = block_of(j), sub = (at & page_shift) * BLOCK;
-    const uint32_t bar = bars + (j & (ST - 1)) * 8, dst = ring + (j & (ST - 1)) * STEP_BYTES + (lane & (NB - 1)) * BYTES;
-    mask = 0;
-    ks = vs = 0.f;
+  struct Held {
+    int row;                                         // of the tensor map
+    uint32_t mask;                                   // visible tokens; in the upper half the block's place in its page
+    float ks, vs;
+  };
+  auto open = [&](int list, int phys) {
+    Held x = {0, 0, 0.f, 0.f};
+    const int at = block_of(list);
     if (at >= 0 && (unsigned)phys < (unsigned)p.P_phys) {
-      mask = visible_mask(vis, n_tok, at * BLOCK);
-      const int row = (l * p.P_phys + phys) * p.Hkv + h;
-      mbar_arrive_expect_tx(bar, BYTES);
-      tma_load_4d(dst, &tmap, 0, sub, 0, row, bar, stream);
+      x.row = (l * p.P_phys + phys) * p.Hkv + h;
+      x.mask = visible_mask(vis, n_tok, at * BLOCK) | (uint32_t)(at & page_shift) << 16;
       if (E4M3) {
-        const float *s = p.scales + ((size_t)row * 2 << page_shift) + (at & page_shift);
-        ks = s[0];
-        vs = s[per_page];
-      } else {
-        tma_load_4d(dst + BYTES / 2, &tmap, 64, sub, 0, row, bar, stream);
+        const float *s = p.scales + ((size_t)x.row * 2 << page_shift) + (at & page_shift);
+        x.ks = s[0];
+        x.vs = s[per_page];
       }
+    }
+    return x;
+  };
+  auto copy = [&](int j, const Held &x) {            // the lanes of step j
+    const uint32_t bar = bars + (j & (ST - 1)) * 8, dst = ring + (j & (ST - 1)) * STEP_BYTES + (lane & (NB - 1)) * BYTES;
+    if (x.mask) {
+      const int sub = (x.mask >> 16) * BLOCK;
+      mbar_arrive_expect_tx(bar, BYTES);
+      tma_load_4d(dst, &tmap, 0, sub, 0, x.row, bar, stream);
+      if (!E4M3) tma_load_4d(dst + BYTES / 2, &tmap, 64, sub, 0, x.row, bar, stream);
     } else {
       mbar_arrive(bar);
     }
-    look_up(j + PER);
   };
-  look_up(lane / NB);
-  if (lane / NB < ST && lane / NB < nt) issue(lane / NB);
+  int phys = look_up(0);
+  Held held = open(0, phys), next = {0, 0, 0.f, 0.f};
+  if (lane / NB < ST && lane / NB < nt) copy(lane / NB, held);
 
   uint32_t q[8][2];                                  // fragments of head g
   float qs[2] = {p.scale_log2, p.scale_log2};        // factors of the scores of heads 2t, 2t + 1
@@ -293,11 +304,14 @@ __global__ void __launch_bounds__(32 * NW)
       q[i][1] = g < p.G ? *(const uint32_t *)(r + 16 * i + 8) : 0u;
     }
   }
-  const int mi = lane >> 3, rr = lane & 7;           // ldmatrix: matrix and row of this lane's address
-  const int tok0 = E4M3 ? g ^ (g & 1) << 2 : g;      // the token of row g of the fragments; row g + 8: 8 more
-  const int v0 = 2 * t, v1 = (2 * t + 1) ^ 4;        // E4M3: tokens summed by this lane, and 8 more
-  const uint32_t k_at = tok0 * 128 + ((t ^ (tok0 & 7)) << 4);
-  const uint32_t v_at0 = (BLOCK + v0) * 128 + ((g ^ v0) << 4), v_at1 = (BLOCK + v1) * 128 + ((g ^ v1) << 4);
+  /* tokens of rows g and g + 8 of the scores; the rows whose address this lane gives to ldmatrix */
+  const int tok0 = E4M3 ? g ^ (g & 1) << 2 : g, tok1 = E4M3 ? 8 + (tok0 ^ 4) : g + 8;
+  const int mi = lane >> 3, rr = lane & 7;
+  const int pair = (lane & 15) >> 2 << 1 | (lane & 1), pair_tok = pair ^ (pair & 1) << 2;
+  const int v_row = E4M3 ? (lane & 2 ? 8 + (pair_tok ^ 4) : pair_tok) : (mi >> 1) * 8 + rr;
+  const uint32_t k_lane = E4M3 ? tok0 * 128 + ((t ^ tok0) << 4) : ((mi & 1) * 8 + rr) * 128 + (((mi >> 1) ^ rr) << 4);
+  const uint32_t k_lane8 = tok1 * 128 + ((t ^ (tok1 & 7)) << 4);      // E4M3
+  const uint32_t v_lane = (BLOCK + v_row) * 128 + (((E4M3 ? lane >> 4 : mi & 1) ^ (v_row & 7)) << 4);
   const uint32_t zeros = smem_u32(zero);
   float m[2] = {-INFINITY, -INFINITY}, z[2] = {0.f, 0.f}, o[8][4];
   float base[2] = {0.f, 0.f}, lim[2] = {-INFINITY, -INFINITY};
@@ -306,24 +320,42 @@ __global__ void __launch_bounds__(32 * NW)
   bool landed = true;
   int k = 0;
   for (; k < nt; ++k) {
+    if ((k & (PER / 2 - 1)) == 0) {
+      if (k & (PER / 2)) {
+        next = open((k & ~(PER - 1)) + PER, phys);
+      } else {
+        if (k) held = next;
+        phys = look_up(k + PER);
+      }
+    }
+    uint32_t seen[NB];
+    float kscale[NB], vscale[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int from = (k & (PER - 1)) * NB + j;
+      seen[j] = __shfl_sync(0xffffffffu, held.mask, from) & 0xffffu;
+      if (E4M3) {
+        kscale[j] = __shfl_sync(0xffffffffu, held.ks, from);
+        vscale[j] = __shfl_sync(0xffffffffu, held.vs, from);
+      }
+    }
     const uint32_t st = ring + (k & (ST - 1)) * STEP_BYTES, bar = bars + (k & (ST - 1)) * 8, parity = k / ST & 1;
     landed = mbar_try_wait(bar, parity) || wait_copy(bar, parity, p.limit_ns);
     if (!__all_sync(0xffffffffu, landed)) {
       landed = false;
       break;
     }
-    uint32_t seen[NB];
-    float c[NB][4], vscale[NB];
+    float c[NB][4];
+    uint32_t v[NB][4][4];                            // E4M3: V's codes
+    uint32_t v_at[NB];                               // rows of invisible tokens, whatever they hold: zeros
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      const int from = (k & (PER - 1)) * NB + j;
-      seen[j] = __shfl_sync(0xffffffffu, mask, from);
-      float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f}, kscale = 1.f;
+      float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint32_t kb = st + j * BYTES + k_lane;
+      v_at[j] = seen[j] >> v_row & 1 ? st + j * BYTES + v_lane : zeros;
       if (E4M3) {
-        kscale = __shfl_sync(0xffffffffu, ks, from);
-        vscale[j] = __shfl_sync(0xffffffffu, vs, from);
-        const uint32_t kb = st + j * BYTES + k_at;
-        const uint4 a = lds128(kb), a8 = lds128(kb + 8 * 128), e = lds128(kb ^ 64), e8 = lds128((kb ^ 64) + 8 * 128);
+        const uint32_t kb8 = st + j * BYTES + k_lane8;
+        const uint4 a = lds128(kb), a8 = lds128(kb8), e = lds128(kb ^ 64), e8 = lds128(kb8 ^ 64);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           mma_f16(x, f16_lo(word(a, i)), f16_lo(word(a8, i)), f16_hi(word(a, i)), f16_hi(word(a8, i)), q[i][0], q[i][1], x[0],
@@ -331,18 +363,26 @@ __global__ void __launch_bounds__(32 * NW)
           mma_f16(y, f16_lo(word(e, i)), f16_lo(word(e8, i)), f16_hi(word(e, i)), f16_hi(word(e8, i)), q[4 + i][0],
                   q[4 + i][1], y[0], y[1], y[2], y[3]);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ldmatrix_b8_trans(v_at[j] ^ i << 5, v[j][i]);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           uint32_t a0, a1, a2, a3;
-          ldmatrix_x4(swz<TILE>(st, (mi & 1) * 8 + rr, i * 16 + (mi >> 1) * 8), a0, a1, a2, a3);
+          ldmatrix_x4((kb ^ (i & 3) << 5) + (i >> 2) * (BYTES / 2), a0, a1, a2, a3);
           mma_bf16(i & 1 ? y : x, a0, a1, a2, a3, q[i][0], q[i][1]);
         }
       }
-      /* token tok0, heads 2t, 2t + 1; token tok0 + 8 */
+      /* heads 2t, 2t + 1 of tokens tok0 (0, 1) and tok1 (2, 3) */
+      const float f0 = E4M3 ? qs[0] * kscale[j] : qs[0], f1 = E4M3 ? qs[1] * kscale[j] : qs[1];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        c[j][i] = seen[j] >> (tok0 + 8 * (i >> 1)) & 1 && 2 * t + (i & 1) < p.G ? (x[i] + y[i]) * qs[i & 1] * kscale : -INFINITY;
+      for (int i = 0; i < 4; ++i) c[j][i] = (x[i] + y[i]) * (i & 1 ? f1 : f0);
+      if (seen[j] != 0xffffu) {
+        const bool in0 = seen[j] >> tok0 & 1, in1 = seen[j] >> tok1 & 1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(i < 2 ? in0 : in1)) c[j][i] = -INFINITY;
+      }
     }
     float mx[2] = {fmaxf(c[0][0], c[0][2]), fmaxf(c[0][1], c[0][3])};
 #pragma unroll
@@ -379,23 +419,11 @@ __global__ void __launch_bounds__(32 * NW)
       z[1] += x[1] + x[3];
       if (E4M3) {
         const uint32_t b0 = movmatrix_trans(pack_f16(x[0], x[1])), b1 = movmatrix_trans(pack_f16(x[2], x[3]));
-        const uint32_t vb = st + j * BYTES;
-        uint4 r0 = lds128(vb + v_at0), r1 = lds128(vb + v_at1), r2 = lds128(vb + v_at0 + 8 * 128),
-              r3 = lds128(vb + v_at1 + 8 * 128);
-        if (seen[j] != 0xffffu) {                    // what invisible tokens hold may be NaN
-          const uint4 none = make_uint4(0, 0, 0, 0);
-          if (!(seen[j] >> v0 & 1)) r0 = none;
-          if (!(seen[j] >> v1 & 1)) r1 = none;
-          if (!(seen[j] >> v0 & 0x100)) r2 = none;
-          if (!(seen[j] >> v1 & 0x100)) r3 = none;
-        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {                // channels 16 g + 2 i, + 1
-          const int sel = i & 1 ? 0x7362 : 0x5140;
-          const uint32_t lo = __byte_perm(word(r0, i >> 1), word(r1, i >> 1), sel);
-          const uint32_t hi = __byte_perm(word(r2, i >> 1), word(r3, i >> 1), sel);
+        for (int i = 0; i < 8; ++i) {                // channels 16 i + g, + 8
+          const uint32_t c0 = v[j][i >> 1][2 * (i & 1)], c8 = v[j][i >> 1][2 * (i & 1) + 1];
           float d[4];
-          mma_f16(d, f16_lo(lo), f16_hi(lo), f16_lo(hi), f16_hi(hi), b0, b1, 0.f, 0.f, 0.f, 0.f);
+          mma_f16(d, f16_lo(c0), f16_lo(c8), f16_hi(c0), f16_hi(c8), b0, b1, 0.f, 0.f, 0.f, 0.f);
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[i][e] = fmaf(d[e], vscale[j], o[i][e]);
         }
@@ -408,22 +436,20 @@ __global__ void __launch_bounds__(32 * NW)
           lo[i] = movmatrix_trans(
               pack_bf16(x[2 * i] - __uint_as_float(u << 16), x[2 * i + 1] - __uint_as_float(u & 0xffff0000u)));
         }
-        /* rows of invisible tokens, whatever they hold: zeros */
-        const int vr = (mi >> 1) * 8 + rr;
-        const bool in = seen[j] >> vr & 1;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {                // channels 16 i + g, + 8
           uint32_t a0, a1, a2, a3;
-          ldmatrix_x4_trans(in ? swz<TILE>(st, BLOCK + vr, i * 16 + (mi & 1) * 8) : zeros, a0, a1, a2, a3);
+          ldmatrix_x4_trans((v_at[j] ^ (i & 3) << 5) + (v_at[j] == zeros ? 0 : (i >> 2) * (BYTES / 2)), a0, a1, a2, a3);
           mma_bf16(o[i], a0, a1, a2, a3, hi[0], hi[1]);
           mma_bf16(o[i], a0, a1, a2, a3, lo[0], lo[1]);
         }
       }
     }
     __syncwarp();
-    if (k + ST < nt && lane / NB == (k + ST) % PER) {   // refill the stage: its reads come before the copy
+    const int j = k + ST;
+    if (j < nt && lane / NB == (j & (PER - 1))) {    // refill the stage: its reads come before the copy
       fence_proxy_async_smem();
-      issue(k + ST);
+      copy(j, (k ^ j) & PER ? next : held);
     }
   }
   if (!landed) {                                     // what is in flight must land before the stages are reused
@@ -445,8 +471,7 @@ __global__ void __launch_bounds__(32 * NW)
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int d = E4M3 ? 16 * g + 2 * i + (e >> 1) : 16 * i + g + 8 * (e >> 1);
-      so[warp * WARP_FLOATS + (2 * t + (e & 1)) * OS + d] = o[i][e];
+      so[warp * WARP_FLOATS + (2 * t + (e & 1)) * OS + 16 * i + g + 8 * (e >> 1)] = o[i][e];
     }
   __syncthreads();
   /* the CTA's sums: 4 channels of a head per thread, 8 / NW heads per warp */
