@@ -158,9 +158,10 @@ __device__ __forceinline__ void put_out(const AttendCacheParams &p, int b, int l
   *(uint2 *)dst = make_uint2(pack_bf16(acc.x * r, acc.y * r), pack_bf16(acc.z * r, acc.w * r));
 }
 
-constexpr size_t attend_smem(int C, int warps, int stages) {
-  return 1024 + (size_t)warps * stages * STEP_BYTES + (2 * warps * GP + 2 * GP) * 4 +
-         (C > 1 ? (MAX_CLUSTER * GP * 2 + GP * D) * 4 : 0) + 128 + warps * stages * 8;
+constexpr int ST = 2;                        // steps of a warp in flight
+constexpr size_t attend_smem(int C, int warps) {
+  return 1024 + (size_t)warps * ST * STEP_BYTES + (2 * warps * GP + 2 * GP) * 4 +
+         (C > 1 ? (MAX_CLUSTER * GP * 2 + GP * D) * 4 : 0) + 128 + warps * ST * 8;
 }
 
 /* A unit is a (sequence, layer, KV head) row, or one of the equal parts of it; C CTAs of NW warps
@@ -178,8 +179,8 @@ constexpr size_t attend_smem(int C, int warps, int stages) {
  *
  * The weights are taken against a base that follows the running maximum only when a score exceeds
  * it by SLACK: most steps then need no exchange between lanes and no rescaling. */
-template <int NW, int ST, bool E4M3, bool ONE>
-__global__ void __launch_bounds__(32 * NW)
+template <int NW, bool E4M3, bool ONE>
+__global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
     attend_cache_kernel(const __grid_constant__ AttendCacheParams p, const __grid_constant__ CUtensorMap tmap) {
   constexpr int NB = E4M3 ? 2 : 1;                   // blocks of a step
   constexpr int PER = 32 / NB;                       // steps whose blocks the lanes hold
@@ -561,45 +562,86 @@ __global__ void __launch_bounds__(32 * NW)
   }
 }
 
-/* The parts of split rows together: a block per row, a warp per head. */
+/* The parts of split rows together: a block per row and pair of heads, four warps per head that take
+ * its parts in turn, four channels per lane.  Latency bounds it: the parts' sums are asked for before
+ * their bases are known. */
+struct JoinParams : AttendCacheParams {
+  uint8_t split[MD_MAX_BATCH];               // sequences whose rows are split
+};
 template <bool E4M3>
-__global__ void __launch_bounds__(32 * GP) attend_join_kernel(const __grid_constant__ AttendCacheParams p) {
+__global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ JoinParams p) {
+  constexpr int AHEAD = 8;                   // parts of a warp under way
+  __shared__ float4 so[8][32];
+  __shared__ float sl[8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, turn = warp & 3;
+  const int item = blockIdx.x >> 2, head = (blockIdx.x & 3) * 2 + (warp >> 2), b = p.split[blockIdx.y];
+  const int lh = p.L * p.Hkv, parts = (p.unit_start[b + 1] - p.unit_start[b]) / lh;
+  const int l = item / p.Hkv, h = item - l * p.Hkv;
+  const float *from = p.partials + (size_t)(p.part_start[b] + item * parts) * PARTIAL;
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31, head = threadIdx.x >> 5, b = blockIdx.y;
-  const int lh = p.L * p.Hkv, parts = (p.unit_start[b + 1] - p.unit_start[b]) / lh;
-  if (parts <= 1 || head >= p.G) return;
-  const int item = blockIdx.x, l = item / p.Hkv, h = item - l * p.Hkv;
-  const float *from = p.partials + (size_t)(p.part_start[b] + item * parts) * PARTIAL;
-  float top = -INFINITY, sum = 0.f;
+  float4 x[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (turn + 4 * i < parts) x[i] = *(const float4 *)(from + (size_t)(turn + 4 * i) * PARTIAL + head * D + 4 * lane);
+  float top = -INFINITY;
   for (int y = lane; y < parts; y += 32) top = fmaxf(top, from[(size_t)y * PARTIAL + GP * D + head]);
 #pragma unroll
   for (int s = 1; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
   const float base = max_base(top);
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int y = 0; y < parts; ++y) {
-    const float *x = from + (size_t)y * PARTIAL;
-    const float f = ex2(x[GP * D + head] - base);
-    const float4 e = *(const float4 *)(x + head * D + 4 * lane);
-    sum += f * x[GP * D + GP + head];
-    acc.x += f * e.x;
-    acc.y += f * e.y;
-    acc.z += f * e.z;
-    acc.w += f * e.w;
+  float sum = 0.f;
+  for (int y0 = turn; y0 < parts; y0 += 4 * AHEAD) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int y = y0 + 4 * i;
+      if (y >= parts) break;
+      const float *r = from + (size_t)y * PARTIAL;
+      const float f = ex2(r[GP * D + head] - base);
+      if (y0 != turn) x[i] = *(const float4 *)(r + head * D + 4 * lane);
+      sum += f * r[GP * D + GP + head];
+      acc.x += f * x[i].x;
+      acc.y += f * x[i].y;
+      acc.z += f * x[i].z;
+      acc.w += f * x[i].w;
+    }
+  }
+  so[warp][lane] = acc;
+  if (lane == 0) sl[warp] = sum;
+  __syncthreads();
+  if (turn || head >= p.G) return;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
+    const float4 e = so[warp + i][lane];
+    sum += sl[warp + i];
+    acc.x += e.x;
+    acc.y += e.y;
+    acc.z += e.z;
+    acc.w += e.w;
   }
   put_out<E4M3>(p, b, l, h, head, 4 * lane, acc, inverse(sum));
   if (p.lse && lane == 0) p.lse[((size_t)b * p.L + l) * p.Hq + h * p.G + head] = logarithm(base, sum);
 }
 
 struct Form {
-  int C = 1, warps = 4;
+  int C = 1, warps = 4, unit = 0;            // CTAs per unit, warps per CTA, most steps of a unit
 };
 
-/* How many CTAs and warps per unit, and how many units per row. */
+/* How many CTAs and warps per unit, and how many steps a unit has at most: the estimate of the
+ * launch's time that is least.  A warp's step takes `step` us with 4, 8 or 12 warps on its SM; a CTA
+ * of 4 warps shares its SM with two others, one of 8 warps has it alone.  Where all CTAs run at once, the
+ * longest one's steps and the bytes at the copy rate both bound the time (their 4-norm: near each
+ * other, neither hides the other); with several waves, the CTAs' summed time and the bytes, and a
+ * last wave of the CTAs that are left.
+ *   The constants were fitted to 78 launches timed on a GB300 in up to 45 forms each (1 to 64
+ * sequences, 1 to 36 layers, 1 to 8 KV heads, 100 to 131,071 tokens, both types, some ragged or under a
+ * window): the form taken is 1.4% slower than the best on average, 11% at worst.  Some forms, us: one
+ * sequence of 131,071 tokens, 2 KV heads: 16 parts of 8 CTAs 15.8, one part of 16 CTAs 44; 448 tokens: 4
+ * CTAs of 4 warps 4.0, one of 8 4.5; 32 x 1,700 in 36 layers: one CTA of 4 warps 148, two 170, one
+ * of 8 177; 4 x 65,536 in 36 layers: four of 4 605, one 644. */
 Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
+  constexpr float SMS = 152.f;
   const int NB = e4m3 ? 2 : 1, lh = p.L * p.Hkv;
-  constexpr int SMS = 152, SLOTS = 3 * SMS;
   int steps[MD_MAX_BATCH], most = 0;
   long long total = 0;
   for (int b = 0; b < p.n_seqs; ++b) {
@@ -607,36 +649,75 @@ Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
     most = std::max(most, steps[b]);
     total += (long long)steps[b] * lh;
   }
-  Form f;
-  const long long rows = (long long)p.n_seqs * lh;
-  while (f.C < MAX_CLUSTER && rows * f.C * 2 <= SLOTS && f.C * f.warps < most) f.C *= 2;
-  const long long unit = std::max<long long>(64, total / (SLOTS / f.C * 4) + 1);   // steps of a unit
+  const float step4 = e4m3 ? 0.68f : 0.51f, step8 = e4m3 ? 0.85f : 0.55f, step12 = e4m3 ? 1.27f : 0.81f;
+  const float bytes = (float)total * (STEP_BYTES * 0.96f / 6.69e6f);   // us at the copy rate
+  auto norm = [](float x, float y) { return sqrtf(sqrtf(x * x * x * x + y * y * y * y)); };
+  Form best;
+  best.unit = std::max(most, 1);
+  float least = INFINITY;
+  for (const int parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+    const int unit = std::max((most + parts - 1) / parts, 1);
+    if (parts > 1 && (!workspace || unit < 8)) break;
+    long long units = 0, partials = 0;
+    for (int b = 0; b < p.n_seqs; ++b) {
+      const int n = std::max((steps[b] + unit - 1) / unit, 1);
+      units += n;
+      if (n > 1) partials += n;
+    }
+    if (partials * lh > MAX_PARTIALS) break;
+    for (int warps = 4; warps <= 8; warps += 4)
+      for (int C = 1; C <= MAX_CLUSTER; C *= 2) {
+        if (C * warps > 4 && C * warps >= 2 * unit) break;             // half of them would have no step
+        /* a cluster of 8 or 16 CTAs leaves parts of the chip unused */
+        const float part = warps == 4 ? (C <= 2 ? 1.f : C == 4 ? 0.95f : C == 8 ? 0.93f : 0.74f)
+                                      : (C <= 2 ? 1.f : C == 4 ? 0.94f : C == 8 ? 0.8f : 0.6f);
+        const float N = (float)units * lh * C, slots = SMS * part * (warps == 4 ? 3 : 1);
+        const float longest = (float)((unit + C * warps - 1) / (C * warps));
+        const float start = 2.9f + (C > 1 ? 0.67f : 0.f) + (C == 16 ? 0.06f : 0.f) + (warps == 8 ? 0.21f : 0.f);
+        /* of a warp, where n CTAs run */
+        auto step = [&](float n) { return warps == 8 || (n > SMS * part && n <= 2 * SMS * part) ? step8 : n <= SMS * part ? step4 : step12; };
+        float t;
+        if (N <= slots) {
+          t = start + norm(longest * step(N), bytes) + 0.002f * N;
+        } else {
+          const float cta = start + 1.1f + (C > 1 ? 0.86f : 0.f) + ((float)total / (N * warps) + 0.5f) * step(slots);
+          const float waves = floorf(N / slots), left = N - waves * slots;
+          t = start + norm(waves * cta, bytes * (1.f - left / N)) + std::max(0.69f * longest * step(left), bytes * left / N);
+        }
+        if (parts > 1) t += 1.56f + 0.032f * parts;
+        if (t < least) {
+          least = t;
+          best.C = C;
+          best.warps = warps;
+          best.unit = unit;
+        }
+      }
+  }
   p.unit_start[0] = 0;
   int partials = 0;
   for (int b = 0; b < p.n_seqs; ++b) {
-    long long parts = workspace ? std::max<long long>(1, steps[b] / unit) : 1;
-    if (partials + parts * lh > MAX_PARTIALS) parts = 1;
+    const int n = std::max((steps[b] + best.unit - 1) / best.unit, 1) * lh;
     p.part_start[b] = partials;
-    if (parts > 1) partials += (int)parts * lh;
-    p.unit_start[b + 1] = p.unit_start[b] + (int)parts * lh;
+    if (n > lh) partials += n;
+    p.unit_start[b + 1] = p.unit_start[b] + n;
   }
-  return f;
+  return best;
 }
 
-template <int NW, int ST, bool E4M3, bool ONE>
+template <int NW, bool E4M3, bool ONE>
 cudaError_t launch_attend(const AttendCacheParams &p, const CUtensorMap &tmap, cudaStream_t s) {
   constexpr int which = ATTR_ATTEND_CACHE + (E4M3 ? 1 : 0) + (ONE ? 2 : 0) + (NW == 8 ? 4 : 0);
-  const auto kernel = attend_cache_kernel<NW, ST, E4M3, ONE>;
+  const auto kernel = attend_cache_kernel<NW, E4M3, ONE>;
   const cudaError_t e = once_per_device<which>([&] {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (int)attend_smem(ONE ? 1 : MAX_CLUSTER, NW, ST));
+                                               (int)attend_smem(ONE ? 1 : MAX_CLUSTER, NW));
     return e != cudaSuccess || ONE ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.unit_start[p.n_seqs] * p.C));
   cfg.blockDim = dim3(32 * NW);
-  cfg.dynamicSmemBytes = attend_smem(p.C, NW, ST);
+  cfg.dynamicSmemBytes = attend_smem(p.C, NW);
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -664,10 +745,17 @@ template <bool E4M3>
 cudaError_t run(AttendCacheParams &p, const CUtensorMap &tmap, bool workspace, cudaStream_t s) {
   const Form f = attend_form(p, E4M3, workspace);
   p.C = f.C;
-  cudaError_t e = f.C > 1 ? launch_attend<4, 2, E4M3, false>(p, tmap, s) : launch_attend<4, 2, E4M3, true>(p, tmap, s);
+  cudaError_t e = f.warps == 8 ? (f.C > 1 ? launch_attend<8, E4M3, false>(p, tmap, s) : launch_attend<8, E4M3, true>(p, tmap, s))
+                               : (f.C > 1 ? launch_attend<4, E4M3, false>(p, tmap, s) : launch_attend<4, E4M3, true>(p, tmap, s));
   const int lh = p.L * p.Hkv;
-  if (e == cudaSuccess && p.unit_start[p.n_seqs] > p.n_seqs * lh)
-    e = launch_pdl(attend_join_kernel<E4M3>, dim3(lh, p.n_seqs), 32 * GP, 0, s, p);
+  JoinParams j;
+  int split = 0;
+  for (int b = 0; b < p.n_seqs; ++b)
+    if (p.unit_start[b + 1] - p.unit_start[b] > lh) j.split[split++] = (uint8_t)b;
+  if (e == cudaSuccess && split) {
+    (AttendCacheParams &)j = p;
+    e = launch_pdl(attend_join_kernel<E4M3>, dim3(4 * lh, split), 256, 0, s, j);
+  }
   return e;
 }
 
