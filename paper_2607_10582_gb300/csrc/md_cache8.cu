@@ -23,162 +23,263 @@ struct Cache8Params {
   int block_start[MD_MAX_BATCH + 1];     // blocks of the sequences before
 };
 
-/* Four consecutive elements of a row, as they lie in memory and as fp32. */
+/* W consecutive elements of a row, as they lie in memory. */
+template <class T, int W>
+struct Piece {
+  static constexpr int WORDS = W * (int)sizeof(T) / 4;
+  uint32_t w[WORDS];
+  __device__ __forceinline__ void load(const T *p) {
+    if constexpr (WORDS == 2) {
+      const uint2 u = *(const uint2 *)p;
+      w[0] = u.x, w[1] = u.y;
+    } else {
+      const uint4 u = *(const uint4 *)p;
+      w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    }
+  }
+  __device__ __forceinline__ void store(T *p) const {
+    if constexpr (WORDS == 2) *(uint2 *)p = make_uint2(w[0], w[1]);
+    else *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+/* Per type: a word's elements as fp32, and back; the larger sizes of two words' elements, as
+ * integers, which order like them with what is not finite on top. */
 template <class T>
-struct Four {                            // bf16, f16
-  uint2 u;
-  __device__ __forceinline__ void load(const T *p) { u = *(const uint2 *)p; }
-  __device__ __forceinline__ void store(T *p) const { *(uint2 *)p = u; }
+struct Type;
+template <>
+struct Type<__nv_bfloat16> {
+  static constexpr int PER_WORD = 2;
+  static constexpr uint32_t SIGNS = 0x80008000u;
+  static __device__ __forceinline__ void floats(uint32_t w, float *f) {
+    f[0] = __uint_as_float(w << 16);
+    f[1] = __uint_as_float(w & 0xffff0000u);
+  }
+  static __device__ __forceinline__ uint32_t word(const float *f) { return pack_bf16(f[0], f[1]); }
+  static __device__ __forceinline__ float size(uint32_t bits) { return __uint_as_float(bits << 16); }
 };
 template <>
-struct Four<float> {
-  float4 u;
-  __device__ __forceinline__ void load(const float *p) { u = *(const float4 *)p; }
-  __device__ __forceinline__ void store(float *p) const { *(float4 *)p = u; }
+struct Type<__half> {
+  static constexpr int PER_WORD = 2;
+  static constexpr uint32_t SIGNS = 0x80008000u;
+  static __device__ __forceinline__ void floats(uint32_t w, float *f) {
+    const float2 x = __half22float2(*(const __half2 *)&w);
+    f[0] = x.x;
+    f[1] = x.y;
+  }
+  static __device__ __forceinline__ uint32_t word(const float *f) {
+    const __half2 x = __floats2half2_rn(f[0], f[1]);
+    return *(const uint32_t *)&x;
+  }
+  static __device__ __forceinline__ float size(uint32_t bits) {
+    float f[2];
+    floats(bits, f);
+    return f[0];
+  }
 };
-__device__ __forceinline__ float4 floats(const Four<__nv_bfloat16> &x) {
-  return make_float4(__uint_as_float(x.u.x << 16), __uint_as_float(x.u.x & 0xffff0000u), __uint_as_float(x.u.y << 16),
-                     __uint_as_float(x.u.y & 0xffff0000u));
+template <>
+struct Type<float> {
+  static constexpr int PER_WORD = 1;
+  static constexpr uint32_t SIGNS = 0x80000000u;
+  static __device__ __forceinline__ void floats(uint32_t w, float *f) { f[0] = __uint_as_float(w); }
+  static __device__ __forceinline__ uint32_t word(const float *f) { return __float_as_uint(f[0]); }
+  static __device__ __forceinline__ float size(uint32_t bits) { return __uint_as_float(bits); }
+};
+template <class T>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+  if constexpr (Type<T>::PER_WORD == 1) return max(a, b);
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
-__device__ __forceinline__ float4 floats(const Four<__half> &x) {
-  const float2 a = __half22float2(*(const __half2 *)&x.u.x), b = __half22float2(*(const __half2 *)&x.u.y);
-  return make_float4(a.x, a.y, b.x, b.y);
-}
-__device__ __forceinline__ float4 floats(const Four<float> &x) { return x.u; }
-__device__ __forceinline__ void round_to(Four<__nv_bfloat16> &y, float4 x) {
-  y.u = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
-}
-__device__ __forceinline__ void round_to(Four<__half> &y, float4 x) {
-  const __half2 a = __floats2half2_rn(x.x, x.y), b = __floats2half2_rn(x.z, x.w);
-  y.u = make_uint2(*(const uint32_t *)&a, *(const uint32_t *)&b);
-}
-__device__ __forceinline__ void round_to(Four<float> &y, float4 x) { y.u = x; }
 
-/* Four codes of four values; NaN stays NaN. */
-__device__ __forceinline__ uint32_t encode4(float4 x) {
+/* Codes of four values; NaN stays NaN. */
+__device__ __forceinline__ uint32_t encode4(const float *x) {
   uint16_t lo, hi;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x.y), "f"(x.x));
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x.w), "f"(x.z));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[1]), "f"(x[0]));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[3]), "f"(x[2]));
   return (uint32_t)hi << 16 | lo;
 }
-__device__ __forceinline__ float4 decode4(uint32_t c) {
+__device__ __forceinline__ void decode4(uint32_t c, float s, float *x) {
   uint32_t lo, hi;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((uint16_t)c));
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((uint16_t)(c >> 16)));
   const float2 a = __half22float2(*(const __half2 *)&lo), b = __half22float2(*(const __half2 *)&hi);
-  return make_float4(a.x, a.y, b.x, b.y);
+  x[0] = a.x * s, x[1] = a.y * s, x[2] = b.x * s, x[3] = b.y * s;
 }
-__device__ __forceinline__ float4 times(float4 x, float s) { return make_float4(x.x * s, x.y * s, x.z * s, x.w * s); }
+/* W codes of a row. */
+template <int W>
+struct Codes {
+  uint32_t c[W / 4];
+  __device__ __forceinline__ void load(const uint8_t *p) {
+    if constexpr (W == 4) {
+      c[0] = *(const uint32_t *)p;
+    } else {
+      const uint2 u = *(const uint2 *)p;
+      c[0] = u.x, c[1] = u.y;
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t *p) const {
+    if constexpr (W == 4) *(uint32_t *)p = c[0];
+    else *(uint2 *)p = make_uint2(c[0], c[1]);
+  }
+};
 
-/* A block's part of a call: a warp per (block of 16 tokens, layer, KV head, K or V), a lane per
- * four channels of its rows. */
+/* A block's part of a call: a warp per (layer, block of 16 tokens, KV head, K or V), a lane per W
+ * channels of every (32 W / 128)th of its rows. */
 struct Unit {
-  int which, layer, head;      // K: 0, V: 1
+  int which;                   // K: 0, V: 1
   int lo, hi;                  // slots of the block that the call is about
-  long long row;               // the row of slot 0 (before the first one, if the block begins earlier)
+  long long at;                // of slot 0 in the rows (before them, if the block begins earlier)
   uint8_t *codes;              // of slot 0
   float *scale;                // null: not in the pool
 };
-__device__ __forceinline__ Unit unit_of(const Cache8Params &p, long long u) {
-  Unit r;
-  r.which = (int)(u & 1);
-  u >>= 1;
-  r.head = (int)(u % p.Hkv);
-  u /= p.Hkv;
-  const int blocks = p.block_start[p.n_seqs];
-  r.layer = (int)(u / blocks);
-  const int at = (int)(u - (long long)r.layer * blocks);
-  int b = 0, hi = p.n_seqs;              // the sequence: block_start[b] <= at < block_start[b + 1]
-  while (hi - b > 1) {
+__device__ __forceinline__ bool unit_of(const Cache8Params &p, Unit &r) {
+  const unsigned v = blockIdx.x * 8 + (threadIdx.x >> 5), per = 2 * p.Hkv;
+  const int at = (int)(v / per), hw = (int)(v - at * per), layer = blockIdx.y, head = hw >> 1;
+  if (at >= p.block_start[p.n_seqs]) return false;
+  int b = 0;                             // the sequence: block_start[b] <= at < block_start[b + 1]
+  for (int hi = p.n_seqs; hi - b > 1;) {
     const int mid = (b + hi) >> 1;
     if (p.block_start[mid] <= at) b = mid;
     else hi = mid;
   }
+  r.which = hw & 1;
   const int first = p.first[b], count = p.row_start[b + 1] - p.row_start[b];
-  const int block = first / BLOCK + at - p.block_start[b], tok = block * BLOCK;
+  const int tok = (first / BLOCK + at - p.block_start[b]) * BLOCK;
   r.lo = max(first - tok, 0);
   r.hi = min(first + count - tok, BLOCK);
-  r.row = (long long)p.row_start[b] + tok - first;
-  const int pg = tok / p.ps, part = (tok - pg * p.ps) / BLOCK;
+  r.at = ((long long)p.row_start[b] + tok - first) * p.row[r.which] + layer * p.layer[r.which] + head * p.head[r.which];
+  const int pg = p.ps == 16 ? tok >> 4 : tok >> 5, part = (tok & (p.ps - 1)) / BLOCK;
   const int phys = p.block_table[(size_t)b * p.P_max + pg];
   const bool in = (unsigned)phys < (unsigned)p.P_phys;
-  const size_t rows = ((((size_t)r.layer * p.P_phys + (in ? phys : 0)) * p.Hkv + r.head) * 2 + r.which) * p.ps + part * BLOCK;
+  const size_t rows = ((((size_t)layer * p.P_phys + (in ? phys : 0)) * p.Hkv + head) * 2 + r.which) * p.ps + part * BLOCK;
   r.codes = p.pool + rows * D;
   r.scale = in ? p.scales + rows / BLOCK : nullptr;
-  return r;
+  return true;
 }
 
 /* The scale is a power of two: x / s and the codes of a block that moves to a larger scale
  * are then exact (but for subnormal codes), and a float code has the same relative precision in
  * every binade, so that a scale of max / 448 would gain nothing but part of a binade at the
  * small end. */
-template <class T>
+template <class T, int W>
 __global__ void __launch_bounds__(256) write_cache8_kernel(const __grid_constant__ Cache8Params p) {
+  using X = Type<T>;
+  constexpr int R = 32 * W / D, N = BLOCK / R;       // rows of the warp at once, rows of a lane
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const long long units = (long long)p.block_start[p.n_seqs] * p.L * p.Hkv * 2;
-  for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (long long)gridDim.x * 8) {
-    const Unit t = unit_of(p, u);
-    if (!t.scale) continue;
-    const T *src = (const T *)p.rows[t.which] + t.row * p.row[t.which] + t.layer * p.layer[t.which] +
-                   t.head * p.head[t.which] + 4 * lane;
-    const float before = t.lo > 0 ? *t.scale : 0.f;
-    Four<T> x[BLOCK];
+  const int lane = threadIdx.x & 31, row0 = lane / (D / W), d = lane % (D / W) * W;
+  Unit t;
+  if (!unit_of(p, t) || !t.scale) return;
+  const T *src = (const T *)p.rows[t.which] + t.at + d;
+  const float before = t.lo > 0 ? *t.scale : 0.f;
+  Piece<T, W> x[N];
 #pragma unroll
-    for (int r = 0; r < BLOCK; ++r)
-      if (r >= t.lo && r < t.hi) x[r].load(src + r * p.row[t.which]);
-    float most = 0.f;                    // of the finite values
+  for (int i = 0; i < N; ++i) {
+    const int r = R * i + row0;
+    if (r >= t.lo && r < t.hi) {
+      x[i].load(src + r * p.row[t.which]);
+    } else {
 #pragma unroll
-    for (int r = 0; r < BLOCK; ++r)
-      if (r >= t.lo && r < t.hi) {
-        const float4 f = floats(x[r]);
-        auto size = [](float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.f; };
-        most = fmaxf(fmaxf(most, fmaxf(size(f.x), size(f.y))), fmaxf(size(f.z), size(f.w)));
-      }
-    /* 448 is 1.75 x 2^8: fractions above 1.75 carry into the next exponent */
-    const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(most)) + 0x1fffffu;
-    const float least = __uint_as_float(max((int)(bits >> 23) - 8, 1) << 23);
-    const float scale = fmaxf(before, least), inv = 1.f / scale;
-    uint32_t *dst = (uint32_t *)t.codes + lane;
-    if (t.lo > 0 && scale > before) {
-      const float ratio = before * inv;
-#pragma unroll
-      for (int r = 0; r < BLOCK; ++r)
-        if (r < t.lo) dst[r * (D / 4)] = encode4(times(decode4(dst[r * (D / 4)]), ratio));
+      for (int k = 0; k < Piece<T, W>::WORDS; ++k) x[i].w[k] = 0;
     }
-#pragma unroll
-    for (int r = 0; r < BLOCK; ++r)
-      if (r >= t.lo && r < t.hi) {
-        const float4 f = floats(x[r]);
-        auto code = [&](float v) { return fmaf(v, 0.f, v * inv); };   // infinities become NaN
-        dst[r * (D / 4)] = encode4(make_float4(code(f.x), code(f.y), code(f.z), code(f.w)));
-      }
-    if (lane == 0 && scale != before) *t.scale = scale;
   }
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int k = 0; k < Piece<T, W>::WORDS; ++k) most = larger<T>(most, x[i].w[k] & ~X::SIGNS);
+  if (X::PER_WORD == 2) most = max(most >> 16, most & 0xffffu);
+  float size = X::size(__reduce_max_sync(0xffffffffu, most));
+  const bool odd = !(size < INFINITY);               // something is not finite: it is left out
+  if (odd) {
+    size = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int k = 0; k < Piece<T, W>::WORDS; ++k) {
+        float f[2] = {0.f, 0.f};
+        X::floats(x[i].w[k], f);
+        size = fmaxf(size, fmaxf(fabsf(f[0]) < INFINITY ? fabsf(f[0]) : 0.f, fabsf(f[1]) < INFINITY ? fabsf(f[1]) : 0.f));
+      }
+    size = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(size)));
+  }
+  /* 448 is 1.75 x 2^8: fractions above 1.75 carry into the next exponent */
+  const float least = __uint_as_float(max((int)(__float_as_uint(size) + 0x1fffffu >> 23) - 8, 1) << 23);
+  const float scale = fmaxf(before, least), inv = 1.f / scale;
+  uint8_t *dst = t.codes + d;
+  if (t.lo > 0 && scale > before) {
+    const float ratio = before * inv;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = R * i + row0;
+      if (r >= t.lo) continue;
+      Codes<W> c;
+      c.load(dst + r * D);
+#pragma unroll
+      for (int k = 0; k < W / 4; ++k) {
+        float f[4];
+        decode4(c.c[k], ratio, f);
+        c.c[k] = encode4(f);
+      }
+      c.store(dst + r * D);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int r = R * i + row0;
+    if (r < t.lo || r >= t.hi) continue;
+    float f[W];
+#pragma unroll
+    for (int k = 0; k < Piece<T, W>::WORDS; ++k) X::floats(x[i].w[k], f + k * X::PER_WORD);
+    if (odd) {
+#pragma unroll
+      for (int k = 0; k < W; ++k) f[k] = fmaf(f[k], 0.f, f[k]);      // infinities become NaN
+    }
+    Codes<W> c;
+#pragma unroll
+    for (int k = 0; k < W; ++k) f[k] *= inv;
+#pragma unroll
+    for (int k = 0; k < W / 4; ++k) c.c[k] = encode4(f + 4 * k);
+    c.store(dst + r * D);
+  }
+  if (lane == 0 && scale != before) *t.scale = scale;
 }
 
-template <class T>
+template <class T, int W>
 __global__ void __launch_bounds__(256) read_cache8_kernel(const __grid_constant__ Cache8Params p) {
+  using X = Type<T>;
+  constexpr int R = 32 * W / D, N = BLOCK / R;
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const long long units = (long long)p.block_start[p.n_seqs] * p.L * p.Hkv * 2;
-  for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (long long)gridDim.x * 8) {
-    const Unit t = unit_of(p, u);
-    T *dst = (T *)p.rows[t.which] + t.row * p.row[t.which] + t.layer * p.layer[t.which] + t.head * p.head[t.which] + 4 * lane;
-    const uint32_t *src = (const uint32_t *)t.codes + lane;
-    uint32_t c[BLOCK];
+  const int lane = threadIdx.x & 31, row0 = lane / (D / W), d = lane % (D / W) * W;
+  Unit t;
+  if (!unit_of(p, t)) return;
+  T *dst = (T *)p.rows[t.which] + t.at + d;
+  Codes<W> c[N];
 #pragma unroll
-    for (int r = 0; r < BLOCK; ++r) c[r] = t.scale && r >= t.lo && r < t.hi ? src[r * (D / 4)] : 0x7f7f7f7fu;
-    const float scale = t.scale ? *t.scale : 1.f;
+  for (int i = 0; i < N; ++i) {
+    const int r = R * i + row0;
+    if (t.scale && r >= t.lo && r < t.hi) {
+      c[i].load(t.codes + r * D + d);
+    } else {
 #pragma unroll
-    for (int r = 0; r < BLOCK; ++r)
-      if (r >= t.lo && r < t.hi) {
-        Four<T> y;
-        round_to(y, times(decode4(c[r]), scale));
-        y.store(dst + r * p.row[t.which]);
-      }
+      for (int k = 0; k < W / 4; ++k) c[i].c[k] = 0x7f7f7f7fu;
+    }
+  }
+  const float scale = t.scale ? *t.scale : 1.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int r = R * i + row0;
+    if (r < t.lo || r >= t.hi) continue;
+    float f[W];
+#pragma unroll
+    for (int k = 0; k < W / 4; ++k) decode4(c[i].c[k], scale, f + 4 * k);
+    Piece<T, W> y;
+#pragma unroll
+    for (int k = 0; k < Piece<T, W>::WORDS; ++k) y.w[k] = X::word(f + k * X::PER_WORD);
+    y.store(dst + r * p.row[t.which]);
   }
 }
 
@@ -232,12 +333,20 @@ md_status cache8_params(const md_cache8_args *args, Cache8Params &p) {
   return MD_OK;
 }
 
+/* Rows of two-byte elements that are aligned to 16 bytes go 16 bytes at a time. */
+bool wide(const Cache8Params &p) {
+  for (int i = 0; i < 2; ++i)
+    if (!aligned(p.rows[i], 16) || ((p.row[i] | p.layer[i] | p.head[i]) & 7)) return false;
+  return true;
+}
+
 template <class F>
-md_status launch(const Cache8Params &p, int type, void *stream, F kernels) {
-  const long long units = (long long)p.block_start[p.n_seqs] * p.L * p.Hkv * 2, blocks = (units + 7) / 8;
+md_status launch(const Cache8Params &p, void *stream, F kernel) {
+  const long long units = (long long)p.block_start[p.n_seqs] * p.Hkv * 2;
   if (units == 0) return MD_OK;
-  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20));
-  return launch_pdl(kernels(type), grid, 256, 0, (cudaStream_t)stream, p) == cudaSuccess ? MD_OK : MD_ERR_CUDA;
+  if (units >= 1LL << 31) return MD_ERR_INVALID_ARG;
+  const dim3 grid((unsigned)((units + 7) / 8), p.L);
+  return launch_pdl(kernel, grid, 256, 0, (cudaStream_t)stream, p) == cudaSuccess ? MD_OK : MD_ERR_CUDA;
 }
 
 }  // namespace
@@ -251,11 +360,11 @@ MD_API md_status md_write_cache8(const md_cache8_args *args) {
   Cache8Params p;
   const md_status st = cache8_params(args, p);
   if (st != MD_OK) return st;
-  return launch(p, args->type, args->stream, [](int type) {
-    return type == MD_TYPE_BF16  ? write_cache8_kernel<__nv_bfloat16>
-           : type == MD_TYPE_F16 ? write_cache8_kernel<__half>
-                                 : write_cache8_kernel<float>;
-  });
+  const bool w = wide(p);
+  return launch(p, args->stream,
+                args->type == MD_TYPE_BF16  ? w ? write_cache8_kernel<__nv_bfloat16, 8> : write_cache8_kernel<__nv_bfloat16, 4>
+                : args->type == MD_TYPE_F16 ? w ? write_cache8_kernel<__half, 8> : write_cache8_kernel<__half, 4>
+                                            : write_cache8_kernel<float, 4>);
 }
 
 MD_API md_status md_read_cache8(const md_cache8_args *args) {
@@ -263,9 +372,9 @@ MD_API md_status md_read_cache8(const md_cache8_args *args) {
   Cache8Params p;
   const md_status st = cache8_params(args, p);
   if (st != MD_OK) return st;
-  return launch(p, args->type, args->stream, [](int type) {
-    return type == MD_TYPE_BF16  ? read_cache8_kernel<__nv_bfloat16>
-           : type == MD_TYPE_F16 ? read_cache8_kernel<__half>
-                                 : read_cache8_kernel<float>;
-  });
+  const bool w = wide(p);
+  return launch(p, args->stream,
+                args->type == MD_TYPE_BF16  ? w ? read_cache8_kernel<__nv_bfloat16, 8> : read_cache8_kernel<__nv_bfloat16, 4>
+                : args->type == MD_TYPE_F16 ? w ? read_cache8_kernel<__half, 8> : read_cache8_kernel<__half, 4>
+                                            : read_cache8_kernel<float, 4>);
 }
