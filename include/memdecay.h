@@ -614,12 +614,13 @@ md_status md_sparse_enable(md_ctx *ctx, int top_pages, int first_pages, int last
  *   pool_dev         e4m3 [L][num_phys_pages][Hkv][2][page_size][128], 16-byte aligned:
  *                    md_decode_step's layout with a byte per element
  *   scales_dev       fp32 [L][num_phys_pages][Hkv][2][page_size / 16]: one for each block
- *                    of 16 tokens of a layer, page, KV head, and K or V; 8-byte aligned.
- *                    A code c stands for c * scale
+ *                    of 16 tokens of a layer, page, KV head, and K or V.  A code c
+ *                    stands for c * scale
  *   block_table_dev  int32 [batch][max_pages_per_seq] physical page ids
  * Limits as md_config's (batch <= MD_MAX_BATCH, pages of 16 or 32 tokens, at most
  * MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS tokens per sequence).  The calls allocate nothing,
- * keep nothing and enqueue their work on `stream`. */
+ * keep nothing and enqueue their work on `stream`.  What a call writes overlaps nothing else
+ * that it reads or writes. */
 #define MD_SCALE_TOKENS 16        /* tokens of a scale */
 
 /* The tokens of md_write_cache8 and md_read_cache8: of each sequence b, count_host[b]
@@ -648,8 +649,9 @@ typedef struct {
  * step's mostly does, s is at least its scale until then; where that grows, the codes of the
  * tokens before are moved to it: exactly, but for those that fall below 2^-6 s, which are
  * rounded once more.  Slots behind the new tokens are left as they are.
- * The slots of a block before first_host[b] must have been written.  A page belongs to one
- * sequence of the call.  Rows whose block-table entry lies outside the pool are not written. */
+ * The slots of a block before first_host[b] must have been written.  A page that the call
+ * writes is one sequence's, once in its table.  Rows whose block-table entry lies outside the
+ * pool are not written. */
 md_status md_write_cache8(const md_cache8_args *args);
 
 /* Reads tokens back into rows: code times scale, rounded once to the rows' type (bf16 and
@@ -666,8 +668,9 @@ md_status md_read_cache8(const md_cache8_args *args);
  * read, and what lies in other slots, NaN included, has no part in the result.  A
  * sequence without visible tokens yields zeros, and -inf as its logarithm.  Pages whose
  * block-table entry lies outside the pool are taken for pages without tokens.
- *   E4M3  the softmax weights enter the product with V rounded to 11 bits (f16), the queries
- *         as f16 relative to the head's largest: exactly, but for elements below 2^-29 of it
+ *   E4M3  the softmax weights enter the product with V rounded to 11 bits (f16; those below
+ *         2^-19 of the largest to a multiple of 2^-29 of it), the queries as f16 relative to
+ *         the head's largest element: exactly, but for elements below 2^-29 of it
  *   BF16  the weights enter as two bf16 terms each.  Infinite values of one sign make their
  *         channel infinite, whatever their tokens' weights
  * How a row is split over CTAs goes by the launch's shape and whether there is a workspace:

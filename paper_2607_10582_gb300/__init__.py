@@ -580,8 +580,7 @@ def md_attend_cache(q, pool, block_table, n_tokens, out, *, scales=None, window=
         if x is None and name == "window":
             a.window = -1
             continue
-        x = int(_whole(name, [x], np.int64)[0].reshape(-1)[0])
-        if x < 0:
+        if np.ndim(x) != 0 or (x := int(_whole(name, [x], np.int64)[0][0])) < 0:
             _bad(f"{name}: a whole number from 0 on expected")
         setattr(a, name, min(x, (1 << 31) - 1))
     a.q_dev = _dense("q", q, (B, L, Hq, MD_HEAD_DIM), "bf16")

@@ -773,7 +773,7 @@ MD_API md_status md_attend_cache(const md_attend_cache_args *args) {
   auto aligned = [](const void *x, size_t to) { return x && ((uintptr_t)x & (to - 1)) == 0; };
   const bool e4m3 = a.type == MD_TYPE_E4M3;
   if ((!e4m3 && a.type != MD_TYPE_BF16) || a.window < -1 || a.sinks < 0 || a.num_q_heads < 1 || !aligned(a.q_dev, 16) ||
-      !aligned(a.pool_dev, 16) || (e4m3 && !aligned(a.scales_dev, 8)) || !aligned(a.block_table_dev, 4) ||
+      !aligned(a.pool_dev, 16) || (e4m3 && !aligned(a.scales_dev, 4)) || !aligned(a.block_table_dev, 4) ||
       !aligned(a.out_dev, 8) || ((uintptr_t)a.lse_dev & 3) ||
       !page_set(p, a.block_table_dev, a.n_tokens_host, a.batch, a.num_layers, a.num_q_heads, a.num_kv_heads, a.page_size,
                 a.max_pages_per_seq, a.num_phys_pages))

@@ -304,7 +304,7 @@ md_status cache8_params(const md_cache8_args *args, Cache8Params &p) {
                 a.num_phys_pages))
     return MD_ERR_INVALID_ARG;
   const size_t base = a.type == MD_TYPE_F32 ? 16 : 8;
-  if (!aligned(a.pool_dev, 16) || !aligned(a.scales_dev, 8) || !aligned(a.block_table_dev, 4)) return MD_ERR_INVALID_ARG;
+  if (!aligned(a.pool_dev, 16) || !aligned(a.scales_dev, 4) || !aligned(a.block_table_dev, 4)) return MD_ERR_INVALID_ARG;
   if ((a.k_row | a.k_layer | a.k_head | a.v_row | a.v_layer | a.v_head) & 3) return MD_ERR_INVALID_ARG;
   p.rows[0] = a.k;
   p.rows[1] = a.v;

@@ -422,7 +422,7 @@ REFUSED = [dict(batch=0), dict(batch=257), dict(num_layers=0), dict(num_layers=2
            dict(page_size=64), dict(max_pages_per_seq=0), dict(max_pages_per_seq=1 << 15), dict(num_phys_pages=0),
            dict(num_phys_pages=1 << 27), dict(type=md.MD_TYPE_F16), dict(type=md.MD_TYPE_F32), dict(type=4), dict(type=-1),
            dict(window=-2), dict(sinks=-1), dict(q_dev=None), dict(q_dev=AT + 8), dict(pool_dev=None),
-           dict(pool_dev=AT + 8), dict(scales_dev=None), dict(scales_dev=AT + 4), dict(block_table_dev=None),
+           dict(pool_dev=AT + 8), dict(scales_dev=None), dict(scales_dev=AT + 2), dict(block_table_dev=None),
            dict(block_table_dev=AT + 2), dict(n_tokens_host=None), dict(n_tokens_host=[65, 0]), dict(n_tokens_host=[-1, 0]),
            dict(out_dev=None), dict(out_dev=AT + 4), dict(lse_dev=AT + 2)]
 

@@ -310,7 +310,7 @@ REFUSED = [dict(batch=0), dict(batch=257), dict(num_layers=0), dict(num_layers=2
            dict(first_host=None), dict(count_host=None), dict(first_host=[-1, 0]), dict(count_host=[-1, 3]),
            dict(first_host=[60, 0]), dict(first_host=[(1 << 31) - 1, 0], count_host=[(1 << 31) - 1, 0]), dict(k=None),
            dict(v=None), dict(k=(1 << 20) + 4), dict(type=md.MD_TYPE_F32, v=(1 << 20) + 8), dict(k_row=6), dict(v_head=-2),
-           dict(pool_dev=None), dict(pool_dev=(1 << 20) + 8), dict(scales_dev=None), dict(scales_dev=(1 << 20) + 4),
+           dict(pool_dev=None), dict(pool_dev=(1 << 20) + 8), dict(scales_dev=None), dict(scales_dev=(1 << 20) + 2),
            dict(block_table_dev=None), dict(block_table_dev=(1 << 20) + 2)]
 
 
