@@ -34,6 +34,7 @@ struct AttendCacheParams : PageSet {
   long long limit_ns;
   int window, sinks;                         // window: INT_MAX for all
   int C;                                     // CTAs per unit
+  int early;                                 // all CTAs run at once: their first pages go to L2 ahead of the wait
   int unit_start[MD_MAX_BATCH + 1];          // units of the sequences before
   int part_start[MD_MAX_BATCH];              // first partial of a sequence whose rows are split
 };
@@ -113,6 +114,14 @@ __device__ __forceinline__ void ldmatrix_b8_trans(uint32_t addr, uint32_t (&r)[4
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                : "r"(addr));
 }
+__device__ __forceinline__ void prefetch_l2(const void *p) {
+  asm volatile("prefetch.global.L2 [%0];" ::"l"((uint64_t)__cvta_generic_to_global(p)) : "memory");
+}
+__device__ __forceinline__ void prefetch_l2_bulk(const void *p, uint32_t bytes) {     // multiples of 16
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"((uint64_t)__cvta_generic_to_global(p)), "r"(bytes)
+               : "memory");
+}
+
 /* Sums over channels d .. d + 3 of bf16 V rows with finite weights, of which some came out NaN:
  * infinite where the row's visible tokens have infinite values of one sign and no NaN, as
  * every weight is above 0 (the two terms of a weight may be 0 or cancel, and their products with
@@ -225,6 +234,25 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
   const size_t q_row = ((size_t)b * p.L + l) * p.Hq + h * p.G;
   const uint64_t stream = policy_evict_first();
   const int per_page = p.ps / BLOCK, page_shift = per_page - 1;   // 1 or 2 blocks
+  /* While the launch before ends: the pages of the first steps go into L2, by the table as it is
+   * now.  Only where to look depends on it, so that an entry that is about to change costs a useless
+   * copy; the table is read again behind the wait (and past L1 here, which would keep what it read).
+   * One layer of 131,071 tokens 15.8 -> 15.0 us, 8 x 13,001 13.2 -> 12.3, 8 x 32,768 in bf16 in 4 layers
+   * under a window of 1,000 9.4 -> 8.3.  Where CTAs come in waves it gains nothing. */
+  if (p.early) {
+    const int i = (s0 + w + W * (lane / NB)) * NB + (lane & (NB - 1));
+    if (lane / NB < min(ST, nt) && i < vis.blocks) {
+      const int at = i < vis.head ? i : i - vis.head + vis.tail;
+      const int page = ld_volatile(p.block_table + (size_t)b * p.P_max + (at >> page_shift));
+      if ((unsigned)page < (unsigned)p.P_phys) {
+        const size_t row = ((size_t)l * p.P_phys + page) * p.Hkv + h;
+        const uint8_t *k_rows = (const uint8_t *)p.pool + (row * 2 * p.ps + (at & page_shift) * BLOCK) * (BYTES / 2 / BLOCK);
+        prefetch_l2_bulk(k_rows, BYTES / 2);
+        prefetch_l2_bulk(k_rows + (size_t)p.ps * (BYTES / 2 / BLOCK), BYTES / 2);
+        if (E4M3) prefetch_l2(p.scales + (row * 2 << page_shift) + (at & page_shift));
+      }
+    }
+  }
   pdl_wait();
   pdl_trigger();
 
@@ -745,6 +773,7 @@ template <bool E4M3>
 cudaError_t run(AttendCacheParams &p, const CUtensorMap &tmap, bool workspace, cudaStream_t s) {
   const Form f = attend_form(p, E4M3, workspace);
   p.C = f.C;
+  p.early = (long long)p.unit_start[p.n_seqs] * f.C <= (f.warps == 8 ? 152 : 3 * 152);
   cudaError_t e = f.warps == 8 ? (f.C > 1 ? launch_attend<8, E4M3, false>(p, tmap, s) : launch_attend<8, E4M3, true>(p, tmap, s))
                                : (f.C > 1 ? launch_attend<4, E4M3, false>(p, tmap, s) : launch_attend<4, E4M3, true>(p, tmap, s));
   const int lh = p.L * p.Hkv;

@@ -349,6 +349,35 @@ def test_two_streams_and_two_graphs():
 
 
 @gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_tables_and_pools_that_change_between_calls(kind):
+    """Call after call without a wait, the tables, rows and queries rewritten in between: each call sees
+    what was there when it was its turn."""
+    _need_gpu()
+    c = Case(kind, 1, 16, 2, 16, [2000, 300, 17], seed=20)
+    tables, got = [c.bt], []
+    for i in range(5):                                            # the same pages, others' places; some outside
+        t = c.bt.clone()
+        t[0, :125] = t[0, torch.randperm(125, device="cuda")]
+        t[1, i] = (-1, c.P, 1 << 30, -9, c.P + 5)[i]
+        tables.append(t)
+    qs = [torch.randn_like(c.q) for _ in tables]
+    now, q = c.bt.clone(), c.q.clone()
+    torch.cuda.synchronize()
+    for t, x in zip(tables * 2, qs * 2):
+        out, lse = torch.empty_like(q), torch.empty((3, 1, 16), device="cuda")
+        md.md_attend_cache(q, c.pool, now, c.n, out, scales=c.scales, lse=lse)     # busy with the one before
+        now.copy_(t)
+        q.copy_(x)
+        out, lse = torch.empty_like(q), torch.empty((3, 1, 16), device="cuda")
+        md.md_attend_cache(q, c.pool, now, c.n, out, scales=c.scales, lse=lse)
+        got.append((t, x, out, lse))
+    for t, x, out, lse in got:
+        c.table, c.q = t.cpu().numpy(), x
+        c.check(out, lse)
+
+
+@gpu
 @pytest.mark.parametrize("ps", [16, 32])
 def test_a_decode_loop_on_an_eight_bit_cache(ps):
     """Rows from a projection, written as they come (a prompt, then step by step, layer by layer),
