@@ -18,6 +18,7 @@ import pytest
 
 import paper_2607_10582_gb300 as md
 from paper_2607_10582_gb300 import build as mdbuild
+from tests.attend_forms import FORMS
 
 torch = pytest.importorskip("torch")
 D = 128
@@ -142,6 +143,16 @@ def test_all_tokens(kind, L, Hq, Hkv, ps, lengths):
     md.md_attend_cache(c.q, c.pool, c.bt, c.n, again, scales=c.scales)      # without the logarithms
     assert torch.equal(again, out)
     c.check(*c.attend(workspace=True))
+
+
+@gpu
+@pytest.mark.parametrize("kind,L,Hkv,workspace,lengths,form", FORMS)
+def test_every_form(kind, L, Hkv, workspace, lengths, form):
+    _need_gpu()
+    c = Case(kind, L, 5 * Hkv, Hkv, 16 if form[0] % 3 else 32, lengths, seed=sum(lengths))
+    c.check(*c.attend(bool(workspace)))
+    window = max(0, max(lengths) - 3)
+    c.check(*c.attend(bool(workspace), window=window, sinks=2), window, 2)
 
 
 @gpu
