@@ -35,8 +35,9 @@ struct AttendCacheParams : PageSet {
   int window, sinks;                         // window: INT_MAX for all
   int C;                                     // CTAs per unit
   int early;                                 // all CTAs run at once: their first pages go to L2 ahead of the wait
-  int unit_start[MD_MAX_BATCH + 1];          // units of the sequences before
-  int part_start[MD_MAX_BATCH];              // first partial of a sequence whose rows are split
+  int unit_start[MD_MAX_BATCH + 1];          // units of the sequences before, in the order that they are worked in
+  int part_start[MD_MAX_BATCH];              // first partial of a sequence whose rows are split (in that order)
+  uint8_t order[MD_MAX_BATCH];               // the sequence at each place of that order
 };
 
 /* The visible tokens of a sequence by blocks of 16: the first `head` blocks, and those from block
@@ -215,14 +216,15 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
   if (warp == 0) zero[lane] = 0.f;
   __syncthreads();
   if (!ONE) cluster_arrive();                        // this CTA runs: the others may write its shared memory
-  int b = 0;                                         // the sequence: unit_start[b] <= unit < unit_start[b + 1]
-  for (int hi = p.n_seqs; hi - b > 1;) {
-    const int mid = (b + hi) >> 1;
-    if (p.unit_start[mid] <= unit) b = mid;
+  int place = 0;                                     // of the sequence: unit_start[place] <= unit < unit_start[place + 1]
+  for (int hi = p.n_seqs; hi - place > 1;) {
+    const int mid = (place + hi) >> 1;
+    if (p.unit_start[mid] <= unit) place = mid;
     else hi = mid;
   }
-  const int lh = p.L * p.Hkv, parts = (p.unit_start[b + 1] - p.unit_start[b]) / lh;
-  const int item = (unit - p.unit_start[b]) / parts, part = unit - p.unit_start[b] - item * parts;
+  const int b = p.order[place], at_unit = unit - p.unit_start[place], partial_at = p.part_start[place] + at_unit;
+  const int lh = p.L * p.Hkv, parts = (p.unit_start[place + 1] - p.unit_start[place]) / lh;
+  const int item = at_unit / parts, part = at_unit - item * parts;
   const int l = item / p.Hkv, h = item - l * p.Hkv;
   const int n_tok = p.n_tokens[b];
   const Visible vis = visible(n_tok, p.window, p.sinks);
@@ -505,6 +507,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
   __syncthreads();
   /* the CTA's sums: 4 channels of a head per thread, 8 / NW heads per warp */
   const int slice = GP * D / C;
+  const size_t lse_row = ((size_t)b * p.L + l) * p.Hq + h * p.G;
   float4 acc[GP / NW];
   float top[GP / NW], sum[GP / NW];
 #pragma unroll
@@ -527,7 +530,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
       acc[i].w += f * e.w;
     }
   }
-  float *partial = p.partials + (size_t)(p.part_start[b] + unit - p.unit_start[b]) * PARTIAL;   // where parts > 1
+  float *partial = p.partials + (size_t)partial_at * PARTIAL;   // where parts > 1
   if (ONE) {
 #pragma unroll
     for (int i = 0; i < GP / NW; ++i) {
@@ -540,7 +543,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
         }
       } else if (head < p.G) {
         put_out<E4M3>(p, b, l, h, head, 4 * lane, acc[i], inverse(sum[i]));
-        if (p.lse && lane == 0) p.lse[q_row + head] = logarithm(max_base(top[i]), sum[i]);
+        if (p.lse && lane == 0) p.lse[lse_row + head] = logarithm(max_base(top[i]), sum[i]);
       }
     }
     return;
@@ -567,7 +570,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
         partial[GP * D + head] = most;
         partial[GP * D + GP + head] = s;
       } else if (p.lse && head < p.G) {
-        p.lse[q_row + head] = logarithm(to, s);
+        p.lse[lse_row + head] = logarithm(to, s);
       }
     }
   }
@@ -594,7 +597,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
  * its parts in turn, four channels per lane.  Latency bounds it: the parts' sums are asked for before
  * their bases are known. */
 struct JoinParams : AttendCacheParams {
-  uint8_t split[MD_MAX_BATCH];               // sequences whose rows are split
+  uint8_t split[MD_MAX_BATCH];               // places of the sequences whose rows are split
 };
 template <bool E4M3>
 __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ JoinParams p) {
@@ -602,10 +605,11 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
   __shared__ float4 so[8][32];
   __shared__ float sl[8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, turn = warp & 3;
-  const int item = blockIdx.x >> 2, head = (blockIdx.x & 3) * 2 + (warp >> 2), b = p.split[blockIdx.y];
-  const int lh = p.L * p.Hkv, parts = (p.unit_start[b + 1] - p.unit_start[b]) / lh;
+  const int item = blockIdx.x >> 2, head = (blockIdx.x & 3) * 2 + (warp >> 2);
+  const int place = p.split[blockIdx.y], b = p.order[place];
+  const int lh = p.L * p.Hkv, parts = (p.unit_start[place + 1] - p.unit_start[place]) / lh;
   const int l = item / p.Hkv, h = item - l * p.Hkv;
-  const float *from = p.partials + (size_t)(p.part_start[b] + item * parts) * PARTIAL;
+  const float *from = p.partials + (size_t)(p.part_start[place] + item * parts) * PARTIAL;
   pdl_wait();
   pdl_trigger();
   float4 x[AHEAD];
@@ -653,6 +657,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
 
 struct Form {
   int C = 1, warps = 4, unit = 0;            // CTAs per unit, warps per CTA, most steps of a unit
+  bool waves = false;                        // more CTAs than run at once
 };
 
 /* How many CTAs and warps per unit, and how many steps a unit has at most: the estimate of the
@@ -660,13 +665,14 @@ struct Form {
  * of 4 warps shares its SM with two others, one of 8 warps has it alone.  Where all CTAs run at once, the
  * longest one's steps and the bytes at the copy rate both bound the time (their 4-norm: near each
  * other, neither hides the other); with several waves, the CTAs' summed time and the bytes, and a
- * last wave of the CTAs that are left.
- *   The constants were fitted to 78 launches timed on a GB300 in up to 45 forms each (1 to 64
- * sequences, 1 to 36 layers, 1 to 8 KV heads, 100 to 131,071 tokens, both types, some ragged or under a
- * window): the form taken is 1.4% slower than the best on average, 11% at worst.  Some forms, us: one
- * sequence of 131,071 tokens, 2 KV heads: 16 parts of 8 CTAs 15.8, one part of 16 CTAs 44; 448 tokens: 4
- * CTAs of 4 warps 4.0, one of 8 4.5; 32 x 1,700 in 36 layers: one CTA of 4 warps 148, two 170, one
- * of 8 177; 4 x 65,536 in 36 layers: four of 4 605, one 644. */
+ * last wave of the CTAs that are left, which are shorter ones: then the longest rows go first (16
+ * ragged sequences of up to 4,001 tokens in 36 layers 130.8 -> 127.4 us).
+ *   The constants were fitted to 91 launches timed on a GB300 in up to 45 forms each (1 to 128
+ * sequences, 1 to 36 layers, 1 to 8 KV heads, 100 to 131,071 tokens, both types, a third of them ragged or
+ * under a window): the form taken is 0.7% slower than the best on average, 5% at worst.  Some forms,
+ * us: one sequence of 131,071 tokens, 2 KV heads: 16 parts of 8 CTAs 15.8, one part of 16 CTAs 44; 448
+ * tokens: 4 CTAs of 4 warps 4.0, one of 8 4.5; 32 x 1,700 in 36 layers: one CTA of 4 warps 148, two 170,
+ * one of 8 177; 4 x 65,536 in 36 layers: two of 8 613, one of 4 644. */
 Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
   constexpr float SMS = 152.f;
   const int NB = e4m3 ? 2 : 1, lh = p.L * p.Hkv;
@@ -677,8 +683,8 @@ Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
     most = std::max(most, steps[b]);
     total += (long long)steps[b] * lh;
   }
-  const float step4 = e4m3 ? 0.68f : 0.51f, step8 = e4m3 ? 0.85f : 0.55f, step12 = e4m3 ? 1.27f : 0.81f;
-  const float bytes = (float)total * (STEP_BYTES * 0.96f / 6.69e6f);   // us at the copy rate
+  const float step4 = e4m3 ? 0.657f : 0.489f, step8 = e4m3 ? 0.813f : 0.628f, step12 = e4m3 ? 1.218f : 0.908f;
+  const float bytes = (float)total * (STEP_BYTES * 0.978f / 6.69e6f);   // us at the copy rate
   auto norm = [](float x, float y) { return sqrtf(sqrtf(x * x * x * x + y * y * y * y)); };
   Form best;
   best.unit = std::max(most, 1);
@@ -694,40 +700,50 @@ Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
     }
     if (partials * lh > MAX_PARTIALS) break;
     for (int warps = 4; warps <= 8; warps += 4)
-      for (int C = 1; C <= MAX_CLUSTER; C *= 2) {
+      for (int log_C = 0; 1 << log_C <= MAX_CLUSTER; ++log_C) {
+        const int C = 1 << log_C;
         if (C * warps > 4 && C * warps >= 2 * unit) break;             // half of them would have no step
         /* a cluster of 8 or 16 CTAs leaves parts of the chip unused */
         const float part = warps == 4 ? (C <= 2 ? 1.f : C == 4 ? 0.95f : C == 8 ? 0.93f : 0.74f)
                                       : (C <= 2 ? 1.f : C == 4 ? 0.94f : C == 8 ? 0.8f : 0.6f);
         const float N = (float)units * lh * C, slots = SMS * part * (warps == 4 ? 3 : 1);
         const float longest = (float)((unit + C * warps - 1) / (C * warps));
-        const float start = 2.9f + (C > 1 ? 0.67f : 0.f) + (C == 16 ? 0.06f : 0.f) + (warps == 8 ? 0.21f : 0.f);
+        const float start = 2.65f + (C > 1 ? 0.82f : 0.f) + (C == 16 ? 0.187f : 0.f) + (warps == 8 ? 0.139f : 0.f);
         /* of a warp, where n CTAs run */
         auto step = [&](float n) { return warps == 8 || (n > SMS * part && n <= 2 * SMS * part) ? step8 : n <= SMS * part ? step4 : step12; };
         float t;
         if (N <= slots) {
-          t = start + norm(longest * step(N), bytes) + 0.002f * N;
+          t = start + norm(longest * step(N), bytes) + 0.0019f * N;
         } else {
-          const float cta = start + 1.1f + (C > 1 ? 0.86f : 0.f) + ((float)total / (N * warps) + 0.5f) * step(slots);
+          const float steps_each = (float)total / (N * warps) + 0.5f;
+          const float cta = start + 1.316f + 0.701f * log_C + steps_each * step(slots);
           const float waves = floorf(N / slots), left = N - waves * slots;
-          t = start + norm(waves * cta, bytes * (1.f - left / N)) + std::max(0.69f * longest * step(left), bytes * left / N);
+          const float last = 0.6f * longest + 0.4f * std::min(longest, steps_each);
+          t = start + norm(waves * cta, bytes * (1.f - left / N)) + std::max(0.533f * last * step(left), bytes * left / N);
+          t = std::max(t, start + 1.316f + 0.81f * longest * step(slots));
         }
-        if (parts > 1) t += 1.56f + 0.032f * parts;
+        if (parts > 1) t += 1.791f + 0.0217f * parts;
         if (t < least) {
           least = t;
           best.C = C;
           best.warps = warps;
           best.unit = unit;
+          best.waves = N > slots;
         }
       }
   }
+  auto parts_of = [&](int b) { return std::max((steps[b] + best.unit - 1) / best.unit, 1); };
+  uint32_t key[MD_MAX_BATCH];                // steps of a unit, then the sequence
+  for (int b = 0; b < p.n_seqs; ++b) key[b] = (uint32_t)(steps[b] / parts_of(b)) << 8 | (uint32_t)b;
+  if (best.waves) std::sort(key, key + p.n_seqs, [](uint32_t x, uint32_t y) { return x > y; });
   p.unit_start[0] = 0;
   int partials = 0;
-  for (int b = 0; b < p.n_seqs; ++b) {
-    const int n = std::max((steps[b] + best.unit - 1) / best.unit, 1) * lh;
-    p.part_start[b] = partials;
+  for (int i = 0; i < p.n_seqs; ++i) {
+    const int b = key[i] & 255, n = parts_of(b) * lh;
+    p.order[i] = (uint8_t)b;
+    p.part_start[i] = partials;
     if (n > lh) partials += n;
-    p.unit_start[b + 1] = p.unit_start[b] + n;
+    p.unit_start[i + 1] = p.unit_start[i] + n;
   }
   return best;
 }
@@ -773,7 +789,7 @@ template <bool E4M3>
 cudaError_t run(AttendCacheParams &p, const CUtensorMap &tmap, bool workspace, cudaStream_t s) {
   const Form f = attend_form(p, E4M3, workspace);
   p.C = f.C;
-  p.early = (long long)p.unit_start[p.n_seqs] * f.C <= (f.warps == 8 ? 152 : 3 * 152);
+  p.early = !f.waves;
   cudaError_t e = f.warps == 8 ? (f.C > 1 ? launch_attend<8, E4M3, false>(p, tmap, s) : launch_attend<8, E4M3, true>(p, tmap, s))
                                : (f.C > 1 ? launch_attend<4, E4M3, false>(p, tmap, s) : launch_attend<4, E4M3, true>(p, tmap, s));
   const int lh = p.L * p.Hkv;
