@@ -11,6 +11,10 @@ namespace {
 
 constexpr int BLOCK = MD_SCALE_TOKENS;
 
+/* N: sequences that there is room for.  Few sequences take small parameters: a call that writes one
+ * token takes 3.1 us of the host instead of 3.6. */
+constexpr int FEW = 16;
+template <int N>
 struct Cache8Params {
   void *rows[2];                         // k, v
   long long row[2], layer[2], head[2];   // their strides, in elements
@@ -18,9 +22,9 @@ struct Cache8Params {
   float *scales;
   const int32_t *block_table;
   int L, Hkv, ps, P_phys, P_max, n_seqs;
-  int first[MD_MAX_BATCH];               // position of a sequence's first row
-  int row_start[MD_MAX_BATCH + 1];       // rows of the sequences before
-  int block_start[MD_MAX_BATCH + 1];     // blocks of the sequences before
+  int first[N];                          // position of a sequence's first row
+  int row_start[N + 1];                  // rows of the sequences before
+  int block_start[N + 1];                // blocks of the sequences before
 };
 
 /* W consecutive elements of a row, as they lie in memory. */
@@ -134,7 +138,8 @@ struct Unit {
   uint8_t *codes;              // of slot 0
   float *scale;                // null: not in the pool
 };
-__device__ __forceinline__ bool unit_of(const Cache8Params &p, Unit &r) {
+template <int N>
+__device__ __forceinline__ bool unit_of(const Cache8Params<N> &p, Unit &r) {
   const unsigned v = blockIdx.x * 8 + (threadIdx.x >> 5), per = 2 * p.Hkv;
   const int at = (int)(v / per), hw = (int)(v - at * per), layer = blockIdx.y, head = hw >> 1;
   if (at >= p.block_start[p.n_seqs]) return false;
@@ -163,8 +168,8 @@ __device__ __forceinline__ bool unit_of(const Cache8Params &p, Unit &r) {
  * are then exact (but for subnormal codes), and a float code has the same relative precision in
  * every binade, so that a scale of max / 448 would gain nothing but part of a binade at the
  * small end. */
-template <class T, int W>
-__global__ void __launch_bounds__(256) write_cache8_kernel(const __grid_constant__ Cache8Params p) {
+template <class T, int W, int SEQS>
+__global__ void __launch_bounds__(256) write_cache8_kernel(const __grid_constant__ Cache8Params<SEQS> p) {
   using X = Type<T>;
   constexpr int R = 32 * W / D, N = BLOCK / R;       // rows of the warp at once, rows of a lane
   pdl_wait();
@@ -247,8 +252,8 @@ __global__ void __launch_bounds__(256) write_cache8_kernel(const __grid_constant
   if (lane == 0 && scale != before) *t.scale = scale;
 }
 
-template <class T, int W>
-__global__ void __launch_bounds__(256) read_cache8_kernel(const __grid_constant__ Cache8Params p) {
+template <class T, int W, int SEQS>
+__global__ void __launch_bounds__(256) read_cache8_kernel(const __grid_constant__ Cache8Params<SEQS> p) {
   using X = Type<T>;
   constexpr int R = 32 * W / D, N = BLOCK / R;
   pdl_wait();
@@ -286,10 +291,8 @@ __global__ void __launch_bounds__(256) read_cache8_kernel(const __grid_constant_
 bool aligned(const void *p, size_t a) { return p && ((uintptr_t)p & (a - 1)) == 0; }
 
 /* The checks of both calls, and their launches' parameters. */
-md_status cache8_params(const md_cache8_args *args, Cache8Params &p) {
-  if (!args || !args->first_host || !args->count_host || args->batch < 1 || args->batch > MD_MAX_BATCH)
-    return MD_ERR_INVALID_ARG;
-  const md_cache8_args &a = *args;
+template <int N>
+md_status cache8_params(const md_cache8_args &a, Cache8Params<N> &p) {
   if (a.type < MD_TYPE_BF16 || a.type > MD_TYPE_F32) return MD_ERR_INVALID_ARG;
   const long long limit = (long long)MD_MAX_CHUNKS * MD_MAX_CHUNK_TOKENS;
   int32_t n[MD_MAX_BATCH];
@@ -334,19 +337,38 @@ md_status cache8_params(const md_cache8_args *args, Cache8Params &p) {
 }
 
 /* Rows of two-byte elements that are aligned to 16 bytes go 16 bytes at a time. */
-bool wide(const Cache8Params &p) {
+template <int N>
+bool wide(const Cache8Params<N> &p) {
   for (int i = 0; i < 2; ++i)
     if (!aligned(p.rows[i], 16) || ((p.row[i] | p.layer[i] | p.head[i]) & 7)) return false;
   return true;
 }
 
-template <class F>
-md_status launch(const Cache8Params &p, void *stream, F kernel) {
+template <int N, bool WRITE>
+md_status cache8(const md_cache8_args &a) {
+  Cache8Params<N> p;
+  const md_status st = cache8_params(a, p);
+  if (st != MD_OK) return st;
   const long long units = (long long)p.block_start[p.n_seqs] * p.Hkv * 2;
   if (units == 0) return MD_OK;
   if (units >= 1LL << 31) return MD_ERR_INVALID_ARG;
   const dim3 grid((unsigned)((units + 7) / 8), p.L);
-  return launch_pdl(kernel, grid, 256, 0, (cudaStream_t)stream, p) == cudaSuccess ? MD_OK : MD_ERR_CUDA;
+  auto launch = [&](auto write, auto read) {
+    return launch_pdl(WRITE ? write : read, grid, 256, 0, (cudaStream_t)a.stream, p) == cudaSuccess ? MD_OK : MD_ERR_CUDA;
+  };
+  if (a.type == MD_TYPE_F32) return launch(write_cache8_kernel<float, 4, N>, read_cache8_kernel<float, 4, N>);
+  const bool w = wide(p);
+  if (a.type == MD_TYPE_BF16)
+    return w ? launch(write_cache8_kernel<__nv_bfloat16, 8, N>, read_cache8_kernel<__nv_bfloat16, 8, N>)
+             : launch(write_cache8_kernel<__nv_bfloat16, 4, N>, read_cache8_kernel<__nv_bfloat16, 4, N>);
+  return w ? launch(write_cache8_kernel<__half, 8, N>, read_cache8_kernel<__half, 8, N>)
+           : launch(write_cache8_kernel<__half, 4, N>, read_cache8_kernel<__half, 4, N>);
+}
+
+template <bool WRITE>
+md_status cache8(const md_cache8_args *a) {
+  if (!a || !a->first_host || !a->count_host || a->batch < 1 || a->batch > MD_MAX_BATCH) return MD_ERR_INVALID_ARG;
+  return a->batch <= FEW ? cache8<FEW, WRITE>(*a) : cache8<MD_MAX_BATCH, WRITE>(*a);
 }
 
 }  // namespace
@@ -355,26 +377,6 @@ md_status launch(const Cache8Params &p, void *stream, F kernel) {
 
 #define MD_API extern "C" __attribute__((visibility("default")))
 
-MD_API md_status md_write_cache8(const md_cache8_args *args) {
-  using namespace md;
-  Cache8Params p;
-  const md_status st = cache8_params(args, p);
-  if (st != MD_OK) return st;
-  const bool w = wide(p);
-  return launch(p, args->stream,
-                args->type == MD_TYPE_BF16  ? w ? write_cache8_kernel<__nv_bfloat16, 8> : write_cache8_kernel<__nv_bfloat16, 4>
-                : args->type == MD_TYPE_F16 ? w ? write_cache8_kernel<__half, 8> : write_cache8_kernel<__half, 4>
-                                            : write_cache8_kernel<float, 4>);
-}
+MD_API md_status md_write_cache8(const md_cache8_args *args) { return md::cache8<true>(args); }
 
-MD_API md_status md_read_cache8(const md_cache8_args *args) {
-  using namespace md;
-  Cache8Params p;
-  const md_status st = cache8_params(args, p);
-  if (st != MD_OK) return st;
-  const bool w = wide(p);
-  return launch(p, args->stream,
-                args->type == MD_TYPE_BF16  ? w ? read_cache8_kernel<__nv_bfloat16, 8> : read_cache8_kernel<__nv_bfloat16, 4>
-                : args->type == MD_TYPE_F16 ? w ? read_cache8_kernel<__half, 8> : read_cache8_kernel<__half, 4>
-                                            : read_cache8_kernel<float, 4>);
-}
+MD_API md_status md_read_cache8(const md_cache8_args *args) { return md::cache8<false>(args); }

@@ -157,6 +157,16 @@ def test_every_form(kind, L, Hkv, workspace, lengths, form):
 
 @gpu
 @pytest.mark.parametrize("kind", KINDS)
+def test_the_largest_batch(kind):
+    """256 ragged sequences, some empty, one long, in the order that the launch sorts them into."""
+    _need_gpu()
+    c = Case(kind, 1, 8, 2, 16, [(b * 37) % 200 if b != 101 else 6000 for b in range(md.MD_MAX_BATCH)], seed=31)
+    for workspace in (False, True):
+        c.check(*c.attend(workspace))
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("window,sinks", [(0, 0), (0, 5), (1, 0), (1, 1), (5, 0), (16, 16), (17, 4), (100, 33), (1000, 16),
                                           (None, 7), (1 << 40, 1 << 40), (3, 4000)])
 @pytest.mark.parametrize("L,Hq,Hkv,ps,lengths", [SHAPES[2], SHAPES[3], SHAPES[4]])

@@ -174,6 +174,25 @@ def test_rows_are_stored_and_read_back(ps, kind, layout):
 
 
 @gpu
+@pytest.mark.parametrize("batch", [16, 17, md.MD_MAX_BATCH])
+def test_batches_up_to_the_largest(batch):
+    """Sequences without new tokens among them."""
+    _need_gpu()
+    s = Store(1, 1, 16, batch, 2, seed=batch)
+    for step in range(2):
+        count = [(b * 7 + step) % 13 for b in range(batch)]
+        k, v = s.rows(sum(count), "bf16")
+        s.write(k, v, count)
+    s.check()
+    k, v = (torch.zeros((sum(s.n), 1, 1, D), device="cuda") for _ in range(2))
+    md.md_read_cache8(k, v, s.pool, s.sc, s.bt, np.zeros(batch, np.int32), np.array(s.n, np.int32))
+    at = [(s.table[b, t // 16], t % 16) for b in range(batch) for t in range(s.n[b])]
+    for x, which in ((k, 0), (v, 1)):
+        want = np.stack([decode(s.codes[0, p, 0, which, t]) * s.scales[0, p, 0, which, 0] for p, t in at])
+        assert np.array_equal(x[:, 0, 0].cpu().numpy(), want.astype(np.float32))
+
+
+@gpu
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 def test_scales_of_blocks_grow_with_their_tokens(kind):
     """Token by token, each larger or smaller than those before by up to 2^20: codes move to the new
