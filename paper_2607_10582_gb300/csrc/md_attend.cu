@@ -19,7 +19,8 @@ constexpr int STEP_BYTES = 8192;             // K and V of a step: 32 tokens of 
 constexpr int PARTIAL = GP * D + 2 * GP;     // floats of a part of a row: O [8][128], exponents [8], sums [8]
 constexpr int MAX_PARTIALS = MD_ATTEND_WORKSPACE / (PARTIAL * 4);
 constexpr float SLACK = 10.f;                // log2 of the most that a weight may be above its base
-constexpr float LIFT = 5.f;                  // log2 of the weight at the base (E4M3)
+constexpr float LIFT = 5.f;                  // log2 of the weight at the base (E4M3): f16 ends 2^-29 below it
+constexpr float LOWER = 1.f / 32;            // 2^-LIFT, taken back by V's scales and the sums
 constexpr int OS = D + 4;                    // padded row of a warp's O
 static_assert(GP * OS * 4 <= STEP_BYTES, "a warp's O fits a stage");
 
@@ -171,7 +172,7 @@ __device__ __forceinline__ void put_out(const AttendCacheParams &p, int b, int l
 constexpr int ST = 2;                        // steps of a warp in flight
 constexpr size_t attend_smem(int C, int warps) {
   return 1024 + (size_t)warps * ST * STEP_BYTES + (2 * warps * GP + 2 * GP) * 4 +
-         (C > 1 ? (MAX_CLUSTER * GP * 2 + GP * D) * 4 : 0) + 128 + warps * ST * 8;
+         (C > 1 ? (MAX_CLUSTER * GP * 2 + GP * D) * 4 : 0) + 128 + warps * ST * 8 + 8;
 }
 
 /* A unit is a (sequence, layer, KV head) row, or one of the equal parts of it; C CTAs of NW warps
@@ -205,6 +206,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
   float *xo = fin + 2 * GP;                          // [C][1024 / C] every CTA's part of this one's slice
   float *xml = xo + (ONE ? 0 : GP * D);              // [C][8][2]
   uint64_t *full = (uint64_t *)(xml + (ONE ? 0 : MAX_CLUSTER * GP * 2));    // [NW][ST]
+  int *partial_at = (int *)(full + NW * ST);         // place of this unit among the partials
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int C = ONE ? 1 : p.C, unit = blockIdx.x / C, rank = blockIdx.x - unit * C;
   const uint32_t ring = smem_u32(so) + warp * ST * STEP_BYTES, bars = smem_u32(full + warp * ST);
@@ -222,7 +224,8 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
     if (p.unit_start[mid] <= unit) place = mid;
     else hi = mid;
   }
-  const int b = p.order[place], at_unit = unit - p.unit_start[place], partial_at = p.part_start[place] + at_unit;
+  const int b = p.order[place], at_unit = unit - p.unit_start[place];
+  if (threadIdx.x == 0) *partial_at = p.part_start[place] + at_unit;
   const int lh = p.L * p.Hkv, parts = (p.unit_start[place + 1] - p.unit_start[place]) / lh;
   const int item = at_unit / parts, part = at_unit - item * parts;
   const int l = item / p.Hkv, h = item - l * p.Hkv;
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
       if (E4M3) {
         const float *s = p.scales + ((size_t)x.row * 2 << page_shift) + (at & page_shift);
         x.ks = s[0];
-        x.vs = s[per_page];
+        x.vs = s[per_page];                          // not a use of it: the copy goes out first
       }
     }
     return x;
@@ -367,7 +370,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
       seen[j] = __shfl_sync(0xffffffffu, held.mask, from) & 0xffffu;
       if (E4M3) {
         kscale[j] = __shfl_sync(0xffffffffu, held.ks, from);
-        vscale[j] = __shfl_sync(0xffffffffu, held.vs, from);
+        vscale[j] = __shfl_sync(0xffffffffu, held.vs, from) * LOWER;
       }
     }
     const uint32_t st = ring + (k & (ST - 1)) * STEP_BYTES, bar = bars + (k & (ST - 1)) * 8, parity = k / ST & 1;
@@ -494,8 +497,8 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
   if (g == 0)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      sm[warp * GP + 2 * t + i] = m[i] - (E4M3 ? LIFT : 0.f);
-      sl[warp * GP + 2 * t + i] = z[i];
+      sm[warp * GP + 2 * t + i] = m[i];
+      sl[warp * GP + 2 * t + i] = E4M3 ? z[i] * LOWER : z[i];
     }
   __syncwarp();
 #pragma unroll
@@ -530,7 +533,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
       acc[i].w += f * e.w;
     }
   }
-  float *partial = p.partials + (size_t)partial_at * PARTIAL;   // where parts > 1
+  float *partial = p.partials + (size_t)*partial_at * PARTIAL;   // where parts > 1
   if (ONE) {
 #pragma unroll
     for (int i = 0; i < GP / NW; ++i) {

@@ -103,7 +103,7 @@ class Case:
                         assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(z.isnan(), x.isnan().any(1))
                         continue
                     tol = 2.0 ** -8 * ref.abs() + (2 * delta + 2.0 ** -11 + 2.0 ** -15) * (p @ v.abs()) + \
-                        2.0 ** -30 * v.abs().sum(0) + 1e-30
+                        2.0 ** -30 * v.abs().sum(0) + 2.0 ** -133
                     assert ((got - ref).abs() <= tol).all(), (b, l, h, float(((got - ref).abs() / tol).max()))
                     want = torch.logsumexp(x, -1)
                     tol = delta + 2.0 ** -21 * float(x.abs().max()) + 2.0 ** -20 + len(toks) / 8 * 2.0 ** -24
@@ -238,6 +238,23 @@ def test_queries_of_any_size(kind, size):
         c.pool[:, :, :, 0] = (c.pool[:, :, :, 0].float() / size).bfloat16()
     c.q = (c.q.float() * size).bfloat16()
     c.check(*c.attend())
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", [2.0 ** -100, 2.0 ** 100])
+def test_values_of_any_size(kind, size):
+    """Values near the ends of the range: no sum on the way overflows, none falls to zero."""
+    _need_gpu()
+    c = Case(kind, 1, 8, 2, 16, [500, 3, 40], seed=17)
+    if c.scales is not None:
+        c.scales[:, :, :, 1] *= size
+    else:
+        c.pool[:, :, :, 1] = (c.pool[:, :, :, 1].float() * size).bfloat16()
+    for workspace in (False, True):
+        out, lse = c.attend(workspace)
+        assert out.isfinite().all() and (out != 0).any(-1).all()
+        c.check(out, lse)
 
 
 @gpu
