@@ -673,6 +673,8 @@ md_status md_read_cache8(const md_cache8_args *args);
  *         the head's largest element: exactly, but for elements below 2^-29 of it
  *   BF16  the weights enter as two bf16 terms each.  Infinite values of one sign make their
  *         channel infinite, whatever their tokens' weights
+ * The sums with V hold weights of up to 2^10: values below 2^100 are safe at any length,
+ * those of larger ones may overflow on the way.
  * How a row is split over CTAs goes by the launch's shape and whether there is a workspace:
  * calls of the same shape give the same bits, others may round differently.  The kernel's
  * waits for its own copies are bounded (2 s); a row that gives up is NaN.

@@ -259,6 +259,30 @@ def test_values_of_any_size(kind, size):
 
 @gpu
 @pytest.mark.parametrize("kind", KINDS)
+def test_the_largest_values_at_the_largest_weights(kind):
+    """131,071 values of 1.75 x 2^99 that all exceed their warp's first maximum by 9.9 in log2, just too
+    little to rescale: sums of up to 2^(17 + 9.9 + 99.8), below 2^128 even in one place."""
+    _need_gpu()
+    n, low = 131071, 8192                                         # each of up to 128 warps sees 32 low ones or more first
+    c = Case(kind, 1, 4, 1, 16, [n], seed=18, spare=0)
+    phys = c.bt[0, :c.pages[0]].long()
+    x = torch.zeros((c.pages[0], 16, D), device="cuda")
+    c.q.fill_(1)                                                  # logits 128 k / sqrt(128), x log2(e): 16.32 k
+    k, v = (16.0, 448.0) if kind == "e4m3" else (0.605, 1.75 * 2.0 ** 99)
+    x[low // 16:] = k
+    c.pool[0, phys, 0, 0] = x.to(c.pool.dtype)
+    c.pool[0, phys, 0, 1] = torch.full_like(x, v).to(c.pool.dtype)
+    c.pool[0, phys[-1], 0, :, 15] = math.nan                      # no token
+    if c.scales is not None:
+        c.scales[:, :, :, 0], c.scales[:, :, :, 1] = 0.605 / 16, 2.0 ** 91
+    for workspace in (False, True):
+        out, lse = c.attend(workspace)
+        assert out.isfinite().all()
+        c.check(out, lse)
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
 def test_nan_where_a_visible_token_has_it(kind):
     _need_gpu()
     nan = 0x7fc0 if kind == "bf16" else 0x7f
