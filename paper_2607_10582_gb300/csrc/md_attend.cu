@@ -175,8 +175,11 @@ constexpr size_t attend_smem(int C, int warps) {
          (C > 1 ? (MAX_CLUSTER * GP * 2 + GP * D) * 4 : 0) + 128 + warps * ST * 8 + 8;
 }
 
+/* What works on a unit. */
+enum Team { WARP, CTA, CLUSTER };
+
 /* A unit is a (sequence, layer, KV head) row, or one of the equal parts of it; C CTAs of NW warps
- * per unit, a cluster.  The unit's blocks go to the warps in turn, a step at a time; a
+ * per unit, a cluster, or, for many short rows, a warp.  The unit's blocks go to the warps in turn, a step at a time; a
  * warp copies its own steps by TMA (K and V rows, 128-byte swizzle), ST in flight, and computes
  *   S = K Q^T   rows are tokens, columns the group's heads
  *   O^T = V^T P^T  rows are channels, summed over the tokens.
@@ -190,13 +193,14 @@ constexpr size_t attend_smem(int C, int warps) {
  *
  * The weights are taken against a base that follows the running maximum only when a score exceeds
  * it by SLACK: most steps then need no exchange between lanes and no rescaling. */
-template <int NW, bool E4M3, bool ONE>
+template <int NW, bool E4M3, Team TEAM>
 __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
     attend_cache_kernel(const __grid_constant__ AttendCacheParams p, const __grid_constant__ CUtensorMap tmap) {
   constexpr int NB = E4M3 ? 2 : 1;                   // blocks of a step
   constexpr int PER = 32 / NB;                       // steps whose blocks the lanes hold
   constexpr int BYTES = STEP_BYTES / NB;             // of a block
   constexpr int WARP_FLOATS = ST * STEP_BYTES / 4;
+  constexpr bool ONE = TEAM != CLUSTER;
   extern __shared__ uint8_t smem_raw[];
   float *so = (float *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);   // [NW] the warps' stages, later their O [8][OS]
   float *zero = so + NW * WARP_FLOATS;               // 128 bytes of zeros
@@ -208,7 +212,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
   uint64_t *full = (uint64_t *)(xml + (ONE ? 0 : MAX_CLUSTER * GP * 2));    // [NW][ST]
   int *partial_at = (int *)(full + NW * ST);         // place of this unit among the partials
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int C = ONE ? 1 : p.C, unit = blockIdx.x / C, rank = blockIdx.x - unit * C;
+  const int C = ONE ? 1 : p.C, unit = TEAM == WARP ? blockIdx.x * NW + warp : blockIdx.x / C, rank = ONE ? 0 : blockIdx.x - unit * C;
   const uint32_t ring = smem_u32(so) + warp * ST * STEP_BYTES, bars = smem_u32(full + warp * ST);
   if (lane < ST) {
     mbar_init(bars + lane * 8, NB);
@@ -217,6 +221,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
   if (lane == 0) tma_prefetch_desc(&tmap);
   if (warp == 0) zero[lane] = 0.f;
   __syncthreads();
+  if (TEAM == WARP && unit >= p.unit_start[p.n_seqs]) return;
   if (!ONE) cluster_arrive();                        // this CTA runs: the others may write its shared memory
   int place = 0;                                     // of the sequence: unit_start[place] <= unit < unit_start[place + 1]
   for (int hi = p.n_seqs; hi - place > 1;) {
@@ -225,8 +230,8 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
     else hi = mid;
   }
   const int b = p.order[place], at_unit = unit - p.unit_start[place];
-  if (threadIdx.x == 0) *partial_at = p.part_start[place] + at_unit;
-  const int lh = p.L * p.Hkv, parts = (p.unit_start[place + 1] - p.unit_start[place]) / lh;
+  if (TEAM != WARP && threadIdx.x == 0) *partial_at = p.part_start[place] + at_unit;
+  const int lh = p.L * p.Hkv, parts = TEAM == WARP ? 1 : (p.unit_start[place + 1] - p.unit_start[place]) / lh;
   const int item = at_unit / parts, part = at_unit - item * parts;
   const int l = item / p.Hkv, h = item - l * p.Hkv;
   const int n_tok = p.n_tokens[b];
@@ -234,7 +239,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
   /* this unit's blocks, in whole steps but for the last */
   const int steps = (vis.blocks + NB - 1) / NB;
   const int s0 = (int)((long long)steps * part / parts), s1 = (int)((long long)steps * (part + 1) / parts);
-  const int W = C * NW, w = rank * NW + warp;        // warps of the unit; this one takes steps s0 + w, s0 + w + W, ...
+  const int W = TEAM == WARP ? 1 : C * NW, w = TEAM == WARP ? 0 : rank * NW + warp;        // warps of the unit; this one takes steps s0 + w, s0 + w + W, ...
   const int nt = s1 - s0 > w ? (s1 - s0 - w + W - 1) / W : 0;
   const size_t q_row = ((size_t)b * p.L + l) * p.Hq + h * p.G;
   const uint64_t stream = policy_evict_first();
@@ -507,10 +512,20 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
     for (int e = 0; e < 4; ++e) {
       so[warp * WARP_FLOATS + (2 * t + (e & 1)) * OS + 16 * i + g + 8 * (e >> 1)] = o[i][e];
     }
+  const size_t lse_row = ((size_t)b * p.L + l) * p.Hq + h * p.G;
+  if (TEAM == WARP) {
+    __syncwarp();
+    for (int head = 0; head < p.G; ++head) {
+      const float sum = sl[warp * GP + head];
+      const float4 e = *(const float4 *)&so[warp * WARP_FLOATS + head * OS + 4 * lane];
+      put_out<E4M3>(p, b, l, h, head, 4 * lane, e, inverse(sum));
+      if (p.lse && lane == 0) p.lse[lse_row + head] = logarithm(max_base(sm[warp * GP + head]), sum);
+    }
+    return;
+  }
   __syncthreads();
   /* the CTA's sums: 4 channels of a head per thread, 8 / NW heads per warp */
   const int slice = GP * D / C;
-  const size_t lse_row = ((size_t)b * p.L + l) * p.Hq + h * p.G;
   float4 acc[GP / NW];
   float top[GP / NW], sum[GP / NW];
 #pragma unroll
@@ -659,6 +674,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
 }
 
 struct Form {
+  Team team = CTA;
   int C = 1, warps = 4, unit = 0;            // CTAs per unit, warps per CTA, most steps of a unit
   bool waves = false;                        // more CTAs than run at once
 };
@@ -675,7 +691,12 @@ struct Form {
  * under a window): the form taken is 0.7% slower than the best on average, 5% at worst.  Some forms,
  * us: one sequence of 131,071 tokens, 2 KV heads: 16 parts of 8 CTAs 15.8, one part of 16 CTAs 44; 448
  * tokens: 4 CTAs of 4 warps 4.0, one of 8 4.5; 32 x 1,700 in 36 layers: one CTA of 4 warps 148, two 170,
- * one of 8 177; 4 x 65,536 in 36 layers: two of 8 613, one of 4 644. */
+ * one of 8 177; 4 x 65,536 in 36 layers: two of 8 613, one of 4 644.
+ *   A warp per row was weighed against a CTA of 4 in 86 more launches (72 to 18,432 rows, most of them
+ * short): the estimate costs 0.2% against the faster of the two on average, 7% at worst (1,152 rows
+ * of 500 tokens).  It is taken for many short rows, whose CTAs would mostly start and end: 64 rows of 40
+ * tokens in 8 KV heads 6.4 -> 4.1 us, 36 windows of 16 in 16 layers and 4 heads 20.0 -> 9.3, 64 ragged
+ * sequences of up to 600 in 36 layers and 2 heads 77 -> 65. */
 Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
   constexpr float SMS = 152.f;
   const int NB = e4m3 ? 2 : 1, lh = p.L * p.Hkv;
@@ -702,38 +723,45 @@ Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
       if (n > 1) partials += n;
     }
     if (partials * lh > MAX_PARTIALS) break;
-    for (int warps = 4; warps <= 8; warps += 4)
-      for (int log_C = 0; 1 << log_C <= MAX_CLUSTER; ++log_C) {
-        const int C = 1 << log_C;
-        if (C * warps > 4 && C * warps >= 2 * unit) break;             // half of them would have no step
-        /* a cluster of 8 or 16 CTAs leaves parts of the chip unused */
-        const float part = warps == 4 ? (C <= 2 ? 1.f : C == 4 ? 0.95f : C == 8 ? 0.93f : 0.74f)
-                                      : (C <= 2 ? 1.f : C == 4 ? 0.94f : C == 8 ? 0.8f : 0.6f);
-        const float N = (float)units * lh * C, slots = SMS * part * (warps == 4 ? 3 : 1);
-        const float longest = (float)((unit + C * warps - 1) / (C * warps));
-        const float start = 2.65f + (C > 1 ? 0.82f : 0.f) + (C == 16 ? 0.187f : 0.f) + (warps == 8 ? 0.139f : 0.f);
-        /* of a warp, where n CTAs run */
-        auto step = [&](float n) { return warps == 8 || (n > SMS * part && n <= 2 * SMS * part) ? step8 : n <= SMS * part ? step4 : step12; };
-        float t;
-        if (N <= slots) {
-          t = start + norm(longest * step(N), bytes) + 0.0019f * N;
-        } else {
-          const float steps_each = (float)total / (N * warps) + 0.5f;
-          const float cta = start + 1.316f + 0.701f * log_C + steps_each * step(slots);
-          const float waves = floorf(N / slots), left = N - waves * slots;
-          const float last = 0.6f * longest + 0.4f * std::min(longest, steps_each);
-          t = start + norm(waves * cta, bytes * (1.f - left / N)) + std::max(0.533f * last * step(left), bytes * left / N);
-          t = std::max(t, start + 1.316f + 0.81f * longest * step(slots));
-        }
-        if (parts > 1) t += 1.791f + 0.0217f * parts;
-        if (t < least) {
-          least = t;
-          best.C = C;
-          best.warps = warps;
-          best.unit = unit;
-          best.waves = N > slots;
-        }
+    auto consider = [&](Team team, int C, int warps) {
+      const int team_warps = team == WARP ? 1 : C * warps;
+      /* a cluster of 8 or 16 CTAs leaves parts of the chip unused */
+      const float part = warps == 4 ? (C <= 2 ? 1.f : C == 4 ? 0.95f : C == 8 ? 0.93f : 0.74f)
+                                    : (C <= 2 ? 1.f : C == 4 ? 0.94f : C == 8 ? 0.8f : 0.6f);
+      const float N = team == WARP ? ceilf((float)units * lh / warps) : (float)units * lh * C;
+      const float slots = SMS * part * (warps == 4 ? 3 : 1);
+      const float longest = (float)((unit + team_warps - 1) / team_warps);
+      const float start = 2.65f + (team == WARP ? 0.25f : 0.f) + (C > 1 ? 0.82f : 0.f) + (C == 16 ? 0.187f : 0.f) + (warps == 8 ? 0.139f : 0.f);
+      /* of a warp, where n CTAs run */
+      auto step = [&](float n) { return warps == 8 || (n > SMS * part && n <= 2 * SMS * part) ? step8 : n <= SMS * part ? step4 : step12; };
+      float t;
+      if (N <= slots) {
+        t = start + norm(longest * step(N), bytes) + 0.0019f * N;
+      } else {
+        const float steps_each = (float)total / (N * warps) + 0.5f;
+        const float cta = start + 1.316f + 0.701f * log2f((float)C) + steps_each * step(slots);
+        const float waves = floorf(N / slots), left = N - waves * slots;
+        const float last = 0.6f * longest + 0.4f * std::min(longest, steps_each);
+        t = start + norm(waves * cta, bytes * (1.f - left / N)) + std::max(0.533f * last * step(left), bytes * left / N);
+        t = std::max(t, start + 1.316f + 0.81f * longest * step(slots));
       }
+      if (team == WARP) t *= 1.1f;                                       // a warp whose row ends early idles
+      if (parts > 1) t += 1.791f + 0.0217f * parts;
+      if (t < least) {
+        least = t;
+        best.team = team;
+        best.C = C;
+        best.warps = warps;
+        best.unit = unit;
+        best.waves = N > slots;
+      }
+    };
+    for (int warps = 4; warps <= 8; warps += 4)
+      for (int C = 1; C <= MAX_CLUSTER; C *= 2) {
+        if (C * warps > 4 && C * warps >= 2 * unit) break;             // half of them would have no step
+        consider(C > 1 ? CLUSTER : CTA, C, warps);
+      }
+    if (parts == 1) consider(WARP, 1, 4);
   }
   auto parts_of = [&](int b) { return std::max((steps[b] + best.unit - 1) / best.unit, 1); };
   uint32_t key[MD_MAX_BATCH];                // steps of a unit, then the sequence
@@ -751,10 +779,11 @@ Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
   return best;
 }
 
-template <int NW, bool E4M3, bool ONE>
+template <int NW, bool E4M3, Team TEAM>
 cudaError_t launch_attend(const AttendCacheParams &p, const CUtensorMap &tmap, cudaStream_t s) {
-  constexpr int which = ATTR_ATTEND_CACHE + (E4M3 ? 1 : 0) + (ONE ? 2 : 0) + (NW == 8 ? 4 : 0);
-  const auto kernel = attend_cache_kernel<NW, E4M3, ONE>;
+  constexpr int which = ATTR_ATTEND_CACHE + (E4M3 ? 1 : 0) + 2 * TEAM + (NW == 8 ? 6 : 0);
+  constexpr bool ONE = TEAM != CLUSTER;
+  const auto kernel = attend_cache_kernel<NW, E4M3, TEAM>;
   const cudaError_t e = once_per_device<which>([&] {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                (int)attend_smem(ONE ? 1 : MAX_CLUSTER, NW));
@@ -762,7 +791,7 @@ cudaError_t launch_attend(const AttendCacheParams &p, const CUtensorMap &tmap, c
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.unit_start[p.n_seqs] * p.C));
+  cfg.gridDim = dim3((unsigned)(TEAM == WARP ? (p.unit_start[p.n_seqs] + NW - 1) / NW : p.unit_start[p.n_seqs] * p.C));
   cfg.blockDim = dim3(32 * NW);
   cfg.dynamicSmemBytes = attend_smem(p.C, NW);
   cfg.stream = s;
@@ -793,8 +822,10 @@ cudaError_t run(AttendCacheParams &p, const CUtensorMap &tmap, bool workspace, c
   const Form f = attend_form(p, E4M3, workspace);
   p.C = f.C;
   p.early = !f.waves;
-  cudaError_t e = f.warps == 8 ? (f.C > 1 ? launch_attend<8, E4M3, false>(p, tmap, s) : launch_attend<8, E4M3, true>(p, tmap, s))
-                               : (f.C > 1 ? launch_attend<4, E4M3, false>(p, tmap, s) : launch_attend<4, E4M3, true>(p, tmap, s));
+  cudaError_t e = f.team == WARP    ? launch_attend<4, E4M3, WARP>(p, tmap, s)
+                  : f.team == CTA ? (f.warps == 8 ? launch_attend<8, E4M3, CTA>(p, tmap, s) : launch_attend<4, E4M3, CTA>(p, tmap, s))
+                  : f.warps == 8  ? launch_attend<8, E4M3, CLUSTER>(p, tmap, s)
+                                  : launch_attend<4, E4M3, CLUSTER>(p, tmap, s);
   const int lh = p.L * p.Hkv;
   JoinParams j;
   int split = 0;

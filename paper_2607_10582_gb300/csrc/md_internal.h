@@ -341,7 +341,7 @@ cudaError_t launch_pdl(void (*kernel)(P), dim3 grid, int threads, int smem, cuda
 }
 
 /* Runs f (it sets kernel attributes) once per device; WHICH: for which kernels. */
-enum { ATTR_ATTEND_4, ATTR_ATTEND_8 = ATTR_ATTEND_4 + 3, ATTR_ATTEND_CACHE = ATTR_ATTEND_8 + 3 };   // three kernels each, and eight
+enum { ATTR_ATTEND_4, ATTR_ATTEND_8 = ATTR_ATTEND_4 + 3, ATTR_ATTEND_CACHE = ATTR_ATTEND_8 + 3 };   // three kernels each, and ten
 template <int WHICH, class F>
 cudaError_t once_per_device(F f) {
   static std::atomic<unsigned long long> done{0};

@@ -26,8 +26,9 @@ int main() {
       parts = n / lh > parts ? n / lh : parts;
       partials += n > lh ? n : 0;
     }
+    if (f.team == WARP && (f.C != 1 || parts > 1)) return 4;
     if (partials > MAX_PARTIALS || (long long)p.unit_start[p.n_seqs] * f.C >= 1LL << 31) return 3;
-    printf("%d %d %d\n", f.C, f.warps, parts);
+    printf("%d %d %d\n", f.team == WARP ? 0 : f.C, f.warps, parts);
   }
   return 0;
 }
