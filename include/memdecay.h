@@ -668,8 +668,8 @@ md_status md_read_cache8(const md_cache8_args *args);
  * read, and what lies in other slots, NaN included, has no part in the result.  A
  * sequence without visible tokens yields zeros, and -inf as its logarithm.  Pages whose
  * block-table entry lies outside the pool are taken for pages without tokens.
- *   E4M3  the softmax weights enter the product with V rounded to 11 bits (f16; those below
- *         2^-19 of the largest to a multiple of 2^-29 of it), the queries as f16 relative to
+ *   E4M3  the softmax weights enter the product with V as two f16 terms each: 22 bits, or a multiple of
+ *         2^-29 of the largest where that is coarser; the queries as f16 relative to
  *         the head's largest element: exactly, but for elements below 2^-29 of it
  *   BF16  the weights enter as two bf16 terms each.  Infinite values of one sign make their
  *         channel infinite, whatever their tokens' weights
