@@ -648,7 +648,10 @@ typedef struct {
  * even; what is not finite becomes NaN (0x7f).  In a block that held tokens before, as a decode
  * step's mostly does, s is at least its scale until then; where that grows, the codes of the
  * tokens before are moved to it: exactly, but for those that fall below 2^-6 s, which are
- * rounded once more.  Slots behind the new tokens are left as they are.
+ * rounded once more.
+ * The call appends, or goes on from an earlier token than the last: what the last block held
+ * behind the new tokens is lost.  Its codes there stay, but they stand for other values, as the
+ * block's scale may be another one.
  * The slots of a block before first_host[b] must have been written.  A page that the call
  * writes is one sequence's, once in its table.  Rows whose block-table entry lies outside the
  * pool are not written. */

@@ -528,7 +528,8 @@ def _cache8(call, written: bool, k, v, pool, scales, block_table, first, count, 
 def md_write_cache8(k, v, pool, scales, block_table, first, count, *, stream=None):
     """Writes rows into a cache in eight bits: of each sequence, count[b] tokens from position
     first[b] on.  A block of 16 tokens of a layer, KV head, and K or V has one scale, a power of two;
-    a block that holds tokens already keeps it or moves to a larger one; see md_write_cache8 in the header.
+    a block that holds tokens already keeps it or moves to a larger one; what the last block held behind the
+    new tokens is lost; see md_write_cache8 in the header.
       k, v         [rows][L][Hkv][128] bf16, f16 or f32, any strides over rows, layers and heads: the
                    sequences' tokens one after the other (rows behind them are not read)
       pool         e4m3 (or its raw bits, uint8) [L][pages][Hkv][2][page_size][128]; written
