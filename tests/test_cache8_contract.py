@@ -3,10 +3,21 @@ import numpy as np
 import pytest
 
 import paper_2607_10582_gb300 as md
-from tests.test_cache8 import D, Store, _need_gpu, decode
+from tests.test_cache8 import D, Store, _need_gpu, decode, encode
 
 torch = pytest.importorskip("torch")
 gpu = pytest.mark.gpu
+
+
+def test_the_reference_rounds_general_values_as_torch_does():
+    """Against another implementation of the format, value for value, on inputs that 32 bits hold:
+    ordinary ones, subnormal ones, those that become zero, and the largest."""
+    r = np.random.default_rng(0)
+    for size in (60.0, 1.0, 2.0 ** -6, 2.0 ** -9, 2.0 ** -12):
+        x = torch.from_numpy(r.standard_normal(20000) * size).clamp(-448, 448).float()
+        want = x.to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+        assert np.array_equal(encode(x.double().numpy()), want), size
+    assert encode(np.array([448.0, -448.0, 0.0, -0.0])).tolist() == [126, 254, 0, 128]
 
 
 @gpu
