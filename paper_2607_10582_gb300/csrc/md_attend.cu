@@ -32,7 +32,8 @@ struct AttendCacheParams : PageSet {
   float *lse;                                // or null
   float *partials;                           // of rows that are split over units
   float scale_log2;                          // log2(e) / sqrt(D)
-  long long limit_ns;
+  long long limit_ns;                        // of the wait for a copy
+  int lost_step;                             // of a warp, taken for one that did not land; -1: none
   int window, sinks;                         // window: INT_MAX for all
   int C;                                     // CTAs per unit
   int early;                                 // all CTAs run at once: their first pages go to L2 ahead of the wait
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
       }
     }
     const uint32_t st = ring + (k & (ST - 1)) * STEP_BYTES, bar = bars + (k & (ST - 1)) * 8, parity = k / ST & 1;
-    landed = mbar_try_wait(bar, parity) || wait_copy(bar, parity, p.limit_ns);
+    landed = k != p.lost_step && (mbar_try_wait(bar, parity) || wait_copy(bar, parity, p.limit_ns));
     if (!__all_sync(0xffffffffu, landed)) {
       landed = false;
       break;
@@ -849,14 +850,8 @@ cudaError_t run(AttendCacheParams &p, const CUtensorMap &tmap, bool workspace, c
   return e;
 }
 
-}  // namespace
-
-}  // namespace md
-
-#define MD_API extern "C" __attribute__((visibility("default")))
-
-MD_API md_status md_attend_cache(const md_attend_cache_args *args) {
-  using namespace md;
+/* A wait for a copy gives up after limit_ns; lost_step: as above, for tests. */
+md_status attend_cache(const md_attend_cache_args *args, long long limit_ns = 2000000000LL, int lost_step = -1) {
   if (!args) return MD_ERR_INVALID_ARG;
   const md_attend_cache_args &a = *args;
   AttendCacheParams p;
@@ -877,7 +872,8 @@ MD_API md_status md_attend_cache(const md_attend_cache_args *args) {
   p.lse = a.lse_dev;
   p.partials = (float *)a.workspace_dev;
   p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
-  p.limit_ns = 2000000000LL;
+  p.limit_ns = limit_ns;
+  p.lost_step = lost_step;
   p.window = a.window < 0 ? INT32_MAX : a.window;
   p.sinks = a.sinks;
   void *encode = tile_encoder();
@@ -889,4 +885,12 @@ MD_API md_status md_attend_cache(const md_attend_cache_args *args) {
   const cudaStream_t s = (cudaStream_t)a.stream;
   const bool workspace = a.workspace_dev != nullptr;
   return (e4m3 ? run<true>(p, tmap, workspace, s) : run<false>(p, tmap, workspace, s)) == cudaSuccess ? MD_OK : MD_ERR_CUDA;
+}
+
+}  // namespace
+
+}  // namespace md
+
+extern "C" __attribute__((visibility("default"))) md_status md_attend_cache(const md_attend_cache_args *args) {
+  return md::attend_cache(args);
 }
