@@ -25,7 +25,13 @@ __device__ __forceinline__ long long globaltimer() {
  * and its memory is visible; each kernel calls it before its first access to
  * global memory (a warp that makes none may leave without it, but never all of
  * them), so a kernel completes only after its predecessor has.  pdl_trigger() lets the next kernel be
- * scheduled (it then waits in its own pdl_wait()). */
+ * scheduled (it then waits in its own pdl_wait()).
+ *   Two kernels read ahead of the wait.  attend_cache_kernel reads the block table to prefetch pages: what it
+ * reads may be about to change, so it serves as a hint only, is checked against the pool, and
+ * the table is read again behind the wait.  The cluster attention, in the layers after a step's first one, reads
+ * table entries and pages that were complete before that first layer's launch.  Both need that
+ * no kernel calls pdl_trigger() before its own pdl_wait(): then only the kernel ahead is still
+ * running, and what came before it in the stream, allocations included, is done. */
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
