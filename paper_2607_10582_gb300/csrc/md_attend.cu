@@ -253,8 +253,9 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 3 : 1)
   /* While the launch before ends: the pages of the first steps go into L2, by the table as it is
    * now.  Only where to look depends on it, so that an entry that is about to change costs a useless
    * copy; the table is read again behind the wait (and past L1 here, which would keep what it read).
-   * One layer of 131,071 tokens 15.8 -> 15.0 us, 8 x 13,001 13.2 -> 12.3, 8 x 32,768 in bf16 in 4 layers
-   * under a window of 1,000 9.4 -> 8.3.  Where CTAs come in waves it gains nothing. */
+   * One layer of 131,071 tokens 16.6 -> 15.9 us, 8 x 13,001 13.8 -> 13.1, 8 x 32,768 in bf16 in 4 layers
+   * under a window of 1,000 9.4 -> 8.4; some launches lose: 1 x 20,000 8.5 -> 9.0, 32 x 1,700 8.4 -> 8.8.  Where CTAs
+   * come in waves it gains nothing. */
   if (p.early) {
     const int i = (s0 + w + W * (lane / NB)) * NB + (lane & (NB - 1));
     if (lane / NB < min(ST, nt) && i < vis.blocks) {
@@ -697,18 +698,20 @@ struct Form {
  * longest one's steps and the bytes at the copy rate both bound the time (their 4-norm: near each
  * other, neither hides the other); with several waves, the CTAs' summed time and the bytes, and a
  * last wave of the CTAs that are left, which are shorter ones: then the longest rows go first (16
- * ragged sequences of up to 4,001 tokens in 36 layers 130.8 -> 127.4 us).
+ * sequences of 2,000 to 4,001 tokens in 36 layers 134.1 -> 131.2 us).
  *   The constants were fitted to 91 launches timed on a GB300 in up to 45 forms each (1 to 128
  * sequences, 1 to 36 layers, 1 to 8 KV heads, 100 to 131,071 tokens, both types, a third of them ragged or
- * under a window): the form taken is 0.7% slower than the best on average, 5% at worst.  Some forms,
- * us: one sequence of 131,071 tokens, 2 KV heads: 16 parts of 8 CTAs 15.8, one part of 16 CTAs 44; 448
- * tokens: 4 CTAs of 4 warps 4.0, one of 8 4.5; 32 x 1,700 in 36 layers: one CTA of 4 warps 148, two 170,
- * one of 8 177; 4 x 65,536 in 36 layers: two of 8 613, one of 4 644.
- *   A warp per row was weighed against a CTA of 4 in 86 more launches (72 to 18,432 rows, most of them
- * short): the estimate costs 0.2% against the faster of the two on average, 7% at worst (1,152 rows
- * of 500 tokens).  It is taken for many short rows, whose CTAs would mostly start and end: 64 rows of 40
- * tokens in 8 KV heads 6.4 -> 4.1 us, 36 windows of 16 in 16 layers and 4 heads 20.0 -> 9.3, 64 ragged
- * sequences of up to 600 in 36 layers and 2 heads 77 -> 65. */
+ * under a window), and a warp per row was weighed against a CTA of 4 in 86 more (72 to 18,432 rows, most of them
+ * short), while the weights over E4M3 were one f16 term; with two a launch takes up to 9% longer.
+ * All 177 were then timed again, each in its 25 fastest forms: the one taken is 0.9% slower than the
+ * best on average, more than 5% in 12 of them, 14% at worst (512 rows of 150 tokens in bf16: CTAs 11.3 us, warps
+ * 9.9); profiles/attend_cache_forms.csv has them.  Some forms, us: one sequence of 131,071 tokens, 2 KV heads: 16 parts,
+ * each a cluster of 4 CTAs of 8 warps, which is taken, 15.9, of 8 of 4 warps 15.9, one part of 16 CTAs of 8 37; 448
+ * tokens: 4 CTAs of 4 warps, taken, 4.1, 8 4.3, one of 8 warps 4.7; 32 x 1,700 in 36 layers: one CTA of 4 warps, taken,
+ * 118, two 146, one of 8 152; 4 x 65,536 in 36 layers: one of 8, taken, 615, two of 8 623, one of 4 659.
+ *   A warp per row is taken for many short rows, whose CTAs would mostly start and end: 64 rows of 40
+ * tokens in 8 KV heads 6.9 -> 4.4 us, 36 windows of 16 in 16 layers and 4 heads 21.1 -> 9.8, 64 sequences of
+ * 120 to 600 in 36 layers and 2 heads 82 -> 69. */
 Form attend_form(AttendCacheParams &p, bool e4m3, bool workspace) {
   constexpr float SMS = 152.f;
   const int NB = e4m3 ? 2 : 1, lh = p.L * p.Hkv;
